@@ -1,4 +1,4 @@
-"""Thin ctypes binding of include/hps_cache.h, hps_lookup.h and hps_dedup.h: argument marshalling only.
+"""Thin ctypes binding of include/hps_cache.h, hps_lookup.h, hps_dedup.h and hps_seq.h: argument marshalling only.
 
 Every function has the name of the C entry point it calls.  Tensors are torch CUDA (ROCm)
 tensors used purely as device buffers; `stream` is a torch.cuda.Stream or None (= the current
@@ -7,6 +7,7 @@ has not been built, loading raises.
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -37,6 +38,9 @@ EXPORTS = (
     "hps_hostmap_create", "hps_hostmap_destroy", "hps_hostmap_put", "hps_hostmap_get", "hps_hostmap_fetch",
     "hps_hostmap_stats",
     "hps_membench_gather", "hps_membench_gather_half", "hps_membench_copy",
+    "hps_seq_extend", "hps_seq_release", "hps_seq_rope_table", "hps_seq_rope", "hps_seq_append",
+    "hps_seq_attention_create", "hps_seq_attention_destroy", "hps_seq_attention", "hps_seq_attention_flags",
+    "hps_seq_last_error",
 )
 
 # lower-tier fetch callback of hps_lookup.h: (user, keys*, n, rows*)
@@ -62,13 +66,15 @@ def load_library():
             f"{LIB_PATH} is missing: build the HIP extension first "
             "(python -c 'import __graft_entry__ as g; g.build()'); there is no CPU fallback")
     lib = C.CDLL(LIB_PATH)
-    vp, sz, u32 = C.c_void_p, C.c_size_t, C.c_uint32
+    vp, sz, u32, f64 = C.c_void_p, C.c_size_t, C.c_uint32, C.c_double
     lib.hps_last_error.restype = C.c_char_p
     lib.hps_last_error.argtypes = []
     lib.hps_lookup_last_error.restype = C.c_char_p
     lib.hps_lookup_last_error.argtypes = []
     lib.hps_dedup_last_error.restype = C.c_char_p
     lib.hps_dedup_last_error.argtypes = []
+    lib.hps_seq_last_error.restype = C.c_char_p
+    lib.hps_seq_last_error.argtypes = []
     sigs = {
         "hps_cache_create": [sz, u32, u32, C.POINTER(vp)],
         "hps_cache_create_policy": [sz, u32, u32, C.c_int, C.POINTER(vp)],
@@ -100,6 +106,15 @@ def load_library():
         "hps_membench_gather": [vp, vp, sz, u32, vp, vp],
         "hps_membench_gather_half": [vp, vp, sz, vp, C.c_int, vp],
         "hps_membench_copy": [vp, vp, sz, C.c_int, vp],
+        "hps_seq_extend": [vp, vp],
+        "hps_seq_release": [vp, vp, u32, u32, vp, u32, vp, u32, vp, vp, vp],
+        "hps_seq_rope_table": [vp, u32, u32, f64, C.c_int, f64, f64, f64, f64, f64, vp],
+        "hps_seq_rope": [vp, vp],
+        "hps_seq_append": [vp, vp],
+        "hps_seq_attention_create": [sz, u32, C.POINTER(vp)],
+        "hps_seq_attention_destroy": [vp],
+        "hps_seq_attention": [vp, vp, vp],
+        "hps_seq_attention_flags": [vp, C.POINTER(u32), C.c_int],
         "hps_cache_destroy": [vp],
         "hps_cache_query": [vp, vp, sz, vp, vp, vp, vp, vp],
         "hps_cache_insert": [vp, vp, vp, sz, vp],
@@ -476,3 +491,220 @@ def hps_hostmap_fetch(m, keys, dim: int):
     rows = np.empty((keys.shape[0], dim), dtype=np.float32)
     load_library().hps_hostmap_fetch(m, keys.ctypes.data, keys.shape[0], rows.ctypes.data)
     return rows
+
+
+# ---- hps_seq.h: pages of keys and values, rotary positions, attention behind shared histories
+
+HPS_SEQ_F32, HPS_SEQ_F16, HPS_SEQ_BF16 = 0, 1, 2
+HPS_SEQ_SCALE_NONE, HPS_SEQ_SCALE_LINEAR, HPS_SEQ_SCALE_PARTS = 0, 1, 2
+HPS_SEQ_FLAG_LENGTH, HPS_SEQ_FLAG_BLOCK = 1, 2
+
+_SEQ_DTYPES = {torch.float32: HPS_SEQ_F32, torch.float16: HPS_SEQ_F16, torch.bfloat16: HPS_SEQ_BF16}
+# The argument structures of hps_seq.h, packed in native layout: a pointer or a 64-bit stride per P and q.
+_SEQ_EXTEND = struct.Struct("@11P5I0P")
+_SEQ_ROPE = struct.Struct("@PqqPqqPqqPqqPP6I3i0P")
+_SEQ_APPEND = struct.Struct("@PqqPqqPqqPqqPPqqqIIPPP6I2i0P")
+_SEQ_ATTENTION = struct.Struct("@PqqPqqPPqqqII7P12Iif0P")
+
+
+def _check_seq(status):
+    if status != HPS_OK:
+        raise HpsError(status, load_library().hps_seq_last_error().decode())
+
+
+def hps_seq_last_error() -> str:
+    return load_library().hps_seq_last_error().decode()
+
+
+def _ints(t, name, shape=None):
+    """Address of a contiguous int32 array; 0 for None."""
+    if t is None:
+        return 0
+    if not t.is_cuda:
+        raise TypeError(f"{name}: device tensor expected")
+    if t.dtype is not _int32:
+        raise TypeError(f"{name}: expected {_int32}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous tensor expected")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _word(t, name):
+    """Address of the first of one or more int32."""
+    if t.numel() < 1:
+        raise ValueError(f"{name}: one number at least")
+    return _ints(t, name)
+
+
+def _heads(t, name, dtype, tokens, heads, dim):
+    """(address, token stride, head stride) of a tensor [tokens, heads, dim] whose heads are each in one piece."""
+    if not t.is_cuda:
+        raise TypeError(f"{name}: device tensor expected")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != (tokens, heads, dim):
+        raise ValueError(f"{name}: expected shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
+    st, sh, sd = t.stride()
+    if sd != 1 and dim > 1:
+        raise ValueError(f"{name}: the values of a head must be adjacent")
+    return t.data_ptr(), st, sh
+
+
+def _pages(k, v, dtype):
+    """(k, v, block stride, token stride, head stride, blocks, block size) of pages [blocks, block size, heads, dim]."""
+    if not (k.is_cuda and v.is_cuda):
+        raise TypeError("k_pages, v_pages: device tensors expected")
+    if k.dtype is not dtype or v.dtype is not dtype:
+        raise TypeError(f"k_pages, v_pages: expected {dtype}, got {k.dtype} and {v.dtype}")
+    if k.dim() != 4 or k.shape != v.shape:
+        raise ValueError("k_pages, v_pages: expected two tensors [blocks, block size, heads, dim]")
+    stride = k.stride()
+    if stride != v.stride():
+        raise ValueError("k_pages and v_pages must have the same strides")
+    if stride[3] != 1 and k.shape[3] > 1:
+        raise ValueError("k_pages, v_pages: the values of a head must be adjacent")
+    return k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], k.shape[0], k.shape[1]
+
+
+def _dtype_of(t):
+    try:
+        return _SEQ_DTYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"expected float32, float16 or bfloat16, got {t.dtype}") from None
+
+
+def _rope_table_of(table):
+    """(address, positions, values turned) of a table [positions, rot / 2, 2]."""
+    if table is None:
+        return 0, 0, 0
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table: expected a tensor [positions, rot / 2, 2]")
+    return _ptr(table, _float32), table.shape[0], 2 * table.shape[1]
+
+
+def hps_seq_extend(past_lens, new_lens, block_size, free_blocks, n_free, block_table, token_offsets, total_lens, slots, positions, info,
+                   start=None, stream=None) -> None:
+    """Pages for new_lens[r] more tokens of each request: block_table int32 [requests, width] (in and out), free_blocks int32 [blocks], n_free one
+    int32; slots and positions int32 [max tokens], token_offsets int32 [requests + 1], total_lens int32 [requests], info int32 [4]."""
+    n, = past_lens.shape
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("block_table: expected a tensor [requests, width]")
+    most, = slots.shape
+    args = _SEQ_EXTEND.pack(
+        _ints(past_lens, "past_lens"), _ints(new_lens, "new_lens", (n,)), _ints(start, "start", (n,)), _ints(free_blocks, "free_blocks"),
+        _word(n_free, "n_free"), _ints(block_table, "block_table"), _ints(token_offsets, "token_offsets", (n + 1,)),
+        _ints(total_lens, "total_lens", (n,)), _ints(slots, "slots"), _ints(positions, "positions", (most,)), _ints(info, "info", (4,)),
+        n, block_size, free_blocks.numel(), block_table.shape[1], most)
+    status = (_lib or load_library()).hps_seq_extend(args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_release(lens, finished, block_size, block_table, free_blocks, n_free, info, stream=None) -> None:
+    """The blocks of the requests with finished[r] != 0 go back to the free list; n_free may be info[:1]."""
+    n, = lens.shape
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("block_table: expected a tensor [requests, width]")
+    _check_seq(load_library().hps_seq_release(
+        _ints(lens, "lens"), _ints(finished, "finished", (n,)), n, block_size, _ints(block_table, "block_table"), block_table.shape[1],
+        _ints(free_blocks, "free_blocks"), free_blocks.numel(), _word(n_free, "n_free"), _ints(info, "info", (4,)), _stream(stream)))
+
+
+def hps_seq_rope_table(table, base=10000.0, scale=HPS_SEQ_SCALE_NONE, factor=1.0, original=1.0, low=1.0, high=2.0, magnitude=1.0, stream=None) -> None:
+    """Writes table float32 [positions, rot / 2, 2]: cosines and sines."""
+    p, n, rot = _rope_table_of(table)
+    _check_seq(load_library().hps_seq_rope_table(p, n, rot, base, scale, factor, original, low, high, magnitude, _stream(stream)))
+
+
+def hps_seq_rope(q, q_out, positions, table, k=None, k_out=None, interleaved=False, inverse=False, stream=None) -> None:
+    """q, q_out [tokens, heads, dim] (and k, k_out with heads of their own) turned by table[positions]; inverse: the gradient."""
+    T, H, D = q.shape
+    dtype = q.dtype
+    address, n, rot = _rope_table_of(table)
+    none, hk = (0, 0, 0), 0
+    if k is not None:
+        hk = k.shape[1]
+    args = _SEQ_ROPE.pack(
+        *_heads(q, "q", dtype, T, H, D), *(_heads(k, "k", dtype, T, hk, D) if k is not None else none), *_heads(q_out, "q_out", dtype, T, H, D),
+        *(_heads(k_out, "k_out", dtype, T, hk, D) if k is not None else none), _ints(positions, "positions", (T,)), address,
+        T, H, hk, D, rot, n, _dtype_of(q), bool(interleaved), bool(inverse))
+    status = (_lib or load_library()).hps_seq_rope(args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_append(k, v, k_pages, v_pages, slots, q=None, q_out=None, positions=None, table=None, interleaved=False, stream=None) -> None:
+    """Keys (turned, with a table) and values [tokens, kv heads, dim] to slots of pages [blocks, block size, kv heads, dim]; queries
+    [tokens, heads, dim] turned into q_out."""
+    T, hk, D = k.shape
+    dtype = k.dtype
+    address, n, rot = _rope_table_of(table)
+    none, H = (0, 0, 0), 0
+    if q is not None:
+        H = q.shape[1]
+    pages = _pages(k_pages, v_pages, dtype)
+    if k_pages.shape[2:] != (hk, D):
+        raise ValueError("k_pages, v_pages: heads and dim differ from the keys'")
+    if table is not None and positions is None:
+        raise ValueError("positions: needed with a table")
+    args = _SEQ_APPEND.pack(
+        *(_heads(q, "q", dtype, T, H, D) if q is not None else none), *(_heads(q_out, "q_out", dtype, T, H, D) if q is not None else none),
+        *_heads(k, "k", dtype, T, hk, D), *_heads(v, "v", dtype, T, hk, D), *pages, _ints(slots, "slots", (T,)), _ints(positions, "positions", (T,)), address,
+        T, H, hk, D, rot, n, _dtype_of(k), bool(interleaved))
+    status = (_lib or load_library()).hps_seq_append(args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_attention_create(max_rows: int, max_head_dim: int) -> int:
+    """max_rows: tokens * query heads of the largest call."""
+    h = C.c_void_p()
+    _check_seq(load_library().hps_seq_attention_create(max_rows, max_head_dim, C.byref(h)))
+    return h.value
+
+
+def hps_seq_attention_destroy(session) -> None:
+    _check_seq(load_library().hps_seq_attention_destroy(session))
+
+
+def hps_seq_attention_flags(session, clear: bool = False) -> int:
+    f = C.c_uint32()
+    _check_seq(load_library().hps_seq_attention_flags(session, C.byref(f), 1 if clear else 0))
+    return f.value
+
+
+def hps_seq_attention(session, q, k_pages, v_pages, block_table, lens, token_offsets, out, prefix_table=None, prefix_lens=None, group_offsets=None,
+                      lse=None, scale=None, max_new=None, max_len=None, max_prefix=None, max_group=None, stream=None) -> None:
+    """q, out [tokens, heads, dim]; pages [blocks, block size, kv heads, dim]; block_table int32 [requests, width], lens int32 [requests],
+    token_offsets int32 [requests + 1]; prefix_table int32 [groups, width], prefix_lens int32 [groups], group_offsets int32 [groups + 1]; lse float32
+    [tokens, heads].  The bounds max_new, max_len, max_prefix and max_group are, where they are not given, the most that the shapes allow.
+    scale: 1 / sqrt(dim) if None."""
+    T, H, D = q.shape
+    dtype = q.dtype
+    pages = _pages(k_pages, v_pages, dtype)
+    hk, block = k_pages.shape[2], pages[6]
+    if k_pages.shape[3] != D:
+        raise ValueError("k_pages, v_pages: dim differs from the queries'")
+    n, = lens.shape
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("block_table: expected a tensor [requests, width]")
+    width, groups, prefix_width = block_table.shape[1], 0, 0
+    if prefix_lens is not None:
+        groups, = prefix_lens.shape
+        if prefix_table is None or group_offsets is None or prefix_table.dim() != 2 or prefix_table.shape[0] != groups:
+            raise ValueError("prefix_table: expected a tensor [groups, width], and group_offsets with it")
+        prefix_width = prefix_table.shape[1]
+    if lse is not None and lse.shape != (T, H):
+        raise ValueError(f"lse: expected shape {(T, H)}, got {tuple(lse.shape)}")
+    args = _SEQ_ATTENTION.pack(
+        *_heads(q, "q", dtype, T, H, D), *_heads(out, "out", dtype, T, H, D), *pages, _ints(prefix_table, "prefix_table") if groups else 0,
+        _ints(prefix_lens, "prefix_lens") if groups else 0, _ints(group_offsets, "group_offsets", (groups + 1,)) if groups else 0,
+        _ints(block_table, "block_table"), _ints(lens, "lens"), _ints(token_offsets, "token_offsets", (n + 1,)), _ptr(lse, _float32) or 0,
+        T, n, groups, width, prefix_width, T if max_new is None else max_new, T if max_group is None else max_group,
+        width * block if max_len is None else max_len, prefix_width * block if max_prefix is None else max_prefix, H, hk, D,
+        _dtype_of(q), D ** -0.5 if scale is None else scale)
+    status = (_lib or load_library()).hps_seq_attention(session, args, _stream(stream))
+    if status:
+        _check_seq(status)

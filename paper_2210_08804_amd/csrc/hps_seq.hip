@@ -1,0 +1,596 @@
+// Pages of sequence models: block tables and slots from lengths, rotary positions, keys and values written to their
+// pages (hps_seq.h), for gfx950.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+#include <type_traits>
+
+#include "hps_seq_common.h"
+
+namespace {
+
+thread_local char g_err[256];
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+// ---- extend and release -------------------------------------------------------------------
+//
+// Everything follows from two exclusive sums over the requests: of their new tokens, and of their new blocks.  A
+// work-group takes a chunk of 4,096 requests, adds up what all requests in front of it have (nobody waits for anybody:
+// the lengths are few and in the caches, and reading them again costs less than a second launch or a chain of
+// work-groups), scans its own into LDS, and writes its share of the chunk's tokens and blocks, each found by a binary
+// search in LDS.
+constexpr uint32_t kThreads = 1024, kChunk = 4096, kPer = kChunk / kThreads, kWaves = kThreads / 64;
+constexpr uint32_t kMaxSum = 0x7FFFFFFFu;
+
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+struct Sums {                                          // saturating sums are associative, so they scan like any other
+    uint32_t tokens, blocks, over;
+    __device__ __forceinline__ void add(const Sums &o) {
+        tokens = add_sat(tokens, o.tokens);
+        blocks = add_sat(blocks, o.blocks);
+        over = add_sat(over, o.over);
+    }
+};
+
+// One request: its kept tokens, and what it adds.
+struct Request {
+    uint32_t past, fresh, fit, kept, blocks;
+    __device__ __forceinline__ Request(int32_t p, int32_t n, uint32_t cap, uint32_t sh) {
+        const uint32_t round = (1u << sh) - 1u;
+        past = min((uint32_t)max(p, 0), cap);
+        fresh = (uint32_t)max(n, 0);
+        fit = min(fresh, cap - past);
+        kept = (past + round) >> sh;
+        blocks = ((past + fit + round) >> sh) - kept;
+    }
+    __device__ __forceinline__ Sums sums() const { return {fresh, blocks, fresh - fit}; }
+};
+
+// Exclusive scan over the work-group; `total` receives the sum of all.
+__device__ __forceinline__ Sums scan(Sums mine, Sums *l_wave, Sums &total) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    Sums inc = mine;
+    for (uint32_t d = 1; d < 64; d <<= 1) {
+        Sums o{(uint32_t)__shfl_up((int)inc.tokens, d), (uint32_t)__shfl_up((int)inc.blocks, d), (uint32_t)__shfl_up((int)inc.over, d)};
+        if (lane >= d) inc.add(o);
+    }
+    if (lane == 63) l_wave[wave] = inc;
+    Sums exc{(uint32_t)__shfl_up((int)inc.tokens, 1), (uint32_t)__shfl_up((int)inc.blocks, 1), (uint32_t)__shfl_up((int)inc.over, 1)};
+    if (lane == 0) exc = {0, 0, 0};
+    __syncthreads();
+    Sums before{0, 0, 0};
+    total = {0, 0, 0};
+    for (uint32_t w = 0; w < blockDim.x / 64; ++w) {
+        if (w == wave) before = total;
+        total.add(l_wave[w]);
+    }
+    before.add(exc);
+    __syncthreads();
+    return before;
+}
+
+// The last i < n with first[i] <= x, where first[0] <= x < first[n].
+__device__ __forceinline__ uint32_t find(const uint32_t *first, uint32_t n, uint32_t x) {
+    uint32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (first[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+struct ExtendArgs {
+    hps_seq_extend_args_t a;
+    uint32_t sh, cap;                                  // log2 of the block size; tokens that a table holds
+};
+
+__device__ __forceinline__ int32_t new_block(const ExtendArgs &e, uint32_t n_free, uint32_t k) {
+    const int32_t id = k < n_free ? e.a.free_blocks[n_free - 1u - k] : -1;
+    return (uint32_t)id < e.a.n_blocks ? id : -1;
+}
+
+__global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs e) {
+    __shared__ uint32_t l_tok[kChunk + 1], l_blk[kChunk + 1];
+    __shared__ Sums l_wave[kWaves];
+    const hps_seq_extend_args_t &a = e.a;
+    const uint32_t tid = threadIdx.x, r0 = blockIdx.y * kChunk, mine = min(kChunk, a.n_requests - r0);
+    const bool last_chunk = blockIdx.y == gridDim.y - 1;
+    const uint32_t n_free = (uint32_t)min(max(*a.n_free, 0), (int32_t)a.n_blocks);
+
+    Sums front{0, 0, 0};
+    for (uint32_t r = tid; r < r0; r += kThreads) front.add(Request(a.past_lens[r], a.new_lens[r], e.cap, e.sh).sums());
+    Sums part[kPer], sum{0, 0, 0};
+    uint32_t past_fit[kPer];
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) {
+        const uint32_t r = r0 + tid * kPer + i;
+        const bool there = tid * kPer + i < mine;
+        const Request q(there ? a.past_lens[r] : 0, there ? a.new_lens[r] : 0, e.cap, e.sh);
+        part[i] = q.sums();
+        past_fit[i] = q.past + q.fit;
+        sum.add(part[i]);
+    }
+    Sums total, at = scan(sum, l_wave, total);
+    if (r0) {                                          // uniform
+        Sums all;
+        (void)scan(front, l_wave, all);
+        at.add(all);
+        total.add(all);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) {
+        const uint32_t j = tid * kPer + i;
+        if (j < mine) {
+            l_tok[j] = at.tokens;
+            l_blk[j] = at.blocks;
+            if (blockIdx.x == 0) {
+                a.token_offsets[r0 + j] = (int32_t)min(at.tokens, kMaxSum);
+                a.total_lens[r0 + j] = (int32_t)past_fit[i];
+            }
+        }
+        at.add(part[i]);
+    }
+    if (tid == 0) {
+        l_tok[mine] = total.tokens;
+        l_blk[mine] = total.blocks;
+        if (last_chunk && blockIdx.x == 0) {
+            const uint32_t taken = min(total.blocks, n_free);
+            a.token_offsets[a.n_requests] = (int32_t)min(total.tokens, kMaxSum);
+            a.info[0] = (int32_t)(n_free - taken);
+            a.info[1] = (int32_t)min(total.tokens, kMaxSum);
+            a.info[2] = (int32_t)min(total.blocks - taken, kMaxSum);
+            a.info[3] = (int32_t)min(total.over, kMaxSum);
+        }
+    }
+    __syncthreads();
+
+    const uint32_t stride = gridDim.x * kThreads, first = blockIdx.x * kThreads + tid;
+    for (uint64_t k = l_blk[0] + (uint64_t)first; k < l_blk[mine]; k += stride) {
+        const uint32_t i = find(l_blk, mine, (uint32_t)k), r = r0 + i;
+        const Request q(a.past_lens[r], a.new_lens[r], e.cap, e.sh);
+        a.block_table[(size_t)r * a.table_width + q.kept + ((uint32_t)k - l_blk[i])] = new_block(e, n_free, (uint32_t)k);
+    }
+    // Tokens in fours, 16 bytes a store; the first and the last four of a chunk may belong to its neighbours in part.
+    const uint32_t t_begin = min(l_tok[0], a.max_tokens), t_end = min(l_tok[mine], a.max_tokens), t_all = last_chunk ? a.max_tokens : t_end;
+    const bool wide = (((uintptr_t)a.slots | (uintptr_t)a.positions) & 15u) == 0;
+    for (uint64_t g = (t_begin >> 2) + (uint64_t)first; g * 4 < t_all; g += stride) {
+        i32x4 slot, pos;
+        uint32_t i = 0, off = 0, next = 0, last_j = 0xFFFFFFFFu;
+        int32_t id = -1, start = 0;
+        uint32_t past = 0, kept = 0;
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+            const uint32_t t = (uint32_t)g * 4 + c;
+            slot[c] = pos[c] = -1;
+            if (t < t_begin || t >= t_end) continue;
+            if (t >= next) {
+                i = find(l_tok, mine, t);
+                off = l_tok[i];
+                next = l_tok[i + 1];
+                past = min((uint32_t)max(a.past_lens[r0 + i], 0), e.cap);
+                kept = (past + (1u << e.sh) - 1u) >> e.sh;
+                start = a.start ? a.start[r0 + i] : 0;
+                last_j = 0xFFFFFFFFu;
+            }
+            const uint32_t own = past + (t - off), j = own >> e.sh;
+            pos[c] = (int32_t)min((int64_t)start + own, (int64_t)kMaxSum);
+            if (own >= e.cap) continue;
+            if (j != last_j) {
+                id = j < kept ? a.block_table[(size_t)(r0 + i) * a.table_width + j] : new_block(e, n_free, l_blk[i] + (j - kept));
+                last_j = j;
+            }
+            if ((uint32_t)id < a.n_blocks) slot[c] = (int32_t)(((uint32_t)id << e.sh) | (own & ((1u << e.sh) - 1u)));
+        }
+        if (wide && g * 4 >= t_begin && g * 4 + 4 <= t_all) {
+            *(i32x4 *)(a.slots + g * 4) = slot;
+            *(i32x4 *)(a.positions + g * 4) = pos;
+        } else {
+            for (uint32_t c = 0; c < 4; ++c) {
+                const uint32_t t = (uint32_t)g * 4 + c;
+                if (t < t_begin || t >= t_all) continue;
+                a.slots[t] = slot[c];
+                a.positions[t] = pos[c];
+            }
+        }
+    }
+}
+
+struct ReleaseArgs {
+    int32_t *lens;
+    const int32_t *finished;
+    int32_t *table, *free_blocks;
+    const int32_t *n_free;
+    int32_t *info;
+    uint32_t n_requests, sh, cap, width, n_blocks;
+};
+
+// One work-group: requests end seldom, and the free list is one stack whose order the call fixes.
+__global__ void __launch_bounds__(kThreads) release_kernel(const ReleaseArgs a) {
+    __shared__ uint32_t l_blk[kChunk + 1];
+    __shared__ Sums l_wave[kWaves];
+    __shared__ uint32_t l_cnt[kWaves];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    const uint32_t had = (uint32_t)min(max(*a.n_free, 0), (int32_t)a.n_blocks);
+    uint32_t base = had, lost = 0;                     // the same in all threads
+    for (uint32_t r0 = 0; r0 < a.n_requests; r0 += kChunk) {
+        const uint32_t mine = min(kChunk, a.n_requests - r0);
+        uint32_t n[kPer], sum = 0;
+        for (uint32_t i = 0; i < kPer; ++i) {
+            const uint32_t j = tid * kPer + i, r = r0 + j;
+            n[i] = 0;
+            if (j < mine && a.finished[r]) {
+                n[i] = (min((uint32_t)max(a.lens[r], 0), a.cap) + (1u << a.sh) - 1u) >> a.sh;
+                a.lens[r] = 0;
+            }
+            sum = add_sat(sum, n[i]);
+        }
+        Sums total, at = scan({0, sum, 0}, l_wave, total);
+        for (uint32_t i = 0; i < kPer; ++i) {
+            if (tid * kPer + i < mine) l_blk[tid * kPer + i] = at.blocks;
+            at.blocks = add_sat(at.blocks, n[i]);
+        }
+        if (tid == 0) l_blk[mine] = total.blocks;
+        __syncthreads();
+        for (uint64_t k0 = 0; k0 < total.blocks; k0 += kThreads) {
+            const uint32_t k = (uint32_t)k0 + tid;
+            int32_t id = -1;
+            if (k0 + tid < total.blocks) {
+                const uint32_t i = find(l_blk, mine, k);
+                int32_t *entry = a.table + (size_t)(r0 + i) * a.width + (k - l_blk[i]);
+                id = *entry;
+                *entry = -1;
+            }
+            const bool valid = (uint32_t)id < a.n_blocks;
+            const uint64_t m = __ballot(valid);
+            if (lane == 0) l_cnt[wave] = (uint32_t)__popcll(m);
+            __syncthreads();
+            uint32_t at_wave = base, all = 0;
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                if (w < wave) at_wave += l_cnt[w];
+                all += l_cnt[w];
+            }
+            const uint32_t at_lane = at_wave + (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
+            if (valid && at_lane < a.n_blocks) a.free_blocks[at_lane] = id;
+            const uint32_t room = a.n_blocks - base;
+            lost = add_sat(lost, all - min(all, room));
+            base += min(all, room);
+            __syncthreads();
+        }
+        __syncthreads();
+    }
+    if (tid == 0) {
+        a.info[0] = (int32_t)base;
+        a.info[1] = (int32_t)(base - had);
+        a.info[2] = (int32_t)min(lost, kMaxSum);
+    }
+}
+
+// ---- rotary positions ---------------------------------------------------------------------
+
+__global__ void rope_table_kernel(float *table, uint32_t max_pos, uint32_t half, double base, int scale, double factor, double original,
+                                  double low, double high, double magnitude) {
+    const uint64_t n = (uint64_t)max_pos * half;
+    for (uint64_t x = blockIdx.x * (uint64_t)blockDim.x + threadIdx.x; x < n; x += (uint64_t)gridDim.x * blockDim.x) {
+        const uint32_t pos = (uint32_t)(x / half), i = (uint32_t)(x % half);
+        double w = pow(base, -(double)i / (double)half);
+        if (scale == HPS_SEQ_SCALE_LINEAR) w /= factor;
+        if (scale == HPS_SEQ_SCALE_PARTS) {
+            const double turns = original * w / (2.0 * M_PI), g = fmin(fmax((turns - low) / (high - low), 0.0), 1.0);
+            w *= g + (1.0 - g) / factor;
+        }
+        double s, c;
+        sincos((double)pos * w, &s, &c);
+        *(float2 *)(table + x * 2) = make_float2((float)(c * magnitude), (float)(s * magnitude));
+    }
+}
+
+// The heads of a token, in the order queries, keys, values.  `out` of keys and values is an array like the input, or
+// the pages.
+struct RopeArgs {
+    const char *in[3];
+    char *out[3];
+    int64_t in_token[3], in_head[3], out_token[3], out_head[3];         // strides in bytes
+    int64_t page_block;                                                 // of the pages: block stride; out_token is the place's
+    const int32_t *positions, *slots;
+    const float *table;
+    uint32_t heads[3], n_heads;                                         // of each, of all
+    uint32_t head_dim, half, max_pos;                                   // half = rot_dim / 2
+    uint32_t spans, per_pass, n_slots, sh;                              // spans: pairs of vectors of a head; per_pass: heads side by side
+    int32_t interleaved;
+    float sign;
+};
+
+template <typename T, int E> struct alignas(E * sizeof(T) > 16 ? 16 : E * sizeof(T)) Vec { T v[E]; };
+
+// One work-group per token.  A lane has two vectors of 16 bytes of a head (for halves: the two that hold E pairs), which
+// stay the same from head to head, so cosines and sines are read once for all of them; two heads are in flight at a time.
+// Bound by HBM: each input and output passes once.  E = 1 is for rows that are not in whole 16-byte vectors.
+template <typename T, int E, bool kPages>
+__global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+    typedef Vec<T, E> V;
+    const uint32_t t = blockIdx.x, tid = threadIdx.x;
+    const uint32_t lane_head = tid / a.spans, s = tid - lane_head * a.spans;
+    if (lane_head >= a.per_pass) return;
+    const bool turns = a.table != nullptr;
+    const int32_t pos = turns ? a.positions[t] : 0;
+    if (pos < 0) return;
+    uint32_t slot = 0;
+    if (kPages) slot = (uint32_t)a.slots[t];
+    const bool stored = !kPages || slot < a.n_slots;
+
+    // the two vectors (o0, o1, in values), and the pairs in them
+    const bool within = a.interleaved && E > 1;        // pairs lie within a vector
+    uint32_t o0, o1;
+    if (a.interleaved) {
+        o0 = 2 * s * E;
+        o1 = o0 + E;
+    } else {
+        const uint32_t split = a.half / E;             // behind the pairs, two neighbours to a span
+        o0 = s < split ? s * E : 2 * a.half + 2 * (s - split) * E;
+        o1 = s < split ? a.half + s * E : o0 + E;
+    }
+    const bool has0 = o0 < a.head_dim, has1 = o1 < a.head_dim;
+    const bool turn0 = turns && o0 < 2 * a.half, turn1 = turns && o1 < 2 * a.half;
+    float cs[E], sn[E];                                // of the pairs: across the two vectors E, within them E / 2 each
+#pragma unroll
+    for (int j = 0; j < E; ++j) cs[j] = sn[j] = 0.f;
+    if (turn0) {
+        if ((uint32_t)pos < a.max_pos) {
+            const float2 *row = (const float2 *)a.table + (size_t)pos * a.half;
+            const uint32_t pair = within ? s * E : a.interleaved ? s : o0;
+            const uint32_t n = within ? (turn1 ? E : E / 2) : E;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if ((uint32_t)j < n) {
+                    const float2 f = row[pair + j];
+                    cs[j] = f.x;
+                    sn[j] = f.y * a.sign;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) cs[j] = sn[j] = __builtin_nanf("");
+        }
+    }
+
+    constexpr int U = 2;
+    for (uint32_t h0 = lane_head; h0 < a.n_heads; h0 += U * a.per_pass) {
+        V x[U], y[U];
+        char *to[U];
+        bool turned[U], live[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t hh = h0 + u * a.per_pass;
+            const uint32_t seg = hh < a.heads[0] ? 0 : hh < a.heads[0] + a.heads[1] ? 1 : 2;
+            const uint32_t h = hh - (seg > 0 ? a.heads[0] : 0) - (seg > 1 ? a.heads[1] : 0);
+            live[u] = hh < a.n_heads && (seg == 0 || stored);
+            turned[u] = seg < 2;
+            to[u] = nullptr;
+            if (!live[u]) continue;
+            const char *from = (seg == 0 ? a.in[0] : seg == 1 ? a.in[1] : a.in[2]);
+            const int64_t it = seg == 0 ? a.in_token[0] : seg == 1 ? a.in_token[1] : a.in_token[2];
+            const int64_t ih = seg == 0 ? a.in_head[0] : seg == 1 ? a.in_head[1] : a.in_head[2];
+            from += (int64_t)t * it + (int64_t)h * ih;
+            char *dst = seg == 0 ? a.out[0] : seg == 1 ? a.out[1] : a.out[2];
+            const int64_t ot = seg == 0 ? a.out_token[0] : seg == 1 ? a.out_token[1] : a.out_token[2];
+            const int64_t oh = seg == 0 ? a.out_head[0] : seg == 1 ? a.out_head[1] : a.out_head[2];
+            if (kPages && seg > 0) dst += (int64_t)(slot >> a.sh) * a.page_block + (int64_t)(slot & ((1u << a.sh) - 1u)) * ot;
+            else dst += (int64_t)t * ot;
+            to[u] = dst + (int64_t)h * oh;
+            if (has0) x[u] = *(const V *)(from + o0 * sizeof(T));
+            if (has1) y[u] = *(const V *)(from + o1 * sizeof(T));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!live[u]) continue;
+            if (turned[u] && turn0) {
+                if (within) {
+                    if constexpr (E > 1) {
+#pragma unroll
+                        for (int j = 0; j < E / 2; ++j) {
+                            const float p = (float)x[u].v[2 * j], q = (float)x[u].v[2 * j + 1];
+                            x[u].v[2 * j] = (T)(p * cs[j] - q * sn[j]);
+                            x[u].v[2 * j + 1] = (T)(p * sn[j] + q * cs[j]);
+                            if (turn1) {
+                                const float p1 = (float)y[u].v[2 * j], q1 = (float)y[u].v[2 * j + 1];
+                                y[u].v[2 * j] = (T)(p1 * cs[E / 2 + j] - q1 * sn[E / 2 + j]);
+                                y[u].v[2 * j + 1] = (T)(p1 * sn[E / 2 + j] + q1 * cs[E / 2 + j]);
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const float p = (float)x[u].v[j], q = (float)y[u].v[j];
+                        x[u].v[j] = (T)(p * cs[j] - q * sn[j]);
+                        y[u].v[j] = (T)(p * sn[j] + q * cs[j]);
+                    }
+                }
+            }
+            if (has0) *(V *)(to[u] + o0 * sizeof(T)) = x[u];
+            if (has1) *(V *)(to[u] + o1 * sizeof(T)) = y[u];
+        }
+    }
+}
+
+template <typename T, bool kPages>
+hipError_t launch_rope(RopeArgs &a, uint32_t n_tokens, uint32_t rot_dim, hipStream_t st) {
+    constexpr int E = 16 / sizeof(T);
+    a.n_heads = a.heads[0] + a.heads[1] + a.heads[2];
+    // whole vectors: every row starts on 16 bytes, and no vector holds pairs of two kinds
+    bool whole = a.head_dim % E == 0 && (a.interleaved ? rot_dim % E : a.half % E) == 0 && (a.page_block & 15) == 0;
+    for (int i = 0; i < 3; ++i)
+        if (a.heads[i])
+            whole = whole && seq_aligned(a.in[i], 16) && seq_aligned(a.out[i], 16) && ((a.in_token[i] | a.in_head[i] | a.out_token[i] | a.out_head[i]) & 15) == 0;
+    const uint32_t e = whole ? E : 1, rest = a.head_dim - rot_dim;
+    a.spans = a.interleaved ? (a.head_dim / e + 1) / 2 : a.half / e + (rest / e + 1) / 2;
+    uint32_t threads = (a.n_heads * a.spans + 63) / 64 * 64;
+    if (threads > 256) threads = 256;
+    a.per_pass = threads / a.spans;
+    if (whole) hipLaunchKernelGGL((rope_kernel<T, E, kPages>), dim3(n_tokens), dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL((rope_kernel<T, 1, kPages>), dim3(n_tokens), dim3(threads), 0, st, a);
+    return hipGetLastError();
+}
+
+template <bool kPages> hipError_t launch_rope(RopeArgs &a, int dtype, uint32_t n_tokens, uint32_t rot_dim, hipStream_t st) {
+    if (dtype == HPS_SEQ_F32) return launch_rope<float, kPages>(a, n_tokens, rot_dim, st);
+    if (dtype == HPS_SEQ_F16) return launch_rope<_Float16, kPages>(a, n_tokens, rot_dim, st);
+    return launch_rope<__bf16, kPages>(a, n_tokens, rot_dim, st);
+}
+
+int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
+
+hps_status_t check_rope(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens) {
+    SEQ_REQUIRE(dtype == HPS_SEQ_F32 || dtype == HPS_SEQ_F16 || dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F32, HPS_SEQ_F16 or HPS_SEQ_BF16");
+    SEQ_REQUIRE(head_dim > 0 && head_dim <= 512, "head_dim must be in 1 .. 512");
+    SEQ_REQUIRE(n_tokens < (1u << 31), "n_tokens must be < 2^31");
+    if (!table) return HPS_OK;
+    SEQ_REQUIRE(rot_dim % 2 == 0 && rot_dim > 0 && rot_dim <= head_dim, "rot_dim must be even and in 2 .. head_dim");
+    SEQ_REQUIRE(max_pos > 0 && max_pos <= (1u << 31), "max_pos must be in 1 .. 2^31");
+    SEQ_REQUIRE(seq_aligned(table, 8), "table must be 8-byte aligned");
+    SEQ_REQUIRE(n_tokens == 0 || seq_words(positions), "positions must be a 4-byte aligned device pointer");
+    return HPS_OK;
+}
+
+// Puts an array of heads into the arguments' place i; false if it is not there or not aligned to its values.
+bool put(RopeArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, int size) {
+    a.heads[i] = heads;
+    a.in[i] = static_cast<const char *>(in.data);
+    a.out[i] = static_cast<char *>(out.data);
+    a.in_token[i] = in.token_stride * size;
+    a.in_head[i] = in.head_stride * size;
+    a.out_token[i] = out.token_stride * size;
+    a.out_head[i] = out.head_stride * size;
+    return heads == 0 || (in.data && out.data && seq_aligned(in.data, size) && seq_aligned(out.data, size));
+}
+
+}  // namespace
+
+hps_status_t hps_seq_fail(hps_status_t code, const char *what, const char *more) {
+    snprintf(g_err, sizeof(g_err), "%s%s", what, more);
+    return code;
+}
+
+extern "C" {
+
+const char *hps_seq_last_error(void) { return g_err; }
+
+hps_status_t hps_seq_extend(const hps_seq_extend_args_t *args, void *stream) {
+    SEQ_REQUIRE(args, "args must not be NULL");
+    const hps_seq_extend_args_t &a = *args;
+    SEQ_REQUIRE(seq_block_size(a.block_size), "block_size must be a power of two in 1 .. 1024");
+    SEQ_REQUIRE((uint64_t)a.n_blocks * a.block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
+    SEQ_REQUIRE((uint64_t)a.table_width * a.block_size < (1ull << 31), "table_width * block_size must be < 2^31");
+    SEQ_REQUIRE(a.n_requests <= (1u << 24), "n_requests must be <= 2^24");
+    SEQ_REQUIRE(a.max_tokens < (1u << 31), "max_tokens must be < 2^31");
+    SEQ_REQUIRE(seq_words(a.n_free) && seq_words(a.token_offsets) && seq_words(a.info), "n_free, token_offsets and info must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(a.n_blocks == 0 || seq_words(a.free_blocks), "free_blocks must be a 4-byte aligned device pointer");
+    SEQ_REQUIRE(a.max_tokens == 0 || (seq_words(a.slots) && seq_words(a.positions)), "slots and positions must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(a.n_requests == 0 || (seq_words(a.past_lens) && seq_words(a.new_lens) && seq_words(a.total_lens)),
+                "past_lens, new_lens and total_lens must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(a.n_requests == 0 || a.table_width == 0 || seq_words(a.block_table), "block_table must be a 4-byte aligned device pointer");
+    SEQ_REQUIRE(a.start == nullptr || seq_aligned(a.start, 4), "start must be 4-byte aligned");
+    SEQ_REQUIRE(a.n_free != a.info, "info must not be the array that n_free is read from");
+    SEQ_REQUIRE(a.n_requests == 0 || (a.total_lens != a.past_lens && a.total_lens != a.new_lens), "total_lens must be an array of its own");
+    ExtendArgs e{a, (uint32_t)__builtin_ctz(a.block_size), a.table_width * a.block_size};
+    const uint32_t chunks = a.n_requests ? (a.n_requests + kChunk - 1) / kChunk : 1;
+    // a work-group per 4,096 tokens, one store of each lane, and two work-groups per CU at most
+    uint32_t parts = (a.max_tokens + 4095u) / 4096u, most = 512u / chunks;
+    if (parts > most) parts = most;
+    if (parts < 1) parts = 1;
+    hipLaunchKernelGGL(extend_kernel, dim3(parts, chunks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), e);
+    SEQ_TRY(hipGetLastError());
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_release(int32_t *lens, const int32_t *finished, uint32_t n_requests, uint32_t block_size, int32_t *block_table,
+                             uint32_t table_width, int32_t *free_blocks, uint32_t n_blocks, const int32_t *n_free, int32_t *info, void *stream) {
+    SEQ_REQUIRE(seq_block_size(block_size), "block_size must be a power of two in 1 .. 1024");
+    SEQ_REQUIRE((uint64_t)n_blocks * block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
+    SEQ_REQUIRE((uint64_t)table_width * block_size < (1ull << 31), "table_width * block_size must be < 2^31");
+    SEQ_REQUIRE(n_requests <= (1u << 24), "n_requests must be <= 2^24");
+    SEQ_REQUIRE(seq_words(n_free) && seq_words(info), "n_free and info must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(n_blocks == 0 || seq_words(free_blocks), "free_blocks must be a 4-byte aligned device pointer");
+    SEQ_REQUIRE(n_requests == 0 || (seq_words(lens) && seq_words(finished)), "lens and finished must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(n_requests == 0 || table_width == 0 || seq_words(block_table), "block_table must be a 4-byte aligned device pointer");
+    const ReleaseArgs a{lens, finished, block_table, free_blocks, n_free, info, n_requests, (uint32_t)__builtin_ctz(block_size), table_width * block_size,
+                        table_width, n_blocks};
+    hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+    SEQ_TRY(hipGetLastError());
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_rope_table(float *table, uint32_t max_pos, uint32_t rot_dim, double base, int scale, double factor, double original, double low,
+                                double high, double magnitude, void *stream) {
+    SEQ_REQUIRE(rot_dim > 0 && rot_dim % 2 == 0 && rot_dim <= 512, "rot_dim must be even and in 2 .. 512");
+    SEQ_REQUIRE(max_pos <= (1u << 31), "max_pos must be <= 2^31");
+    SEQ_REQUIRE(std::isfinite(base) && base > 0, "base must be finite and > 0");
+    SEQ_REQUIRE(std::isfinite(magnitude), "magnitude must be finite");
+    SEQ_REQUIRE(scale >= HPS_SEQ_SCALE_NONE && scale <= HPS_SEQ_SCALE_PARTS, "scale must be HPS_SEQ_SCALE_NONE, _LINEAR or _PARTS");
+    SEQ_REQUIRE(scale == HPS_SEQ_SCALE_NONE || (std::isfinite(factor) && factor > 0), "factor must be finite and > 0");
+    SEQ_REQUIRE(scale != HPS_SEQ_SCALE_PARTS || (std::isfinite(original) && original > 0 && std::isfinite(low) && std::isfinite(high) && low < high),
+                "original must be finite and > 0, and low < high");
+    if (max_pos == 0) return HPS_OK;
+    SEQ_REQUIRE(table && seq_aligned(table, 8), "table must be an 8-byte aligned device pointer");
+    const uint64_t n = (uint64_t)max_pos * (rot_dim / 2), groups = (n + 255) / 256;
+    hipLaunchKernelGGL(rope_table_kernel, dim3((uint32_t)(groups < 65536 ? groups : 65536)), dim3(256), 0, static_cast<hipStream_t>(stream), table, max_pos,
+                       rot_dim / 2, base, scale, factor, original, low, high, magnitude);
+    SEQ_TRY(hipGetLastError());
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_rope(const hps_seq_rope_args_t *args, void *stream) {
+    SEQ_REQUIRE(args, "args must not be NULL");
+    const hps_seq_rope_args_t &r = *args;
+    SEQ_REQUIRE(r.table, "table must not be NULL");
+    if (hps_status_t st = check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
+    SEQ_REQUIRE((uint64_t)r.q_heads + r.k_heads <= 65536, "at most 65536 heads");
+    if (r.n_tokens == 0 || r.q_heads + r.k_heads == 0) return HPS_OK;
+    RopeArgs a{};
+    SEQ_REQUIRE(put(a, 0, r.q_heads, r.q, r.q_out, size_of(r.dtype)) && put(a, 1, r.k_heads, r.k, r.k_out, size_of(r.dtype)),
+                "q, k, q_out and k_out must be device pointers aligned to their type");
+    a.positions = r.positions;
+    a.table = r.table;
+    a.head_dim = r.head_dim;
+    a.half = r.rot_dim / 2;
+    a.max_pos = r.max_pos;
+    a.interleaved = r.interleaved != 0;
+    a.sign = r.inverse ? -1.f : 1.f;
+    SEQ_TRY(launch_rope<false>(a, r.dtype, r.n_tokens, r.rot_dim, static_cast<hipStream_t>(stream)));
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_append(const hps_seq_append_args_t *args, void *stream) {
+    SEQ_REQUIRE(args, "args must not be NULL");
+    const hps_seq_append_args_t &r = *args;
+    if (hps_status_t st = check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
+    SEQ_REQUIRE(seq_block_size(r.pages.block_size), "block_size must be a power of two in 1 .. 1024");
+    SEQ_REQUIRE((uint64_t)r.pages.n_blocks * r.pages.block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
+    SEQ_REQUIRE(r.kv_heads > 0 && (uint64_t)r.q_heads + 2ull * r.kv_heads <= 65536, "kv_heads must be > 0, and at most 65536 heads in all");
+    if (r.n_tokens == 0) return HPS_OK;
+    SEQ_REQUIRE(seq_words(r.slots), "slots must be a 4-byte aligned device pointer");
+    const int size = size_of(r.dtype);
+    const hps_seq_heads_t pk{r.pages.k, r.pages.token_stride, r.pages.head_stride}, pv{r.pages.v, r.pages.token_stride, r.pages.head_stride};
+    RopeArgs a{};
+    SEQ_REQUIRE(put(a, 0, r.q_heads, r.q, r.q_out, size) && put(a, 1, r.kv_heads, r.k, pk, size) && put(a, 2, r.kv_heads, r.v, pv, size),
+                "q, q_out, k, v and the pages must be device pointers aligned to their type");
+    a.page_block = r.pages.block_stride * size;
+    a.positions = r.positions;
+    a.slots = r.slots;
+    a.table = r.table;
+    a.head_dim = r.head_dim;
+    a.half = r.table ? r.rot_dim / 2 : 0;
+    a.max_pos = r.max_pos;
+    a.n_slots = r.pages.n_blocks * r.pages.block_size;
+    a.sh = (uint32_t)__builtin_ctz(r.pages.block_size);
+    a.interleaved = r.table && r.interleaved;
+    a.sign = 1.f;
+    SEQ_TRY(launch_rope<true>(a, r.dtype, r.n_tokens, r.table ? r.rot_dim : 0, static_cast<hipStream_t>(stream)));
+    return HPS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,857 @@
+// Attention of new tokens over a history that their group shares and over their request's own tokens (hps_seq.h), for
+// gfx950.
+//
+//   o_t = sum_j w_tj v_j / sum_j w_tj,   w_tj = exp(scale * q_t . k_j - m_t)
+//
+// Sums over disjoint sets of keys join: with (m, l, o) = (reference, sum of weights, weighted sum) of each,
+// m = max m_i, l = sum 2^(m_i - m) l_i, o = sum 2^(m_i - m) o_i (in powers of two).  So the history is attended once for
+// all rows of its group - the rows of a matrix product are the (token, query head) pairs that share a key/value head -
+// and a request's own tokens separately; long stretches of keys are cut into chunks where there are few rows; and a
+// second kernel joins what the parts left behind.
+//
+// Scores are computed transposed, S^T = K Q^T, with 32x32x16 matrix instructions: lane l holds 16 of the 32 keys' scores
+// of row l % 32, so a row's maximum and sum are almost wholly within a lane, and the weights, rounded, are at once the
+// second operand of O^T = V^T W^T.  Both products read their first operand from LDS: keys 16 bytes along a row, values
+// transposed on the way (ds_read_b64_tr_b16).  Rows of keys and values go from memory to LDS without registers between; chunks of 16
+// bytes change places within their row there (sw_k, sw_v), so that the lanes of one read meet all banks.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+
+#include "hps_seq_common.h"
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef const __attribute__((address_space(4))) int32_t scalar_i32;
+
+constexpr uint64_t kMagic = 0x4850535345514154ull;
+constexpr float kInf = __builtin_inff();
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr uint32_t kWideRows = 128, kNarrowRows = 32;  // rows of a work-group
+constexpr uint32_t kWideKeys = 64, kNarrowKeys = 32;   // keys of a step: of the work-group, of a wave
+// A row's reference m follows its maximum only when that is this far ahead (in powers of two): weights stay below 2^8,
+// and most steps need no rescaling.
+constexpr float kSlack = 8.f;
+
+struct Args {
+    const char *q, *k, *v;
+    char *out;
+    float *lse, *part_o;
+    float2 *part_ml;                                   // reference and sum of each part's row; sum 0: nothing attended
+    uint32_t *flags;
+    const int32_t *prefix_table, *prefix_lens, *group_offsets, *block_table, *lens, *token_offsets;
+    int64_t q_token, q_head, out_token, out_head, page_block, page_token, page_head;       // strides in bytes
+    uint32_t n_tokens, n_requests, n_groups, table_width, prefix_width, max_new, max_group, max_len, max_prefix;
+    uint32_t q_heads, kv_heads, ratio, head_dim, n_blocks, sh;
+    uint32_t history_groups, history_tiles, history_chunks, history_chunk, history_combos; // work-groups; row tiles; chunks, keys of one; (group, chunk, head)
+    uint32_t own_tiles, own_chunks, own_chunk, own_items;
+    int32_t history_wide, own_mode, direct;            // direct: one part only, results go straight out
+    float c;                                           // scale * log2(e)
+};
+enum { kOwnSplit = 0, kOwnSolo = 1, kOwnWide = 2 };    // a work-group's waves share the keys; have an item each; share the rows
+
+template <typename T> struct Type;
+template <> struct Type<__bf16> {
+    typedef bf16x8 frag;
+    static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static constexpr uint32_t kExp = 0x7F80u;
+};
+template <> struct Type<_Float16> {
+    typedef f16x8 frag;
+    static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static constexpr uint32_t kExp = 0x7C00u;
+};
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ int32_t scalar(const int32_t *p, size_t i) { return ((scalar_i32 *)(uintptr_t)p)[i]; }
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+// maximum and sum with the lane that holds the row's other keys
+__device__ __forceinline__ float both_max(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float both_sum(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// 64 lanes' 16 bytes from base + off to LDS at `to` + 16 * lane.  The caller waits for vmcnt; lanes that are switched
+// off leave their place in LDS alone.  (Not the builtin: the compiler then waits for every such load in front of any
+// read of LDS, and the next step's loads are what is to stay in flight.)
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// What one wave attends with: 32 rows against keys first .. end of one table.
+struct Item {
+    const int32_t *table;
+    uint32_t width, first, end;
+    uint32_t token0, row0, rows;                       // the tile's rows are row0 .. of `rows` (token, head) pairs from token0 on
+    uint32_t head, part;                               // key/value head; part that the result is
+    int32_t causal_from;                               // row's query i sees keys below causal_from + i; or kAll
+};
+constexpr int32_t kAll = 0x7FFFFFFF;
+
+template <typename T, int DT> struct Engine {          // head_dim <= 32 * DT
+    typedef typename Type<T>::frag frag;
+    static constexpr int kRow = DT <= 2 ? 128 : DT <= 4 ? 256 : 512;    // bytes of a row in LDS
+    static constexpr int kChunks = kRow / 16, kSteps = 2 * DT;
+    static constexpr int kLoads = 16 * kRow / 1024, kLoadRows = 1024 / kRow;        // wave loads of 16 rows, rows of one
+    static constexpr uint32_t kLds = 256 * kRow;       // wide: 2 stages of 64 keys and values; narrow: 4 waves of 32
+
+    const Args &a;
+    const uint32_t lane, half, lds;
+    frag q[kSteps];
+    f32x16 o[DT];
+    float m, l;
+    int32_t limit;                                     // the lane's row sees keys below it
+    uint32_t k_at, v_at[2];                            // LDS addresses of the lane's first key and value operands
+    uint32_t k_off[kLoads], v_off[kLoads];             // offsets of its 16 bytes of each wave load of 16 rows
+
+    static __device__ __forceinline__ uint32_t sw_k(uint32_t t) { return t & (kRow == 128 ? 7u : 15u); }
+    static __device__ __forceinline__ uint32_t sw_v(uint32_t t) { return ((kRow == 128 ? (t >> 1) & 1u : t & 3u) << 2) | ((t >> 2) & 3u); }
+
+    __device__ __forceinline__ Engine(const Args &args, uint32_t lds_base) : a(args), lane(threadIdx.x & 63u), half(lane >> 5), lds(lds_base) {
+        const uint32_t n = lane & 31u, g = lane & 15u;
+        k_at = n * kRow + ((half ^ sw_k(n)) << 4);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t t = 4 * half + 8 * j + (g >> 2);
+            v_at[j] = t * kRow + (((2 * ((lane >> 4) & 1u) + ((g & 3u) >> 1)) ^ sw_v(t)) << 4) + (g & 1u) * 8;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t t = i * kLoadRows + lane / kChunks, pos = lane % kChunks;
+            k_off[i] = t * (uint32_t)a.page_token + ((pos ^ sw_k(t)) << 4);
+            v_off[i] = t * (uint32_t)a.page_token + ((pos ^ sw_v(t)) << 4);
+        }
+    }
+
+    // Rows of 16 keys (or values) from token `at` on: whole ones straight to LDS; at the end of the keys, for small blocks
+    // and for a block number that is none, through registers, zeros in the place of what is not there.
+    // Returns whether the loads are still under way.
+    __device__ __forceinline__ bool load16(const Item &it, const char *pages, const uint32_t (&off)[kLoads], bool values, uint32_t at, int32_t id, uint32_t to) {
+        const char *head = pages + (int64_t)it.head * a.page_head;
+        if (a.sh >= 4 && at + 16 <= it.end && (uint32_t)id < a.n_blocks) {
+            const char *base = head + (int64_t)id * a.page_block + (int64_t)(at & ((1u << a.sh) - 1u)) * a.page_token;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ (values ? sw_v(t) : sw_k(t));
+                if (kChunks * 8 == 32 * DT && a.head_dim == 32 * DT) load_to_lds(base, off[i], lds + to + i * 1024);       // uniform
+                else if (chunk * 8 < a.head_dim) load_to_lds(base, off[i], lds + to + i * 1024);
+            }
+            return true;
+        }
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ (values ? sw_v(t) : sw_k(t)), key = at + t;
+            u32x4 x = {0, 0, 0, 0};
+            if (chunk * 8 < a.head_dim && key < it.end) {
+                const uint32_t b = (uint32_t)it.table[key >> a.sh];
+                if (b < a.n_blocks) x = *(const u32x4 *)(head + (int64_t)b * a.page_block + (int64_t)(key & ((1u << a.sh) - 1u)) * a.page_token + chunk * 16);
+                else atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
+            }
+            *(__attribute__((address_space(3))) u32x4 *)(lds_char *)(uintptr_t)(lds + to + i * 1024 + lane * 16) = x;
+        }
+        return false;
+    }
+    // Block of the 16 keys from `at` on; -1 where they are not all there or blocks are smaller.
+    __device__ __forceinline__ int32_t block_of(const Item &it, uint32_t at) const {
+        return a.sh >= 4 && at < it.end ? scalar(it.table, at >> a.sh) : -1;
+    }
+
+    __device__ __forceinline__ void begin(const Item &it, uint32_t row_of_wave) {
+        const uint32_t row = it.row0 + row_of_wave + (lane & 31u), i = row / a.ratio;
+        const bool there = row < it.rows;
+        limit = it.causal_from == kAll ? (int32_t)it.end : min((int32_t)it.end, it.causal_from + (int32_t)i);
+        const char *src = a.q + (int64_t)(it.token0 + i) * a.q_token + (int64_t)(it.head * a.ratio + (row - i * a.ratio)) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (there && (uint32_t)(16 * s + 8 * half) < a.head_dim) x = *(const u32x4 *)(src + (16 * s + 8 * half) * 2);
+            q[s] = __builtin_bit_cast(frag, x);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+        m = -kInf;
+        l = 0.f;
+        if (!there) limit = kAll;                      // their results go nowhere
+    }
+
+    // Scores of 32 keys whose rows start at `at` in LDS.
+    __device__ __forceinline__ f32x16 scores(uint32_t at) const {
+        f32x16 s{};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const frag x = *(__attribute__((address_space(3))) frag *)(lds_char *)(uintptr_t)(lds + at + (k_at ^ (uint32_t)(i << 5)));
+            s = Type<T>::mfma(x, q[i], s);
+        }
+        return s;
+    }
+    __device__ __forceinline__ static uint32_t key_of(int i, uint32_t half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+
+    // Scores to weights, in place; `seen` gets a bit for each of the lane's keys where some are hidden.
+    template <int N> __device__ __forceinline__ void weights(f32x16 (&s)[N], uint32_t at, bool masked, uint32_t (&seen)[N]) {
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                seen[t] = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool see = (int32_t)(at + 32 * t + key_of(i, half)) < limit;
+                    seen[t] |= see ? 1u << i : 0u;
+                    s[t][i] = see ? s[t][i] : -kInf;
+                }
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = both_max(top) * a.c;
+        if (__ballot(top > m + kSlack)) {              // also the first one: m is -inf
+            const float next = fmaxf(m, top), ref = next == -kInf ? 0.f : next, f = exp2_(m - ref);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= f;
+            m = next;
+        }
+        const float ref = m == -kInf ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = exp2_(__builtin_fmaf(s[t][i], a.c, -ref));
+                sum += s[t][i];
+            }
+        l += sum;
+    }
+
+    __device__ __forceinline__ frag values(uint32_t at, int d) const {
+        s16x4 x[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_char *)(uintptr_t)(lds + at + (v_at[j] ^ (uint32_t)(d << 6))));
+        return __builtin_bit_cast(frag, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+
+    // o += weights x values of 32 keys whose rows start at `at`.
+    __device__ __forceinline__ void add_values(const f32x16 &w, uint32_t at) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            frag p;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = (T)w[8 * u + j];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values(at + 16 * u * kRow, d), p, o[d]);
+        }
+    }
+    // The same where some rows do not see some keys: a hidden value that is not finite must not meet the weight 0, so the
+    // values that are not finite are left out of the product and added, as what they are, to the rows that see them.
+    __device__ __forceinline__ void add_values_masked(const f32x16 &w, uint32_t seen, uint32_t at) {
+#pragma unroll 1
+        for (int u = 0; u < 2; ++u) {
+            frag p, sees;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p[j] = (T)(u ? w[8 + j] : w[j]);
+                sees[j] = (T)(float)(seen >> (8 * u + j) & 1u);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const s16x8 x = __builtin_bit_cast(s16x8, values(at + 16 * u * kRow, d));
+                s16x8 fine = x;
+                frag odd{};
+                bool any = false;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t b = (uint16_t)x[j];
+                    if ((b & Type<T>::kExp) != Type<T>::kExp) continue;
+                    any = true;
+                    fine[j] = 0;
+                    odd[j] = (T)((b & 0x7FFFu) != Type<T>::kExp ? 4096.f : b & 0x8000u ? 64.f : 1.f);      // NaN, -inf, +inf: 16 keys of each tell apart
+                }
+                o[d] = Type<T>::mfma(__builtin_bit_cast(frag, fine), p, o[d]);
+                if (__ballot(any)) {
+                    f32x16 n = Type<T>::mfma(odd, sees, f32x16{});
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t k = (uint32_t)n[i];
+                        if (k >= 4096u) o[d][i] = __builtin_nanf("");
+                        if (k & 4095u & ~63u) o[d][i] -= kInf;
+                        if (k & 63u) o[d][i] += kInf;
+                    }
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ int32_t least_limit() const {                // over the wave's rows
+        int32_t x = limit;
+        for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
+        return x;
+    }
+
+    // A work-group's four waves have 32 rows each and share keys and values: 64 a step, two stages, one meeting a step.
+    __device__ __forceinline__ void wide(const Item &it) {
+        const uint32_t wave = uniform(threadIdx.x >> 6);
+        begin(it, 32 * wave);
+        const int32_t least = (int32_t)uniform((uint32_t)least_limit());
+        constexpr uint32_t kStage = 2 * 64 * kRow, kValues = 64 * kRow;
+        uint32_t at = it.first + 16 * wave, stage = 0;
+        int32_t id = block_of(it, at), next = block_of(it, at + 64);
+        load16(it, a.k, k_off, false, at, id, 16 * wave * kRow);
+        load16(it, a.v, v_off, true, at, id, kValues + 16 * wave * kRow);
+        for (uint32_t k0 = it.first; k0 < it.end; k0 += 64) {
+            wait_loads<0>();
+            meet();                                    // everybody's rows are there, and everybody is done with the other stage
+            if (k0 + 64 < it.end) {                    // uniform
+                at += 64;
+                id = next;
+                next = block_of(it, at + 64);
+                const uint32_t to = (stage ^ kStage) + 16 * wave * kRow;
+                load16(it, a.k, k_off, false, at, id, to);
+                load16(it, a.v, v_off, true, at, id, to + kValues);
+            }
+            f32x16 s[2];
+            uint32_t seen[2];
+            s[0] = scores(stage);
+            s[1] = scores(stage + 32 * kRow);
+            const bool masked = (int32_t)(k0 + 64) > least;
+            weights<2>(s, k0, masked, seen);
+            if (masked && it.causal_from != kAll) {
+                add_values_masked(s[0], seen[0], stage + kValues);
+                add_values_masked(s[1], seen[1], stage + kValues + 32 * kRow);
+            } else {
+                add_values(s[0], stage + kValues);
+                add_values(s[1], stage + kValues + 32 * kRow);
+            }
+            stage ^= kStage;
+        }
+    }
+
+    // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon as the
+    // scores are there, the next values behind the product with these.
+    __device__ __forceinline__ void narrow(const Item &it, uint32_t from, uint32_t stride, uint32_t base) {
+        begin(it, 0);
+        const int32_t least = (int32_t)uniform((uint32_t)least_limit());
+        const uint32_t vbase = base + 32 * kRow;
+        if (from >= it.end) return;
+        int32_t id0 = block_of(it, from), id1 = block_of(it, from + 16);
+        bool k_flies, v_flies;                         // uniform
+        auto load = [&](bool values, uint32_t at) {
+            bool x;
+            if (values) x = load16(it, a.v, v_off, true, at, id0, vbase), x &= load16(it, a.v, v_off, true, at + 16, id1, vbase + 16 * kRow);
+            else x = load16(it, a.k, k_off, false, at, id0, base), x &= load16(it, a.k, k_off, false, at + 16, id1, base + 16 * kRow);
+            return x;
+        };
+        k_flies = load(false, from);
+        v_flies = load(true, from);
+        for (uint32_t at = from; at < it.end; at += stride) {
+            const bool more = at + stride < it.end;
+            int32_t n0 = -1, n1 = -1;
+            if (more) n0 = block_of(it, at + stride), n1 = block_of(it, at + stride + 16);
+            if (k_flies && v_flies) wait_loads<2 * kLoads>();
+            else wait_loads<0>();
+            f32x16 s[1];
+            uint32_t seen[1];
+            s[0] = scores(base);
+            id0 = n0;
+            id1 = n1;
+            if (more) {
+                wait_lds();
+                k_flies = load(false, at + stride);
+            }
+            const bool masked = (int32_t)(at + 32) > least;
+            weights<1>(s, at, masked, seen);
+            if (more && k_flies && v_flies) wait_loads<2 * kLoads>();
+            else wait_loads<0>();
+            if (masked && it.causal_from != kAll) add_values_masked(s[0], seen[0], vbase);
+            else add_values(s[0], vbase);
+            if (more) {
+                wait_lds();
+                v_flies = load(true, at + stride);
+            }
+        }
+    }
+
+    // One row's values 32 * d + 8 * i4 + 4 * half ..: to their place, final or as a part.
+    __device__ __forceinline__ void put4(const Item &it, uint32_t row, int d, int i4, f32x4 x, float f) const {
+        const uint32_t dim = 32 * d + 8 * i4 + 4 * half, i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
+        if (dim >= a.head_dim) return;
+        if (a.direct) {
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            t4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = (T)(x[j] * f);
+            *(t4 *)(a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head + dim * 2) = y;
+        } else {
+            *(f32x4 *)(a.part_o + (((size_t)it.part * a.n_tokens + t) * a.q_heads + h) * a.head_dim + dim) = x;
+        }
+    }
+    __device__ __forceinline__ void put_sums(const Item &it, uint32_t row, float ref, float sum) const {
+        const uint32_t i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio);
+        const size_t at = (size_t)(it.token0 + i) * a.q_heads + h;
+        if (!a.direct) a.part_ml[(size_t)it.part * a.n_tokens * a.q_heads + at] = make_float2(ref, sum);
+        else if (a.lse) a.lse[at] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+    }
+    // The wave's own rows, as they are.
+    __device__ __forceinline__ void finish(const Item &it, uint32_t row_of_wave) {
+        const uint32_t row = it.row0 + row_of_wave + (lane & 31u);
+        const float sum = both_sum(l), f = sum == 0.f ? 0.f : 1.f / sum;
+        if (row >= it.rows) return;
+        if (half == 0) put_sums(it, row, m, sum);
+        if (!a.direct && sum == 0.f) return;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put4(it, row, d, i, f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, f);
+    }
+    // The four waves have the same rows and different keys: joined through LDS, each wave a quarter of the values.
+    __device__ __forceinline__ void finish_split(const Item &it, char *shared, float2 *l_ml) {
+        const uint32_t wave = uniform(threadIdx.x >> 6), row = it.row0 + (lane & 31u);
+        const float sum = both_sum(l);
+        __syncthreads();
+        f32x4 *l_o = (f32x4 *)shared;                  // [wave][DT * 4][64]
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                l_o[(wave * DT * 4 + d * 4 + i) * 64 + lane] = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        if (half == 0) l_ml[wave * 32 + lane] = make_float2(m, sum);
+        __syncthreads();
+        float ref = -kInf, total = 0.f, f[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) ref = fmaxf(ref, l_ml[w * 32 + (lane & 31u)].x);
+        const float at = ref == -kInf ? 0.f : ref;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 x = l_ml[w * 32 + (lane & 31u)];
+            f[w] = exp2_(x.x - at);
+            total += f[w] * x.y;
+        }
+        if (row >= it.rows) return;
+        if (wave == 0 && half == 0) put_sums(it, row, ref, total);
+        if (!a.direct && total == 0.f) return;
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        for (int x = wave * DT; x < (int)(wave + 1) * DT; ++x) {
+            f32x4 y{};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) y += f[w] * l_o[(w * DT * 4 + x) * 64 + lane];
+            put4(it, row, x >> 2, x & 3, y, inv);
+        }
+    }
+};
+
+// Rows of a tile whose part has nothing.
+__device__ __forceinline__ void mark_empty(const Args &a, const Item &it, uint32_t part, uint32_t n, uint32_t lane, uint32_t lanes) {
+    for (uint32_t x = lane; x < n && it.row0 + x < it.rows; x += lanes) {
+        const uint32_t row = it.row0 + x, i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio);
+        a.part_ml[((size_t)part * a.n_tokens + it.token0 + i) * a.q_heads + h] = make_float2(-kInf, 0.f);
+    }
+}
+
+__device__ __forceinline__ uint32_t clamp_to(int32_t x, uint32_t most) { return min((uint32_t)max(x, 0), most); }
+
+// A length as the tables and the launch hold it.
+__device__ __forceinline__ uint32_t length(const Args &a, int32_t x, uint32_t width, uint32_t most) {
+    const uint32_t n = (uint32_t)max(x, 0), fits = min(width << a.sh, most);
+    if (n > fits) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+    return min(n, fits);
+}
+
+template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) attend_kernel(const Args a) {
+    typedef Engine<T, DT> E;
+    extern __shared__ __align__(16) char shared[];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_char *)shared;
+    if (a.head_dim != 32 * DT) {                       // places of LDS rows that no load fills
+        for (uint32_t x = threadIdx.x * 16; x < E::kLds; x += kThreads * 16) *(u32x4 *)(shared + x) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    Item it;
+    bool is_wide, solo = false;
+    if (blockIdx.x < a.history_groups) {
+        // Work-groups of one (group, chunk, head) read the same keys: they go to one XCD (workgroups are dealt to the eight in turn).
+        uint32_t combo, tile;
+        if (a.history_combos >= 8) {
+            const uint32_t y = blockIdx.x >> 3;
+            combo = (blockIdx.x & 7u) + 8 * (y / a.history_tiles);
+            tile = y % a.history_tiles;
+            if (combo >= a.history_combos) return;
+        } else {
+            combo = blockIdx.x % a.history_combos;
+            tile = blockIdx.x / a.history_combos;
+        }
+        it.head = combo % a.kv_heads;
+        const uint32_t rest = combo / a.kv_heads, chunk = rest % a.history_chunks, g = rest / a.history_chunks;
+        const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0;
+        if (n > a.max_group) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        is_wide = a.history_wide;
+        it.token0 = t0;
+        it.rows = min(n, a.max_group) * a.ratio;
+        it.row0 = tile * (is_wide ? kWideRows : kNarrowRows);
+        if (it.row0 >= it.rows) return;
+        it.table = a.prefix_table + (size_t)g * a.prefix_width;
+        it.width = a.prefix_width;
+        it.first = chunk * a.history_chunk;
+        it.end = min(length(a, scalar(a.prefix_lens, g), a.prefix_width, a.max_prefix), it.first + a.history_chunk);
+        it.causal_from = kAll;
+        it.part = chunk;
+    } else {
+        uint32_t x = blockIdx.x - a.history_groups;
+        is_wide = a.own_mode == kOwnWide;
+        solo = a.own_mode == kOwnSolo;
+        if (solo) {
+            x = x * kWaves + wave;
+            if (x >= a.own_items) return;              // no wave of a solo work-group waits for another
+        }
+        it.head = x % a.kv_heads;
+        uint32_t rest = x / a.kv_heads;
+        const uint32_t chunk = rest % a.own_chunks;
+        rest /= a.own_chunks;
+        const uint32_t tile = rest % a.own_tiles, r = rest / a.own_tiles;
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r + 1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0, tile_rows = is_wide ? kWideRows : kNarrowRows;
+        if (n > a.max_new) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        it.token0 = t0;
+        it.rows = min(n, a.max_new) * a.ratio;
+        it.row0 = tile * tile_rows;
+        if (it.row0 >= it.rows) return;
+        const uint32_t len = length(a, scalar(a.lens, r), a.table_width, a.max_len);
+        it.table = a.block_table + (size_t)r * a.table_width;
+        it.width = a.table_width;
+        it.first = chunk * a.own_chunk;
+        const int32_t from = (int32_t)len - (int32_t)n + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
+        it.causal_from = n > 1 ? from : kAll;
+        it.end = min((uint32_t)max(last, 0), it.first + a.own_chunk);
+        it.part = a.history_chunks + chunk;
+        if (a.history_chunks && chunk == 0 && ((int32_t)r < scalar(a.group_offsets, 0) || (int32_t)r >= scalar(a.group_offsets, a.n_groups)))
+            for (uint32_t p = 0; p < a.history_chunks; ++p) mark_empty(a, it, p, tile_rows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+    }
+    if (it.first >= it.end && !a.direct) {
+        mark_empty(a, it, it.part, is_wide ? kWideRows : kNarrowRows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+        return;
+    }
+    E e(a, lds_base);
+    constexpr uint32_t kWave = 2 * 32 * E::kRow;       // a narrow wave's part of LDS
+    if (is_wide) {
+        e.wide(it);
+        e.finish(it, 32 * wave);
+    } else if (solo) {
+        e.narrow(it, it.first, 32, wave * kWave);
+        e.finish(it, 0);
+    } else {
+        e.narrow(it, it.first + 32 * wave, 32 * kWaves, wave * kWave);
+        e.finish_split(it, shared, (float2 *)(shared + E::kLds));
+    }
+}
+
+// Joins the parts of a row: kLanes lanes have four values each of every kWays-th part.
+template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kThreads) join_kernel(const Args a, uint32_t parts) {
+    constexpr int kRows = kThreads / (kLanes * kWays);
+    const uint32_t tid = threadIdx.x, x = tid % kLanes, way = tid / kLanes % kWays, r = tid / (kLanes * kWays);
+    const size_t rows = (size_t)a.n_tokens * a.q_heads, row = (size_t)blockIdx.x * kRows + r;
+    const uint32_t t = (uint32_t)(row / a.q_heads), h = (uint32_t)(row - (size_t)t * a.q_heads);
+    const bool live = row < rows && (int32_t)t < scalar(a.token_offsets, a.n_requests);
+    float ref = -kInf, sum = 0.f;
+    f32x4 y{};
+    if (live) {
+        for (uint32_t p = way; p < parts; p += kWays) {
+            const float2 ml = a.part_ml[p * rows + row];
+            if (ml.y == 0.f) continue;
+            f32x4 v{};
+            if (x * 4 < a.head_dim) v = *(const f32x4 *)(a.part_o + (p * rows + row) * a.head_dim + x * 4);
+            const float next = fmaxf(ref, ml.x), at = next == -kInf ? 0.f : next, f = exp2_(ref - at), g = exp2_(ml.x - at);
+            y = y * f + v * g;
+            sum = sum * f + ml.y * g;
+            ref = next;
+        }
+    }
+    if constexpr (kWays > 1) {
+        __shared__ f32x4 l_y[kThreads];
+        __shared__ float2 l_ml[kThreads];
+        l_y[tid] = y;
+        l_ml[tid] = make_float2(ref, sum);
+        __syncthreads();
+        if (way) return;
+#pragma unroll
+        for (int w = 1; w < kWays; ++w) {
+            const float2 ml = l_ml[tid + w * kLanes];
+            if (ml.y == 0.f) continue;
+            const f32x4 v = l_y[tid + w * kLanes];
+            const float next = fmaxf(ref, ml.x), at = next == -kInf ? 0.f : next, f = exp2_(ref - at), g = exp2_(ml.x - at);
+            y = y * f + v * g;
+            sum = sum * f + ml.y * g;
+            ref = next;
+        }
+    }
+    if (!live) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (x * 4 < a.head_dim) {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        t4 z;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = (T)(y[j] * inv);
+        *(t4 *)(a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head + x * 8) = z;
+    }
+    if (a.lse && x == 0) a.lse[row] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+}
+
+__global__ void clear_kernel(uint32_t *p) { *p = 0u; }
+
+// ---- host ---------------------------------------------------------------------------------
+
+uint32_t div_up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+// How many chunks a stretch of `keys` keys is cut into, where one chunk gives `tiles` work-groups and `others` run beside them: the
+// fewest rounds of work-groups, weighed with what each chunk costs by itself (its start and end; its part, written and read again).
+uint32_t choose_chunks(uint64_t tiles, uint32_t keys, uint32_t step, uint32_t slots, uint64_t most) {
+    uint32_t best = 1;
+    double least = 0;
+    const uint32_t limit = div_up(keys, step);
+    for (uint32_t s = 1; s <= limit && s <= most && s <= 1024; ++s) {
+        const uint32_t chunk = div_up(div_up(keys, s), step) * step;
+        if (s > 1 && div_up(keys, chunk) != s) continue;
+        const double rounds = (double)((tiles * s + slots - 1) / slots), cost = rounds * (chunk + 192.0) + 24.0 * s;
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
+struct hps_seq_attention_session {
+    uint64_t magic;
+    size_t max_rows, part_rows;
+    uint32_t max_head_dim, cus;
+    int device;
+    float *part_o;
+    float2 *part_ml;
+    uint32_t *flags;
+};
+
+namespace {
+
+template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
+    constexpr uint32_t bytes = Engine<T, DT>::kLds + kWaves * 32 * sizeof(float2);
+    static_assert(bytes <= 160 * 1024, "LDS of a CU");
+    if (bytes > 64 * 1024)
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
+    hipLaunchKernelGGL((attend_kernel<T, DT>), dim3(groups), dim3(kThreads), bytes, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.direct) return hipSuccess;
+    constexpr int kLanes = DT == 1 ? 8 : DT == 2 ? 16 : DT <= 4 ? 32 : 64;
+    const size_t rows = (size_t)a.n_tokens * a.q_heads;
+    // few rows of many parts: the parts are read side by side
+    if (parts >= 8) hipLaunchKernelGGL((join_kernel<T, kLanes, 4>), dim3(div_up(rows, kThreads / (kLanes * 4))), dim3(kThreads), 0, st, a, parts);
+    else hipLaunchKernelGGL((join_kernel<T, kLanes, 1>), dim3(div_up(rows, kThreads / kLanes)), dim3(kThreads), 0, st, a, parts);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
+    if (a.head_dim <= 32) return launch<T, 1>(a, groups, parts, st);
+    if (a.head_dim <= 64) return launch<T, 2>(a, groups, parts, st);
+    if (a.head_dim <= 96) return launch<T, 3>(a, groups, parts, st);
+    if (a.head_dim <= 128) return launch<T, 4>(a, groups, parts, st);
+    return launch<T, 8>(a, groups, parts, st);
+}
+
+bool multiple16(int64_t stride) { return (stride * 2 & 15) == 0; }
+bool heads16(const hps_seq_heads_t &h) { return h.data && seq_aligned(h.data, 16) && multiple16(h.token_stride) && multiple16(h.head_stride); }
+
+}  // namespace
+
+extern "C" {
+
+hps_status_t hps_seq_attention_create(size_t max_rows, uint32_t max_head_dim, hps_seq_attention_t **out) {
+    SEQ_REQUIRE(out, "out must not be NULL");
+    *out = nullptr;
+    SEQ_REQUIRE(max_rows > 0 && max_rows < (1ull << 31), "max_rows must be in 1 .. 2^31 - 1");
+    SEQ_REQUIRE(max_head_dim > 0 && max_head_dim <= 256, "max_head_dim must be in 1 .. 256");
+    hps_seq_attention_session *s = new (std::nothrow) hps_seq_attention_session();
+    if (!s) return hps_seq_fail(HPS_ERR_OOM, "host allocation failed");
+    s->max_rows = max_rows;
+    s->part_rows = 3 * max_rows + 65536;
+    s->max_head_dim = (max_head_dim + 7) / 8 * 8;
+    int cus = 0;
+    hipError_t e = hipGetDevice(&s->device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, s->device);
+    s->cus = cus > 0 ? (uint32_t)cus : 256u;
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->part_o), s->part_rows * s->max_head_dim * sizeof(float));
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->part_ml), s->part_rows * sizeof(float2));
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->flags), 256);
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(1), 0, 0, s->flags);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) e = hipStreamSynchronize(0);
+    if (e != hipSuccess) {
+        (void)hipFree(s->part_o);
+        (void)hipFree(s->part_ml);
+        (void)hipFree(s->flags);
+        delete s;
+        (void)hipGetLastError();
+        return hps_seq_fail(e == hipErrorOutOfMemory ? HPS_ERR_OOM : HPS_ERR_DEVICE, "hps_seq_attention_create: ", hipGetErrorString(e));
+    }
+    s->magic = kMagic;
+    *out = s;
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s) {
+    if (!s) return HPS_OK;
+    SEQ_REQUIRE(s->magic == kMagic, "not a live attention session");
+    int prev = -1;
+    SEQ_TRY(hipGetDevice(&prev));
+    SEQ_TRY(hipSetDevice(s->device));
+    hipError_t e = hipDeviceSynchronize();
+    (void)hipFree(s->part_o);
+    (void)hipFree(s->part_ml);
+    (void)hipFree(s->flags);
+    s->magic = 0;
+    delete s;
+    (void)hipSetDevice(prev);
+    if (e != hipSuccess) return hps_seq_fail(HPS_ERR_DEVICE, "hipDeviceSynchronize: ", hipGetErrorString(e));
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_attention_flags(hps_seq_attention_t *s, uint32_t *flags, int clear) {
+    SEQ_REQUIRE(s && s->magic == kMagic, "not a live attention session");
+    SEQ_REQUIRE(flags, "flags must not be NULL");
+    SEQ_TRY(hipMemcpy(flags, s->flags, sizeof(uint32_t), hipMemcpyDeviceToHost));
+    const uint32_t zero = 0u;
+    if (clear) SEQ_TRY(hipMemcpy(s->flags, &zero, sizeof(uint32_t), hipMemcpyHostToDevice));
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_args_t *args, void *stream) {
+    SEQ_REQUIRE(s && s->magic == kMagic, "not a live attention session");
+    SEQ_REQUIRE(args, "args must not be NULL");
+    const hps_seq_attention_args_t &r = *args;
+    SEQ_REQUIRE(r.dtype == HPS_SEQ_F16 || r.dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F16 or HPS_SEQ_BF16");
+    SEQ_REQUIRE(r.head_dim > 0 && r.head_dim % 8 == 0 && r.head_dim <= 256, "head_dim must be a multiple of 8 in 8 .. 256");
+    SEQ_REQUIRE(r.head_dim <= s->max_head_dim, "head_dim exceeds the session's max_head_dim");
+    SEQ_REQUIRE(r.kv_heads > 0 && r.q_heads > 0 && r.q_heads % r.kv_heads == 0 && r.q_heads <= 65536, "q_heads must be a multiple of kv_heads, at most 65536");
+    SEQ_REQUIRE(std::isfinite(r.scale) && r.scale > 0, "scale must be finite and > 0");
+    SEQ_REQUIRE((uint64_t)r.n_tokens * r.q_heads <= s->max_rows, "n_tokens * q_heads exceeds the session's max_rows");
+    SEQ_REQUIRE(seq_block_size(r.pages.block_size), "block_size must be a power of two in 1 .. 1024");
+    SEQ_REQUIRE((uint64_t)r.pages.n_blocks * r.pages.block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
+    SEQ_REQUIRE((uint64_t)r.table_width * r.pages.block_size < (1ull << 31) && (uint64_t)r.prefix_width * r.pages.block_size < (1ull << 31),
+                "table_width and prefix_width times block_size must be < 2^31");
+    SEQ_REQUIRE(r.max_len < (1u << 30) && r.max_prefix < (1u << 30), "max_len and max_prefix must be < 2^30");
+    SEQ_REQUIRE(r.n_requests <= (1u << 24) && r.n_groups <= (1u << 24), "n_requests and n_groups must be <= 2^24");
+    if (r.n_tokens == 0 || r.n_requests == 0) return HPS_OK;
+    SEQ_REQUIRE(heads16(r.q) && heads16(r.out), "q and out must be device pointers, 16-byte aligned, their strides multiples of 16 bytes");
+    SEQ_REQUIRE(seq_words(r.token_offsets) && seq_words(r.lens), "token_offsets and lens must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(r.table_width == 0 || seq_words(r.block_table), "block_table must be a 4-byte aligned device pointer");
+    SEQ_REQUIRE(r.pages.n_blocks == 0 || (r.pages.k && r.pages.v && seq_aligned(r.pages.k, 16) && seq_aligned(r.pages.v, 16)), "the pages must be device pointers, 16-byte aligned");
+    SEQ_REQUIRE(multiple16(r.pages.block_stride) && multiple16(r.pages.token_stride) && multiple16(r.pages.head_stride), "the pages' strides must be multiples of 16 bytes");
+    SEQ_REQUIRE(r.pages.token_stride >= 0 && r.pages.token_stride < (1 << 25), "the pages' token_stride must be in 0 .. 2^25 - 1");
+    SEQ_REQUIRE(r.n_groups == 0 || (seq_words(r.prefix_lens) && seq_words(r.group_offsets) && (r.prefix_width == 0 || seq_words(r.prefix_table))),
+                "prefix_table, prefix_lens and group_offsets must be 4-byte aligned device pointers");
+    SEQ_REQUIRE(r.lse == nullptr || seq_aligned(r.lse, 4), "lse must be 4-byte aligned");
+
+    Args a{};
+    a.q = static_cast<const char *>(r.q.data);
+    a.k = static_cast<const char *>(r.pages.k);
+    a.v = static_cast<const char *>(r.pages.v);
+    a.out = static_cast<char *>(r.out.data);
+    a.lse = r.lse;
+    a.part_o = s->part_o;
+    a.part_ml = s->part_ml;
+    a.flags = s->flags;
+    a.prefix_table = r.prefix_table;
+    a.prefix_lens = r.prefix_lens;
+    a.group_offsets = r.group_offsets;
+    a.block_table = r.block_table;
+    a.lens = r.lens;
+    a.token_offsets = r.token_offsets;
+    a.q_token = r.q.token_stride * 2;
+    a.q_head = r.q.head_stride * 2;
+    a.out_token = r.out.token_stride * 2;
+    a.out_head = r.out.head_stride * 2;
+    a.page_block = r.pages.block_stride * 2;
+    a.page_token = r.pages.token_stride * 2;
+    a.page_head = r.pages.head_stride * 2;
+    a.n_tokens = r.n_tokens;
+    a.n_requests = r.n_requests;
+    a.n_groups = r.n_groups;
+    a.table_width = r.table_width;
+    a.prefix_width = r.prefix_width;
+    a.max_new = r.max_new < r.n_tokens ? r.max_new : r.n_tokens;
+    a.max_group = r.max_group < r.n_tokens ? r.max_group : r.n_tokens;
+    a.max_len = r.max_len;
+    a.max_prefix = r.max_prefix;
+    a.q_heads = r.q_heads;
+    a.kv_heads = r.kv_heads;
+    a.ratio = r.q_heads / r.kv_heads;
+    a.head_dim = r.head_dim;
+    a.n_blocks = r.pages.n_blocks;
+    a.sh = (uint32_t)__builtin_ctz(r.pages.block_size);
+    a.c = r.scale * 1.4426950408889634f;
+
+    const uint64_t rows = (uint64_t)r.n_tokens * r.q_heads, part_limit = s->part_rows / rows;
+    const uint32_t slots = s->cus * (r.head_dim <= 128 ? 2 : 1);
+    // own tokens: one part at least, so that every row has one
+    const uint64_t own_rows = (uint64_t)a.max_new * a.ratio;
+    uint32_t own_keys = r.max_len ? r.max_len : 1;
+    const uint64_t requests_heads = (uint64_t)r.n_requests * r.kv_heads;
+    if (own_rows > kNarrowRows) {
+        a.own_mode = kOwnWide;
+        a.own_tiles = div_up(own_rows, kWideRows);
+        a.own_chunks = choose_chunks(requests_heads * a.own_tiles, own_keys, kWideKeys, slots, part_limit / 2);
+        a.own_chunk = div_up(div_up(own_keys, a.own_chunks), kWideKeys) * kWideKeys;
+    } else {
+        a.own_mode = own_keys <= 2 * kNarrowKeys * kWaves ? kOwnSolo : kOwnSplit;
+        a.own_tiles = 1;
+        const uint32_t step = a.own_mode == kOwnSolo ? kNarrowKeys : kNarrowKeys * kWaves;
+        a.own_chunks = a.own_mode == kOwnSolo ? 1 : choose_chunks(requests_heads, own_keys, step, slots, part_limit / 2);
+        a.own_chunk = div_up(div_up(own_keys, a.own_chunks), step) * step;
+    }
+    if (a.own_tiles == 0) a.own_tiles = 1;
+    const uint64_t own_items = requests_heads * a.own_tiles * a.own_chunks, own_groups = a.own_mode == kOwnSolo ? (own_items + kWaves - 1) / kWaves : own_items;
+    uint64_t history_groups = 0;
+    if (r.n_groups && r.max_prefix && a.max_group) {
+        const uint64_t group_rows = (uint64_t)a.max_group * a.ratio;
+        a.history_wide = group_rows > kNarrowRows;
+        a.history_tiles = div_up(group_rows, a.history_wide ? kWideRows : kNarrowRows);
+        const uint32_t step = a.history_wide ? kWideKeys : kNarrowKeys * kWaves;
+        a.history_chunks = choose_chunks((uint64_t)a.history_tiles * r.n_groups * r.kv_heads, r.max_prefix, step, slots, part_limit - a.own_chunks);
+        a.history_chunk = div_up(div_up(r.max_prefix, a.history_chunks), step) * step;
+        const uint64_t combos = (uint64_t)r.n_groups * r.kv_heads * a.history_chunks;
+        SEQ_REQUIRE(combos < (1u << 30), "too many groups, heads and chunks for one launch");
+        a.history_combos = (uint32_t)combos;
+        history_groups = (combos >= 8 ? (combos + 7) / 8 * 8 : combos) * a.history_tiles;
+    }
+    SEQ_REQUIRE(history_groups + own_groups < (1ull << 31) && own_items < (1ull << 31), "too many requests, heads and chunks for one launch");
+    a.history_groups = (uint32_t)history_groups;
+    a.own_items = (uint32_t)own_items;
+    const uint32_t parts = a.history_chunks + a.own_chunks;
+    a.direct = parts == 1;
+    const uint32_t groups = (uint32_t)(history_groups + own_groups);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, groups, parts, st) : launch<__bf16>(a, groups, parts, st));
+    return HPS_OK;
+}
+
+}  // extern "C"

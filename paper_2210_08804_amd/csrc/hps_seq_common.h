@@ -1,0 +1,30 @@
+// What the two files behind hps_seq.h share.  Not part of the C ABI, and not exported.
+#ifndef HPS_SEQ_COMMON_H
+#define HPS_SEQ_COMMON_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "hps_seq.h"
+
+// Stores the message of hps_seq_last_error() (no allocation, so nothing can be thrown) and returns `code`.
+__attribute__((visibility("hidden"))) hps_status_t hps_seq_fail(hps_status_t code, const char *what, const char *more = "");
+
+#define SEQ_TRY(expr)                                                                                                          \
+    do {                                                                                                                       \
+        hipError_t e_ = (expr);                                                                                                \
+        if (e_ != hipSuccess)                                                                                                  \
+            return hps_seq_fail(e_ == hipErrorOutOfMemory ? HPS_ERR_OOM : HPS_ERR_DEVICE, #expr ": ", hipGetErrorString(e_));  \
+    } while (0)
+
+#define SEQ_REQUIRE(cond, msg)                                      \
+    do {                                                            \
+        if (!(cond)) return hps_seq_fail(HPS_ERR_INVALID_ARG, msg); \
+    } while (0)
+
+inline bool seq_aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool seq_words(const void *p) { return p && seq_aligned(p, 4); }                  // an int32 array that is there
+inline bool seq_block_size(uint32_t b) { return b != 0 && (b & (b - 1)) == 0 && b <= HPS_SEQ_MAX_BLOCK; }
+
+#endif  // HPS_SEQ_COMMON_H
