@@ -85,150 +85,180 @@ __device__ __forceinline__ float both_sum(float x) {
     return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
 
-// 64 lanes' 16 bytes from base + off to LDS at `to` + 16 * lane.  The caller waits for vmcnt; lanes that are switched
-// off leave their place in LDS alone.  (Not the builtin: the compiler then waits for every such load in front of any
-// read of LDS, and the next step's loads are what is to stay in flight.)
+// 64 lanes' 16 bytes from base + off (or from an address of each lane) to LDS at `to` + 16 * lane.  The caller waits for vmcnt;
+// lanes that are switched off leave their place in LDS alone.  (Not the builtin: the compiler then waits for every such
+// load in front of any read of LDS, and the next step's loads are what is to stay in flight.)
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// What one wave attends with: 32 rows against keys first .. end of one table.
+// Keeps x in its 16 adjacent registers.  Where a loop's vector starts as a constant or is put together from elements, the
+// compiler takes it to pieces for the loop, and moves them into place in front of every matrix instruction.
+__device__ __forceinline__ void whole(f32x16 &x) { asm("" : "+v"(x)); }
+
+// What a wave attends with: 32 rows against keys first .. end of one table.
 struct Item {
     const int32_t *table;
-    uint32_t width, first, end;
+    uint32_t first, end;
     uint32_t token0, row0, rows;                       // the tile's rows are row0 .. of `rows` (token, head) pairs from token0 on
     uint32_t head, part;                               // key/value head; part that the result is
     int32_t causal_from;                               // row's query i sees keys below causal_from + i; or kAll
 };
 constexpr int32_t kAll = 0x7FFFFFFF;
 
-template <typename T, int DT> struct Engine {          // head_dim <= 32 * DT
+template <typename T, int DT, bool kExact> struct Engine {                  // head_dim <= 32 * DT, or just that
     typedef typename Type<T>::frag frag;
-    static constexpr int kRow = DT <= 2 ? 128 : DT <= 4 ? 256 : 512;    // bytes of a row in LDS
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    static constexpr int kRow = DT <= 2 ? 128 : DT <= 4 ? 256 : 512;        // bytes of a row in LDS
     static constexpr int kChunks = kRow / 16, kSteps = 2 * DT;
     static constexpr int kLoads = 16 * kRow / 1024, kLoadRows = 1024 / kRow;        // wave loads of 16 rows, rows of one
     static constexpr uint32_t kLds = 256 * kRow;       // wide: 2 stages of 64 keys and values; narrow: 4 waves of 32
+    static constexpr uint32_t kWaveLds = 64 * kRow;    // of a narrow wave
+    static constexpr uint32_t kStage = 128 * kRow, kWideValues = 64 * kRow, kNarrowValues = 32 * kRow;
 
     const Args &a;
+    const Item it;
     const uint32_t lane, half, lds;
+    const char *const k_head, *const v_head;
     frag q[kSteps];
     f32x16 o[DT];
     float m, l;
     int32_t limit;                                     // the lane's row sees keys below it
-    uint32_t k_at, v_at[2];                            // LDS addresses of the lane's first key and value operands
-    uint32_t k_off[kLoads], v_off[kLoads];             // offsets of its 16 bytes of each wave load of 16 rows
+    // The lane's places, as a row's offset and a chunk's within the row: the operands of both products in LDS, and the 16
+    // bytes that it loads.  The other chunks are reached by an exclusive or, one instruction each (`fresh` keeps the
+    // compiler from holding all of them in registers instead, which cost spills in the middle of the loop).
+    uint32_t k_row, k_chunk, v_row, v_chunk, load_row, load_k, load_v;
+    uint32_t here;                                     // LDS address of the keys at hand
 
     static __device__ __forceinline__ uint32_t sw_k(uint32_t t) { return t & (kRow == 128 ? 7u : 15u); }
     static __device__ __forceinline__ uint32_t sw_v(uint32_t t) { return ((kRow == 128 ? (t >> 1) & 1u : t & 3u) << 2) | ((t >> 2) & 3u); }
+    template <bool kValues> static __device__ __forceinline__ uint32_t sw(uint32_t t) { return kValues ? sw_v(t) : sw_k(t); }
 
-    __device__ __forceinline__ Engine(const Args &args, uint32_t lds_base) : a(args), lane(threadIdx.x & 63u), half(lane >> 5), lds(lds_base) {
+    __device__ __forceinline__ Engine(const Args &args, const Item &item, uint32_t lds_base, uint32_t first_row)
+        : a(args), it(item), lane(threadIdx.x & 63u), half(lane >> 5), lds(lds_base), k_head(args.k + (int64_t)item.head * args.page_head),
+          v_head(args.v + (int64_t)item.head * args.page_head) {
         const uint32_t n = lane & 31u, g = lane & 15u;
-        k_at = n * kRow + ((half ^ sw_k(n)) << 4);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t t = 4 * half + 8 * j + (g >> 2);
-            v_at[j] = t * kRow + (((2 * ((lane >> 4) & 1u) + ((g & 3u) >> 1)) ^ sw_v(t)) << 4) + (g & 1u) * 8;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint32_t t = i * kLoadRows + lane / kChunks, pos = lane % kChunks;
-            k_off[i] = t * (uint32_t)a.page_token + ((pos ^ sw_k(t)) << 4);
-            v_off[i] = t * (uint32_t)a.page_token + ((pos ^ sw_v(t)) << 4);
-        }
-    }
-
-    // Rows of 16 keys (or values) from token `at` on: whole ones straight to LDS; at the end of the keys, for small blocks
-    // and for a block number that is none, through registers, zeros in the place of what is not there.
-    // Returns whether the loads are still under way.
-    __device__ __forceinline__ bool load16(const Item &it, const char *pages, const uint32_t (&off)[kLoads], bool values, uint32_t at, int32_t id, uint32_t to) {
-        const char *head = pages + (int64_t)it.head * a.page_head;
-        if (a.sh >= 4 && at + 16 <= it.end && (uint32_t)id < a.n_blocks) {
-            const char *base = head + (int64_t)id * a.page_block + (int64_t)(at & ((1u << a.sh) - 1u)) * a.page_token;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ (values ? sw_v(t) : sw_k(t));
-                if (kChunks * 8 == 32 * DT && a.head_dim == 32 * DT) load_to_lds(base, off[i], lds + to + i * 1024);       // uniform
-                else if (chunk * 8 < a.head_dim) load_to_lds(base, off[i], lds + to + i * 1024);
-            }
-            return true;
-        }
-        for (int i = 0; i < kLoads; ++i) {
-            const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ (values ? sw_v(t) : sw_k(t)), key = at + t;
-            u32x4 x = {0, 0, 0, 0};
-            if (chunk * 8 < a.head_dim && key < it.end) {
-                const uint32_t b = (uint32_t)it.table[key >> a.sh];
-                if (b < a.n_blocks) x = *(const u32x4 *)(head + (int64_t)b * a.page_block + (int64_t)(key & ((1u << a.sh) - 1u)) * a.page_token + chunk * 16);
-                else atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
-            }
-            *(__attribute__((address_space(3))) u32x4 *)(lds_char *)(uintptr_t)(lds + to + i * 1024 + lane * 16) = x;
-        }
-        return false;
-    }
-    // Block of the 16 keys from `at` on; -1 where they are not all there or blocks are smaller.
-    __device__ __forceinline__ int32_t block_of(const Item &it, uint32_t at) const {
-        return a.sh >= 4 && at < it.end ? scalar(it.table, at >> a.sh) : -1;
-    }
-
-    __device__ __forceinline__ void begin(const Item &it, uint32_t row_of_wave) {
-        const uint32_t row = it.row0 + row_of_wave + (lane & 31u), i = row / a.ratio;
+        here = lds;
+        k_row = lds + n * kRow;
+        k_chunk = (half ^ sw_k(n)) << 4;
+        const uint32_t t = 4 * half + (g >> 2), r = lane / kChunks;
+        v_row = lds + t * kRow;
+        v_chunk = ((2 * ((lane >> 4) & 1u) + ((g & 3u) >> 1)) ^ sw_v(t)) << 4 | (g & 1u) << 3;
+        load_row = r * (uint32_t)a.page_token;
+        load_k = (lane % kChunks ^ sw_k(r)) << 4;
+        load_v = (lane % kChunks ^ sw_v(r)) << 4;
+        const uint32_t row = it.row0 + first_row + n, i = row / a.ratio;
         const bool there = row < it.rows;
         limit = it.causal_from == kAll ? (int32_t)it.end : min((int32_t)it.end, it.causal_from + (int32_t)i);
         const char *src = a.q + (int64_t)(it.token0 + i) * a.q_token + (int64_t)(it.head * a.ratio + (row - i * a.ratio)) * a.q_head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             u32x4 x = {0, 0, 0, 0};
-            if (there && (uint32_t)(16 * s + 8 * half) < a.head_dim) x = *(const u32x4 *)(src + (16 * s + 8 * half) * 2);
+            if (there && (kExact || (uint32_t)(16 * s + 8 * half) < a.head_dim)) x = *(const u32x4 *)(src + (16 * s + 8 * half) * 2);
             q[s] = __builtin_bit_cast(frag, x);
         }
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+        for (int d = 0; d < DT; ++d) {
+            o[d] = f32x16{};
+            whole(o[d]);
+        }
         m = -kInf;
         l = 0.f;
         if (!there) limit = kAll;                      // their results go nowhere
     }
 
-    // Scores of 32 keys whose rows start at `at` in LDS.
-    __device__ __forceinline__ f32x16 scores(uint32_t at) const {
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(k_chunk), "+v"(v_chunk), "+v"(load_k), "+v"(load_v)); }
+    // of key operand i; of value operand d, its second half 8 rows on
+    __device__ __forceinline__ lds_char *k_at(int i) const { return (lds_char *)(uintptr_t)(k_row + (k_chunk ^ (uint32_t)(i << 5))); }
+    __device__ __forceinline__ lds_char *v_at(int j, int d) const { return (lds_char *)(uintptr_t)(v_row + (v_chunk ^ (uint32_t)(d << 6) ^ (uint32_t)(j << 5))) + j * 8 * kRow; }
+
+    // Block of the 16 keys from `at` on; -1 where there are none, or where blocks are smaller.
+    __device__ __forceinline__ int32_t block_of(uint32_t at) const { return a.sh >= 4 && at < it.end ? scalar(it.table, at >> a.sh) : -1; }
+
+    // Rows of 16 keys (or values) from token `at` on to LDS.  Whole ones of a block: returns true, the loads are under way,
+    // kLoads of them.  At the end of the keys, for small blocks and for a block number that is none: each lane by itself,
+    // zeros in the place of what is not there.
+    template <bool kValues> __device__ __forceinline__ bool load16(uint32_t at, int32_t id, uint32_t to) {
+        const char *head = kValues ? v_head : k_head;
+        if (__builtin_expect(at + 16 <= it.end && (uint32_t)id < a.n_blocks, 1)) {
+            const char *base = head + (int64_t)id * a.page_block + (int64_t)(at & ((1u << a.sh) - 1u)) * a.page_token;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t chunk = (kValues ? load_v : load_k) ^ sw<kValues>(i * kLoadRows) << 4;
+                if (kExact || chunk < 2 * a.head_dim) load_to_lds(base + (int64_t)(i * kLoadRows) * a.page_token, load_row + chunk, to + i * 1024);
+            }
+            return true;
+        }
+#pragma unroll 1
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ sw<kValues>(t), key = at + t;
+            if (!kExact && chunk * 8 >= a.head_dim) continue;               // nothing ever lies there
+            const char *from = nullptr;
+            if (key < it.end) {
+                const uint32_t b = (uint32_t)it.table[key >> a.sh];
+                if (b < a.n_blocks) from = head + (int64_t)b * a.page_block + (int64_t)(key & ((1u << a.sh) - 1u)) * a.page_token + chunk * 16;
+                else atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
+            }
+            if (from) load_to_lds(from, to + i * 1024);
+            else *(lds_u32x4 *)(lds_char *)(uintptr_t)(to + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+        return false;
+    }
+
+    template <bool kValues> __device__ __forceinline__ bool load32(uint32_t at, int32_t id0, int32_t id1, uint32_t to) {
+        const bool x = load16<kValues>(at, id0, to), y = load16<kValues>(at + 16, id1, to + 16 * kRow);
+        return x && y;
+    }
+
+    // Scores of 32 keys, kAt bytes behind the first ones.
+    template <int kAt> __device__ __forceinline__ f32x16 scores() const {
         f32x16 s{};
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const frag x = *(__attribute__((address_space(3))) frag *)(lds_char *)(uintptr_t)(lds + at + (k_at ^ (uint32_t)(i << 5)));
-            s = Type<T>::mfma(x, q[i], s);
-        }
+        for (int i = 0; i < kSteps; ++i) s = Type<T>::mfma(*(__attribute__((address_space(3))) frag *)(k_at(i) + kAt), q[i], s);
         return s;
     }
-    __device__ __forceinline__ static uint32_t key_of(int i, uint32_t half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+    static __device__ __forceinline__ uint32_t key_of(int i, uint32_t half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
-    // Scores to weights, in place; `seen` gets a bit for each of the lane's keys where some are hidden.
-    template <int N> __device__ __forceinline__ void weights(f32x16 (&s)[N], uint32_t at, bool masked, uint32_t (&seen)[N]) {
-        if (masked) {
+    // Hides what the lane's row does not see; a bit for each key that it sees.
+    __device__ __forceinline__ uint32_t hide(f32x16 &s, uint32_t at) const {
+        uint32_t seen = 0;
 #pragma unroll
-            for (int t = 0; t < N; ++t) {
-                seen[t] = 0;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool see = (int32_t)(at + 32 * t + key_of(i, half)) < limit;
-                    seen[t] |= see ? 1u << i : 0u;
-                    s[t][i] = see ? s[t][i] : -kInf;
-                }
-            }
+        for (int i = 0; i < 16; ++i) {
+            const bool see = (int32_t)(at + key_of(i, half)) < limit;
+            seen |= see ? 1u << i : 0u;
+            s[i] = see ? s[i] : -kInf;
         }
+        return seen;
+    }
+
+    // The row's largest score, in powers of two.
+    template <int N> __device__ __forceinline__ float largest(const f32x16 (&s)[N]) const {
         float top = s[0][0];
 #pragma unroll
         for (int t = 0; t < N; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = both_max(top) * a.c;
-        if (__ballot(top > m + kSlack)) {              // also the first one: m is -inf
-            const float next = fmaxf(m, top), ref = next == -kInf ? 0.f : next, f = exp2_(m - ref);
-            l *= f;
+        return both_max(top) * a.c;
+    }
+    // Moves the reference to the largest score so far, and what was summed with it.
+    __device__ __forceinline__ void move(float top) {
+        const float next = fmaxf(m, top), ref = next == -kInf ? 0.f : next, f = exp2_(m - ref);
+        l *= f;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= f;
-            m = next;
+        for (int d = 0; d < DT; ++d) {
+            o[d] *= f;
+            whole(o[d]);
         }
+        m = next;
+    }
+    // Scores to weights, in place.
+    template <int N> __device__ __forceinline__ void weights(f32x16 (&s)[N]) {
         const float ref = m == -kInf ? 0.f : m;
         float sum = 0.f;
 #pragma unroll
@@ -241,190 +271,241 @@ template <typename T, int DT> struct Engine {          // head_dim <= 32 * DT
         l += sum;
     }
 
-    __device__ __forceinline__ frag values(uint32_t at, int d) const {
+    template <int kAt> __device__ __forceinline__ frag values(int d) const {
         s16x4 x[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_char *)(uintptr_t)(lds + at + (v_at[j] ^ (uint32_t)(d << 6))));
+            x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(v_at(j, d) + kAt));
         return __builtin_bit_cast(frag, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
-    // o += weights x values of 32 keys whose rows start at `at`.
-    __device__ __forceinline__ void add_values(const f32x16 &w, uint32_t at) {
+    // o += weights x values of 32 keys, kAt bytes behind the first ones.
+    template <int kAt> __device__ __forceinline__ void add_values(const f32x16 &w) {
+        frag p[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            frag p;
+        for (int j = 0; j < 16; ++j) p[j / 8][j % 8] = (T)w[j];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = (T)w[8 * u + j];
+        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt>(d), p[0], o[d]);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values(at + 16 * u * kRow, d), p, o[d]);
-        }
+        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt + 16 * kRow>(d), p[1], o[d]);
     }
-    // The same where some rows do not see some keys: a hidden value that is not finite must not meet the weight 0, so the
-    // values that are not finite are left out of the product and added, as what they are, to the rows that see them.
-    __device__ __forceinline__ void add_values_masked(const f32x16 &w, uint32_t seen, uint32_t at) {
+    // Whether any value of 32 keys, kAt bytes behind the first ones, is not finite.
+    template <int kAt> __device__ __forceinline__ bool any_odd() const {
+        constexpr uint32_t e = Type<T>::kExp;
+        uint32_t odd = 0;
 #pragma unroll 1
-        for (int u = 0; u < 2; ++u) {
-            frag p, sees;
+        for (uint32_t x = lane * 16; x < 32 * kRow; x += 64 * 16) {
+            const u32x4 y = *(lds_u32x4 *)((lds_char *)(uintptr_t)(here + x) + kAt);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                p[j] = (T)(u ? w[8 + j] : w[j]);
-                sees[j] = (T)(float)(seen >> (8 * u + j) & 1u);
-            }
+            for (int j = 0; j < 4; ++j) odd |= (uint32_t)((y[j] & e) == e) | (uint32_t)((y[j] >> 16 & e) == e);
+        }
+        return __ballot(odd) != 0;
+    }
+    // o += weights x values where some rows do not see some keys.  A hidden value that is not finite must not meet the
+    // weight 0: where there is any that is not finite, the products are formed one by one, with the same rounding.
+    template <int kAt> __device__ __forceinline__ void add_values_hidden(const f32x16 &w, uint32_t seen) {
+        if (!__builtin_expect(any_odd<kAt>(), 0)) return add_values<kAt>(w);
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i) {                 // keys; the lane holds the weights of those with bit 2 as its half
+            const int mine = (i >> 3) * 4 + (i & 3);
+            float x = 0.f;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const s16x8 x = __builtin_bit_cast(s16x8, values(at + 16 * u * kRow, d));
-                s16x8 fine = x;
-                frag odd{};
-                bool any = false;
+            for (int j = 0; j < 16; ++j) x = j == mine ? w[j] : x;
+            const u32x2 both = __builtin_amdgcn_permlane32_swap(__float_as_uint((float)(T)x), __float_as_uint((float)(T)x), false, false);
+            const u32x2 sees = __builtin_amdgcn_permlane32_swap(seen >> mine & 1u, seen >> mine & 1u, false, false);
+            const float wi = __uint_as_float(i & 4 ? both.y : both.x);
+            const bool see = i & 4 ? sees.y : sees.x;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t b = (uint16_t)x[j];
-                    if ((b & Type<T>::kExp) != Type<T>::kExp) continue;
-                    any = true;
-                    fine[j] = 0;
-                    odd[j] = (T)((b & 0x7FFFu) != Type<T>::kExp ? 4096.f : b & 0x8000u ? 64.f : 1.f);      // NaN, -inf, +inf: 16 keys of each tell apart
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t dim = 32 * d + key_of(j, half);
+                    const float v = (float)*(__attribute__((address_space(3))) T *)((lds_char *)(uintptr_t)(here + i * kRow + ((dim / 8 ^ sw_v(i)) << 4) + dim % 8 * 2) + kAt);
+                    o[d][j] += see ? wi * v : 0.f;
                 }
-                o[d] = Type<T>::mfma(__builtin_bit_cast(frag, fine), p, o[d]);
-                if (__ballot(any)) {
-                    f32x16 n = Type<T>::mfma(odd, sees, f32x16{});
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t k = (uint32_t)n[i];
-                        if (k >= 4096u) o[d][i] = __builtin_nanf("");
-                        if (k & 4095u & ~63u) o[d][i] -= kInf;
-                        if (k & 63u) o[d][i] += kInf;
-                    }
-                }
-            }
         }
     }
 
-    __device__ __forceinline__ int32_t least_limit() const {                // over the wave's rows
-        int32_t x = limit;
+    __device__ __forceinline__ uint32_t least_limit() const {               // over the wave's rows
+        int32_t x = max(limit, 0);
         for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
-        return x;
+        return uniform((uint32_t)x);
     }
 
     // A work-group's four waves have 32 rows each and share keys and values: 64 a step, two stages, one meeting a step.
-    __device__ __forceinline__ void wide(const Item &it) {
-        const uint32_t wave = uniform(threadIdx.x >> 6);
-        begin(it, 32 * wave);
-        const int32_t least = (int32_t)uniform((uint32_t)least_limit());
-        constexpr uint32_t kStage = 2 * 64 * kRow, kValues = 64 * kRow;
-        uint32_t at = it.first + 16 * wave, stage = 0;
-        int32_t id = block_of(it, at), next = block_of(it, at + 64);
-        load16(it, a.k, k_off, false, at, id, 16 * wave * kRow);
-        load16(it, a.v, v_off, true, at, id, kValues + 16 * wave * kRow);
-        for (uint32_t k0 = it.first; k0 < it.end; k0 += 64) {
+    // The inner loop has the steps of which every row sees all keys and whose reference stays; the others leave it.
+    __device__ __forceinline__ void wide() {
+        const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit();
+        const uint32_t mine = lds + 16 * wave * kRow;
+        uint32_t at = it.first + 16 * wave, k0 = it.first, stage = 0;
+        int32_t next = block_of(at);
+        if (k0 >= it.end) return;                      // uniform in the work-group, as are the turns of both loops together
+        auto fetch = [&](uint32_t to) {
+            const int32_t id = next;
+            next = block_of(at + 64);
+            load16<false>(at, id, to);
+            load16<true>(at, id, to + kWideValues);
+            at += 64;
+        };
+        auto turn = [&] {
             wait_loads<0>();
             meet();                                    // everybody's rows are there, and everybody is done with the other stage
-            if (k0 + 64 < it.end) {                    // uniform
-                at += 64;
-                id = next;
-                next = block_of(it, at + 64);
-                const uint32_t to = (stage ^ kStage) + 16 * wave * kRow;
-                load16(it, a.k, k_off, false, at, id, to);
-                load16(it, a.v, v_off, true, at, id, to + kValues);
-            }
-            f32x16 s[2];
-            uint32_t seen[2];
-            s[0] = scores(stage);
-            s[1] = scores(stage + 32 * kRow);
-            const bool masked = (int32_t)(k0 + 64) > least;
-            weights<2>(s, k0, masked, seen);
-            if (masked && it.causal_from != kAll) {
-                add_values_masked(s[0], seen[0], stage + kValues);
-                add_values_masked(s[1], seen[1], stage + kValues + 32 * kRow);
-            } else {
-                add_values(s[0], stage + kValues);
-                add_values(s[1], stage + kValues + 32 * kRow);
-            }
-            stage ^= kStage;
-        }
-    }
-
-    // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon as the
-    // scores are there, the next values behind the product with these.
-    __device__ __forceinline__ void narrow(const Item &it, uint32_t from, uint32_t stride, uint32_t base) {
-        begin(it, 0);
-        const int32_t least = (int32_t)uniform((uint32_t)least_limit());
-        const uint32_t vbase = base + 32 * kRow;
-        if (from >= it.end) return;
-        int32_t id0 = block_of(it, from), id1 = block_of(it, from + 16);
-        bool k_flies, v_flies;                         // uniform
-        auto load = [&](bool values, uint32_t at) {
-            bool x;
-            if (values) x = load16(it, a.v, v_off, true, at, id0, vbase), x &= load16(it, a.v, v_off, true, at + 16, id1, vbase + 16 * kRow);
-            else x = load16(it, a.k, k_off, false, at, id0, base), x &= load16(it, a.k, k_off, false, at + 16, id1, base + 16 * kRow);
-            return x;
+            if (k0 + 64 < it.end) fetch(mine + (kStage - stage));
         };
-        k_flies = load(false, from);
-        v_flies = load(true, from);
-        for (uint32_t at = from; at < it.end; at += stride) {
-            const bool more = at + stride < it.end;
-            int32_t n0 = -1, n1 = -1;
-            if (more) n0 = block_of(it, at + stride), n1 = block_of(it, at + stride + 16);
-            if (k_flies && v_flies) wait_loads<2 * kLoads>();
-            else wait_loads<0>();
-            f32x16 s[1];
-            uint32_t seen[1];
-            s[0] = scores(base);
-            id0 = n0;
-            id1 = n1;
-            if (more) {
-                wait_lds();
-                k_flies = load(false, at + stride);
+        auto other = [&] {
+            const uint32_t by = kStage - 2 * stage;    // there or back
+            k_row += by;
+            v_row += by;
+            here += by;
+            stage += by;
+            k0 += 64;
+        };
+        fetch(mine);
+        for (;;) {
+            f32x16 s[2];
+            float top;
+            bool full;
+            for (;;) {
+                if (k0 >= it.end) return;
+                turn();
+                fresh();
+                s[0] = scores<0>();
+                s[1] = scores<32 * kRow>();
+                full = k0 + 64 <= least;
+                if (!full) break;
+                top = largest<2>(s);
+                if (__ballot(top > m + kSlack)) break;                      // also the first time: m is -inf
+                weights<2>(s);
+                add_values<kWideValues>(s[0]);
+                add_values<kWideValues + 32 * kRow>(s[1]);
+                other();
             }
-            const bool masked = (int32_t)(at + 32) > least;
-            weights<1>(s, at, masked, seen);
-            if (more && k_flies && v_flies) wait_loads<2 * kLoads>();
-            else wait_loads<0>();
-            if (masked && it.causal_from != kAll) add_values_masked(s[0], seen[0], vbase);
-            else add_values(s[0], vbase);
-            if (more) {
-                wait_lds();
-                v_flies = load(true, at + stride);
+            uint32_t seen[2] = {0xFFFFu, 0xFFFFu};
+            if (!full) {
+                seen[0] = hide(s[0], k0);
+                seen[1] = hide(s[1], k0 + 32);
+                top = largest<2>(s);
             }
+            move(top);
+            weights<2>(s);
+            if (!full && it.causal_from != kAll) {     // uniform
+                add_values_hidden<kWideValues>(s[0], seen[0]);
+                add_values_hidden<kWideValues + 32 * kRow>(s[1], seen[1]);
+            } else {
+                add_values<kWideValues>(s[0]);
+                add_values<kWideValues + 32 * kRow>(s[1]);
+            }
+            other();
         }
     }
 
-    // One row's values 32 * d + 8 * i4 + 4 * half ..: to their place, final or as a part.
-    __device__ __forceinline__ void put4(const Item &it, uint32_t row, int d, int i4, f32x4 x, float f) const {
-        const uint32_t dim = 32 * d + 8 * i4 + 4 * half, i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
-        if (dim >= a.head_dim) return;
-        if (a.direct) {
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            t4 y;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = (T)(x[j] * f);
-            *(t4 *)(a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head + dim * 2) = y;
-        } else {
-            *(f32x4 *)(a.part_o + (((size_t)it.part * a.n_tokens + t) * a.q_heads + h) * a.head_dim + dim) = x;
+    // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon
+    // as the scores are there, the next values behind the product with these.
+    __device__ __forceinline__ void narrow(uint32_t from, uint32_t stride) {
+        const uint32_t least = least_limit();
+        if (from >= it.end) return;
+        int32_t id0 = block_of(from), id1 = block_of(from + 16);
+        // whether the last keys and the last values asked for are under way, as 2 * kLoads loads each
+        bool keys_fly = load32<false>(from, id0, id1, lds), values_fly = load32<true>(from, id0, id1, lds + kNarrowValues);
+        for (uint32_t at = from;;) {
+            f32x16 s[1];
+            float top;
+            bool full, more;
+            uint32_t next;
+            auto next_values = [&] {
+                if (more) {
+                    wait_lds();
+                    values_fly = load32<true>(next, id0, id1, lds + kNarrowValues);
+                }
+                at = next;
+            };
+            auto wait_values = [&] {
+                if (more && keys_fly && values_fly) wait_loads<2 * kLoads>();
+                else wait_loads<0>();
+            };
+            for (;;) {
+                if (at >= it.end) return;
+                next = at + stride;
+                more = next < it.end;
+                fresh();
+                id0 = block_of(next);
+                id1 = block_of(next + 16);
+                if (keys_fly && values_fly) wait_loads<2 * kLoads>();
+                else wait_loads<0>();
+                s[0] = scores<0>();
+                if (more) {
+                    wait_lds();
+                    keys_fly = load32<false>(next, id0, id1, lds);
+                }
+                full = at + 32 <= least;
+                if (!full) break;
+                top = largest<1>(s);
+                if (__ballot(top > m + kSlack)) break;
+                weights<1>(s);
+                wait_values();
+                add_values<kNarrowValues>(s[0]);
+                next_values();
+            }
+            uint32_t seen = 0xFFFFu;
+            if (!full) {
+                seen = hide(s[0], at);
+                top = largest<1>(s);
+            }
+            move(top);
+            weights<1>(s);
+            wait_values();
+            if (!full && it.causal_from != kAll) add_values_hidden<kNarrowValues>(s[0], seen);
+            else add_values<kNarrowValues>(s[0]);
+            next_values();
         }
     }
-    __device__ __forceinline__ void put_sums(const Item &it, uint32_t row, float ref, float sum) const {
-        const uint32_t i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio);
-        const size_t at = (size_t)(it.token0 + i) * a.q_heads + h;
-        if (!a.direct) a.part_ml[(size_t)it.part * a.n_tokens * a.q_heads + at] = make_float2(ref, sum);
-        else if (a.lse) a.lse[at] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+
+    // Where a row's values go: final, or as a part.
+    struct Place {
+        char *to;
+        bool direct;
+        float f;
+        uint32_t dims;
+        __device__ __forceinline__ void put4(uint32_t dim, f32x4 x) const {
+            if (!kExact && dim >= dims) return;
+            if (direct) {
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                t4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = (T)(x[j] * f);
+                *(t4 *)(to + dim * 2) = y;
+            } else {
+                *(f32x4 *)(to + dim * 4) = x;
+            }
+        }
+    };
+    // Stores the row's reference and sum (one lane of it), and returns its place.
+    __device__ __forceinline__ Place place(uint32_t row, float ref, float sum, bool first) const {
+        const uint32_t i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
+        const size_t at = (size_t)t * a.q_heads + h, part = (size_t)it.part * a.n_tokens * a.q_heads + at;
+        if (first) {
+            if (!a.direct) a.part_ml[part] = make_float2(ref, sum);
+            else if (a.lse) a.lse[at] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+        }
+        return {a.direct ? a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head : (char *)(a.part_o + part * a.head_dim), a.direct != 0, sum == 0.f ? 0.f : 1.f / sum,
+                a.head_dim};
     }
     // The wave's own rows, as they are.
-    __device__ __forceinline__ void finish(const Item &it, uint32_t row_of_wave) {
-        const uint32_t row = it.row0 + row_of_wave + (lane & 31u);
-        const float sum = both_sum(l), f = sum == 0.f ? 0.f : 1.f / sum;
+    __device__ __forceinline__ void finish(uint32_t first_row) {
+        const uint32_t row = it.row0 + first_row + (lane & 31u);
+        const float sum = both_sum(l);
         if (row >= it.rows) return;
-        if (half == 0) put_sums(it, row, m, sum);
-        if (!a.direct && sum == 0.f) return;
+        const Place p = place(row, m, sum, half == 0);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) put4(it, row, d, i, f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, f);
+            for (int i = 0; i < 4; ++i) p.put4(32 * d + 8 * i + 4 * half, f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]});
     }
     // The four waves have the same rows and different keys: joined through LDS, each wave a quarter of the values.
-    __device__ __forceinline__ void finish_split(const Item &it, char *shared, float2 *l_ml) {
+    __device__ __forceinline__ void finish_split(char *shared) {
         const uint32_t wave = uniform(threadIdx.x >> 6), row = it.row0 + (lane & 31u);
         const float sum = both_sum(l);
+        float2 *l_ml = (float2 *)(shared + kLds);
         __syncthreads();
         f32x4 *l_o = (f32x4 *)shared;                  // [wave][DT * 4][64]
 #pragma unroll
@@ -445,14 +526,14 @@ template <typename T, int DT> struct Engine {          // head_dim <= 32 * DT
             total += f[w] * x.y;
         }
         if (row >= it.rows) return;
-        if (wave == 0 && half == 0) put_sums(it, row, ref, total);
-        if (!a.direct && total == 0.f) return;
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        for (int x = wave * DT; x < (int)(wave + 1) * DT; ++x) {
+        const Place p = place(row, ref, total, wave == 0 && half == 0);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const uint32_t x = wave * DT + i;
             f32x4 y{};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) y += f[w] * l_o[(w * DT * 4 + x) * 64 + lane];
-            put4(it, row, x >> 2, x & 3, y, inv);
+            p.put4(8 * x + 4 * half, y);
         }
     }
 };
@@ -474,12 +555,12 @@ __device__ __forceinline__ uint32_t length(const Args &a, int32_t x, uint32_t wi
     return min(n, fits);
 }
 
-template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) attend_kernel(const Args a) {
-    typedef Engine<T, DT> E;
+template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kThreads, DT <= 4 ? 2 : 1) attend_kernel(const Args a) {
+    typedef Engine<T, DT, kExact> E;
     extern __shared__ __align__(16) char shared[];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_char *)shared;
-    if (a.head_dim != 32 * DT) {                       // places of LDS rows that no load fills
+    if (!kExact || DT == 3) {                          // places of LDS rows that no load fills
         for (uint32_t x = threadIdx.x * 16; x < E::kLds; x += kThreads * 16) *(u32x4 *)(shared + x) = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
@@ -497,8 +578,10 @@ template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 
             combo = blockIdx.x % a.history_combos;
             tile = blockIdx.x / a.history_combos;
         }
-        it.head = combo % a.kv_heads;
+        // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
+        // side by side, one head's rows are in few of the L2's channels.
         const uint32_t rest = combo / a.kv_heads, chunk = rest % a.history_chunks, g = rest / a.history_chunks;
+        it.head = (combo + rest) % a.kv_heads;
         const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
         const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
         const uint32_t n = t1 > t0 ? t1 - t0 : 0;
@@ -509,7 +592,6 @@ template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 
         it.row0 = tile * (is_wide ? kWideRows : kNarrowRows);
         if (it.row0 >= it.rows) return;
         it.table = a.prefix_table + (size_t)g * a.prefix_width;
-        it.width = a.prefix_width;
         it.first = chunk * a.history_chunk;
         it.end = min(length(a, scalar(a.prefix_lens, g), a.prefix_width, a.max_prefix), it.first + a.history_chunk);
         it.causal_from = kAll;
@@ -536,7 +618,6 @@ template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 
         if (it.row0 >= it.rows) return;
         const uint32_t len = length(a, scalar(a.lens, r), a.table_width, a.max_len);
         it.table = a.block_table + (size_t)r * a.table_width;
-        it.width = a.table_width;
         it.first = chunk * a.own_chunk;
         const int32_t from = (int32_t)len - (int32_t)n + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
         it.causal_from = n > 1 ? from : kAll;
@@ -549,17 +630,15 @@ template <typename T, int DT> __global__ void __launch_bounds__(kThreads, DT <= 
         mark_empty(a, it, it.part, is_wide ? kWideRows : kNarrowRows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
         return;
     }
-    E e(a, lds_base);
-    constexpr uint32_t kWave = 2 * 32 * E::kRow;       // a narrow wave's part of LDS
     if (is_wide) {
-        e.wide(it);
-        e.finish(it, 32 * wave);
-    } else if (solo) {
-        e.narrow(it, it.first, 32, wave * kWave);
-        e.finish(it, 0);
+        E e(a, it, lds_base, 32 * wave);
+        e.wide();
+        e.finish(32 * wave);
     } else {
-        e.narrow(it, it.first + 32 * wave, 32 * kWaves, wave * kWave);
-        e.finish_split(it, shared, (float2 *)(shared + E::kLds));
+        E e(a, it, lds_base + wave * E::kWaveLds, 0);
+        e.narrow(solo ? it.first : it.first + 32 * wave, solo ? 32 : 32 * kWaves);
+        if (solo) e.finish(0);
+        else e.finish_split(shared);
     }
 }
 
@@ -652,13 +731,17 @@ struct hps_seq_attention_session {
 
 namespace {
 
-template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
-    constexpr uint32_t bytes = Engine<T, DT>::kLds + kWaves * 32 * sizeof(float2);
+template <typename T, int DT, bool kExact> hipError_t launch_attend(const Args &a, uint32_t groups, hipStream_t st) {
+    constexpr uint32_t bytes = Engine<T, DT, kExact>::kLds + kWaves * 32 * sizeof(float2);
     static_assert(bytes <= 160 * 1024, "LDS of a CU");
     if (bytes > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
-    hipLaunchKernelGGL((attend_kernel<T, DT>), dim3(groups), dim3(kThreads), bytes, st, a);
-    if (hipError_t e = hipGetLastError()) return e;
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT, kExact>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
+    hipLaunchKernelGGL((attend_kernel<T, DT, kExact>), dim3(groups), dim3(kThreads), bytes, st, a);
+    return hipGetLastError();
+}
+
+template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
+    if (hipError_t e = a.head_dim == 32 * DT ? launch_attend<T, DT, true>(a, groups, st) : launch_attend<T, DT, false>(a, groups, st)) return e;
     if (a.direct) return hipSuccess;
     constexpr int kLanes = DT == 1 ? 8 : DT == 2 ? 16 : DT <= 4 ? 32 : 64;
     const size_t rows = (size_t)a.n_tokens * a.q_heads;
