@@ -39,8 +39,8 @@ constexpr float kInf = __builtin_inff();
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr uint32_t kWideRows = 128, kNarrowRows = 32;  // rows of a work-group
 constexpr uint32_t kWideKeys = 64, kNarrowKeys = 32;   // keys of a step: of the work-group, of a wave
-// A row's reference m follows its maximum only when that is this far ahead (in powers of two): weights stay below 2^8,
-// and most steps need no rescaling.
+// A row's reference m need not be its maximum: it moves when a score is this far ahead (in powers of two), or weights sum to
+// Type::kMost, which is within the type's range.  Most steps need no rescaling then; precision is relative and the same.
 constexpr float kSlack = 8.f;
 
 struct Args {
@@ -65,11 +65,13 @@ template <> struct Type<__bf16> {
     typedef bf16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7F80u;
+    static constexpr float kMost = 0x1p40f;
 };
 template <> struct Type<_Float16> {
     typedef f16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7C00u;
+    static constexpr float kMost = 0x1p14f;
 };
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -238,12 +240,10 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     }
 
     // The row's largest score, in powers of two.
-    template <int N> __device__ __forceinline__ float largest(const f32x16 (&s)[N]) const {
-        float top = s[0][0];
+    __device__ __forceinline__ float largest(const f32x16 &s) const {
+        float top = s[0];
 #pragma unroll
-        for (int t = 0; t < N; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         return both_max(top) * a.c;
     }
     // Moves the reference to the largest score so far, and what was summed with it.
@@ -257,18 +257,17 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         }
         m = next;
     }
-    // Scores to weights, in place.
-    template <int N> __device__ __forceinline__ void weights(f32x16 (&s)[N]) {
-        const float ref = m == -kInf ? 0.f : m;
+    __device__ __forceinline__ float reference() const { return m == -kInf ? 0.f : m; }       // -inf: nothing but -inf so far
+    // Weights of 32 keys' scores, rounded for the second product, and their sum (of the lane's keys) before that.
+    __device__ __forceinline__ float weights(const f32x16 &s, frag (&w)[2], float ref) const {
         float sum = 0.f;
 #pragma unroll
-        for (int t = 0; t < N; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[t][i] = exp2_(__builtin_fmaf(s[t][i], a.c, -ref));
-                sum += s[t][i];
-            }
-        l += sum;
+        for (int i = 0; i < 16; ++i) {
+            const float x = exp2_(__builtin_fmaf(s[i], a.c, -ref));
+            sum += x;
+            w[i / 8][i % 8] = (T)x;
+        }
+        return sum;
     }
 
     template <int kAt> __device__ __forceinline__ frag values(int d) const {
@@ -280,14 +279,11 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     }
 
     // o += weights x values of 32 keys, kAt bytes behind the first ones.
-    template <int kAt> __device__ __forceinline__ void add_values(const f32x16 &w) {
-        frag p[2];
+    template <int kAt> __device__ __forceinline__ void add_values(const frag (&w)[2]) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) p[j / 8][j % 8] = (T)w[j];
+        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt>(d), w[0], o[d]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt>(d), p[0], o[d]);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt + 16 * kRow>(d), p[1], o[d]);
+        for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt + 16 * kRow>(d), w[1], o[d]);
     }
     // Whether any value of 32 keys, kAt bytes behind the first ones, is not finite.
     template <int kAt> __device__ __forceinline__ bool any_odd() const {
@@ -303,15 +299,15 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     }
     // o += weights x values where some rows do not see some keys.  A hidden value that is not finite must not meet the
     // weight 0: where there is any that is not finite, the products are formed one by one, with the same rounding.
-    template <int kAt> __device__ __forceinline__ void add_values_hidden(const f32x16 &w, uint32_t seen) {
+    template <int kAt> __device__ __forceinline__ void add_values_hidden(const frag (&w)[2], uint32_t seen) {
         if (!__builtin_expect(any_odd<kAt>(), 0)) return add_values<kAt>(w);
 #pragma unroll 1
         for (int i = 0; i < 32; ++i) {                 // keys; the lane holds the weights of those with bit 2 as its half
             const int mine = (i >> 3) * 4 + (i & 3);
             float x = 0.f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x = j == mine ? w[j] : x;
-            const u32x2 both = __builtin_amdgcn_permlane32_swap(__float_as_uint((float)(T)x), __float_as_uint((float)(T)x), false, false);
+            for (int j = 0; j < 16; ++j) x = j == mine ? (float)w[j / 8][j % 8] : x;
+            const u32x2 both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
             const u32x2 sees = __builtin_amdgcn_permlane32_swap(seen >> mine & 1u, seen >> mine & 1u, false, false);
             const float wi = __uint_as_float(i & 4 ? both.y : both.x);
             const bool see = i & 4 ? sees.y : sees.x;
@@ -332,71 +328,96 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         return uniform((uint32_t)x);
     }
 
-    // A work-group's four waves have 32 rows each and share keys and values: 64 a step, two stages, one meeting a step.
-    // The inner loop has the steps of which every row sees all keys and whose reference stays; the others leave it.
+    // A work-group's four waves have 32 rows each and share keys and values: 64 of either a step, two places for either, one
+    // meeting a step.  The scores of the next 32 keys are formed beside the weights of these, so that a wave's matrix
+    // instructions run while it computes exponentials: the keys of a step are 32 ahead of its values.
+    // The inner loop has the steps of which every row sees all keys and whose reference can stay: weights may be large, they
+    // only must not overflow (Type::kMost), which their sum shows.  The others leave it for the end of the step.
     __device__ __forceinline__ void wide() {
-        const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit();
-        const uint32_t mine = lds + 16 * wave * kRow;
-        uint32_t at = it.first + 16 * wave, k0 = it.first, stage = 0;
-        int32_t next = block_of(at);
-        if (k0 >= it.end) return;                      // uniform in the work-group, as are the turns of both loops together
-        auto fetch = [&](uint32_t to) {
-            const int32_t id = next;
-            next = block_of(at + 64);
-            load16<false>(at, id, to);
-            load16<true>(at, id, to + kWideValues);
+        const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit(), mine = 16 * wave;
+        if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
+        uint32_t at = it.first;                        // the step's first value; its first key is 32 further on
+        uint32_t keys_to = lds + mine * kRow, values_to = keys_to + kWideValues, flip = kStage;
+        // keys `first` .. + 32 go to the second half of the other place, as if they were the end of a step in front
+        if (wave >= 2) load16<false>(at + mine - 32, block_of(at + mine - 32), keys_to + kStage);
+        if (at + 32 < it.end) load16<false>(at + 32 + mine, block_of(at + 32 + mine), keys_to);
+        int32_t value_id = block_of(at + mine), key_id = block_of(at + 96 + mine);          // of the values and of the keys that are fetched next
+        load16<true>(at + mine, value_id, values_to);
+        value_id = block_of(at + 64 + mine);
+        wait_loads<0>();
+        meet();
+        k_row += kStage;
+        f32x16 s = scores<32 * kRow>(), t;
+        k_row -= kStage;
+        auto start = [&] {                             // everybody is done with the last step's keys and values
+            wait_loads<0>();
+            meet();
+            if (at + 96 < it.end) load16<false>(at + 96 + mine, key_id, keys_to + flip);
+            if (at + 64 < it.end) load16<true>(at + 64 + mine, value_id, values_to + flip);
+            key_id = block_of(at + 160 + mine);
+            value_id = block_of(at + 128 + mine);
+            fresh();
+        };
+        auto end = [&] {                               // the places change
+            keys_to += flip;
+            values_to += flip;
+            k_row += flip;
+            v_row += flip;
+            here += flip;
+            flip = 0u - flip;
             at += 64;
         };
-        auto turn = [&] {
-            wait_loads<0>();
-            meet();                                    // everybody's rows are there, and everybody is done with the other stage
-            if (k0 + 64 < it.end) fetch(mine + (kStage - stage));
-        };
-        auto other = [&] {
-            const uint32_t by = kStage - 2 * stage;    // there or back
-            k_row += by;
-            v_row += by;
-            here += by;
-            stage += by;
-            k0 += 64;
-        };
-        fetch(mine);
+        frag w[2];
         for (;;) {
-            f32x16 s[2];
-            float top;
-            bool full;
+            uint32_t left = 2;                         // stretches of 32 keys that the step has left
+            bool ahead = false;                        // t has the next stretch's scores
             for (;;) {
-                if (k0 >= it.end) return;
-                turn();
-                fresh();
-                s[0] = scores<0>();
-                s[1] = scores<32 * kRow>();
-                full = k0 + 64 <= least;
-                if (!full) break;
-                top = largest<2>(s);
-                if (__ballot(top > m + kSlack)) break;                      // also the first time: m is -inf
-                weights<2>(s);
-                add_values<kWideValues>(s[0]);
-                add_values<kWideValues + 32 * kRow>(s[1]);
-                other();
+                start();
+                if (at + 64 > least) break;
+                t = scores<0>();
+                float sum = weights(s, w, m);       // infinite, or NaN, the first time: m is -inf
+                if (__ballot(!(sum < Type<T>::kMost))) {
+                    ahead = true;
+                    break;
+                }
+                l += sum;
+                add_values<kWideValues>(w);
+                s = scores<32 * kRow>();
+                sum = weights(t, w, m);
+                if (__ballot(!(sum < Type<T>::kMost))) {
+                    ahead = true;
+                    left = 1;
+                    const f32x16 x = s;
+                    s = t;
+                    t = x;
+                    break;
+                }
+                l += sum;
+                add_values<kWideValues + 32 * kRow>(w);
+                end();
+                if (at >= it.end) return;
             }
-            uint32_t seen[2] = {0xFFFFu, 0xFFFFu};
-            if (!full) {
-                seen[0] = hide(s[0], k0);
-                seen[1] = hide(s[1], k0 + 32);
-                top = largest<2>(s);
+            if (left == 2) {
+                rest<kWideValues>(s, w, at, least);
+                s = ahead ? t : scores<0>();
+                t = scores<32 * kRow>();
             }
-            move(top);
-            weights<2>(s);
-            if (!full && it.causal_from != kAll) {     // uniform
-                add_values_hidden<kWideValues>(s[0], seen[0]);
-                add_values_hidden<kWideValues + 32 * kRow>(s[1], seen[1]);
-            } else {
-                add_values<kWideValues>(s[0]);
-                add_values<kWideValues + 32 * kRow>(s[1]);
-            }
-            other();
+            rest<kWideValues + 32 * kRow>(s, w, at + 32, least);
+            s = t;
+            end();
+            if (at >= it.end) return;
         }
+    }
+    // 32 keys of which some may be hidden, and whose scores may be far above the reference.
+    template <int kAt> __device__ __forceinline__ void rest(f32x16 &s, frag (&w)[2], uint32_t at, uint32_t least) {
+        const bool hidden = at + 32 > least;           // uniform
+        uint32_t seen = 0xFFFFu;
+        if (hidden) seen = hide(s, at);
+        const float top = largest(s);
+        if (__ballot(top > m + kSlack)) move(top);
+        l += weights(s, w, reference());
+        if (hidden && it.causal_from != kAll) add_values_hidden<kAt>(w, seen);
+        else add_values<kAt>(w);
     }
 
     // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon
@@ -408,7 +429,8 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         // whether the last keys and the last values asked for are under way, as 2 * kLoads loads each
         bool keys_fly = load32<false>(from, id0, id1, lds), values_fly = load32<true>(from, id0, id1, lds + kNarrowValues);
         for (uint32_t at = from;;) {
-            f32x16 s[1];
+            f32x16 s;
+            frag w[2];
             float top;
             bool full, more;
             uint32_t next;
@@ -432,30 +454,30 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 id1 = block_of(next + 16);
                 if (keys_fly && values_fly) wait_loads<2 * kLoads>();
                 else wait_loads<0>();
-                s[0] = scores<0>();
+                s = scores<0>();
                 if (more) {
                     wait_lds();
                     keys_fly = load32<false>(next, id0, id1, lds);
                 }
                 full = at + 32 <= least;
                 if (!full) break;
-                top = largest<1>(s);
-                if (__ballot(top > m + kSlack)) break;
-                weights<1>(s);
+                top = largest(s);
+                if (__ballot(top > m + kSlack)) break;                      // also the first time: m is -inf
+                l += weights(s, w, reference());
                 wait_values();
-                add_values<kNarrowValues>(s[0]);
+                add_values<kNarrowValues>(w);
                 next_values();
             }
             uint32_t seen = 0xFFFFu;
             if (!full) {
-                seen = hide(s[0], at);
-                top = largest<1>(s);
+                seen = hide(s, at);
+                top = largest(s);
             }
             move(top);
-            weights<1>(s);
+            l += weights(s, w, reference());
             wait_values();
-            if (!full && it.causal_from != kAll) add_values_hidden<kNarrowValues>(s[0], seen);
-            else add_values<kNarrowValues>(s[0]);
+            if (!full && it.causal_from != kAll) add_values_hidden<kNarrowValues>(w, seen);
+            else add_values<kNarrowValues>(w);
             next_values();
         }
     }
