@@ -664,44 +664,83 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
     }
 }
 
-// Joins the parts of a row: kLanes lanes have four values each of every kWays-th part.
-template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kThreads) join_kernel(const Args a, uint32_t parts) {
-    constexpr int kRows = kThreads / (kLanes * kWays);
-    const uint32_t tid = threadIdx.x, x = tid % kLanes, way = tid / kLanes % kWays, r = tid / (kLanes * kWays);
-    const size_t rows = (size_t)a.n_tokens * a.q_heads, row = (size_t)blockIdx.x * kRows + r;
-    const uint32_t t = (uint32_t)(row / a.q_heads), h = (uint32_t)(row - (size_t)t * a.q_heads);
+// Joins the parts of a row.  A work-group has kRows rows, kLanes lanes with four values each of every kWays-th part.  First
+// every lane computes one part's share of one row (the references and sums of all parts are read side by side), then the
+// values are read, several parts under way at a time.  Bound by the round trips where rows are few, else by reading the parts.
+constexpr int kJoin = 256, kMaxParts = 1024;
+template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kJoin) join_kernel(const Args a, uint32_t parts) {
+    constexpr uint32_t kRows = kJoin / (kLanes * kWays), kPerRow = kJoin / kRows;
+    extern __shared__ __align__(16) char shared[];
+    float *l_share = (float *)shared;                  // [kRows][parts]
+    const uint32_t tid = threadIdx.x, r = tid / kPerRow, i = tid % kPerRow, x = i % kLanes, way = i / kLanes;
+    const size_t rows = (size_t)a.n_tokens * a.q_heads, row = (size_t)blockIdx.x * kRows + r, near = row < rows ? row : rows - 1;
+    const uint32_t t = (uint32_t)(near / a.q_heads), h = (uint32_t)(near - (size_t)t * a.q_heads);
     const bool live = row < rows && (int32_t)t < scalar(a.token_offsets, a.n_requests);
     float ref = -kInf, sum = 0.f;
+    constexpr uint32_t kEach = (kMaxParts + kPerRow - 1) / kPerRow;
+    float2 ml[kEach > 4 ? 4 : kEach];
+    constexpr uint32_t kHeld = kEach > 4 ? 4 : kEach;  // a lane's parts that it holds; what is beyond is read again
+#pragma unroll
+    for (uint32_t j = 0; j < kHeld; ++j) {
+        const uint32_t p = i + j * kPerRow;
+        ml[j] = p < parts ? a.part_ml[p * rows + near] : make_float2(-kInf, 0.f);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kHeld; ++j)
+        if (ml[j].y != 0.f) ref = fmaxf(ref, ml[j].x);
+    for (uint32_t p = i + kHeld * kPerRow; p < parts; p += kPerRow) {
+        const float2 y = a.part_ml[p * rows + near];
+        if (y.y != 0.f) ref = fmaxf(ref, y.x);
+    }
+    // over the row's kPerRow lanes, which are a part of a wave or whole waves
+    __shared__ float l_wave[2][kJoin / 64];
+    constexpr uint32_t kIn = kPerRow < 64 ? kPerRow : 64;
+    for (uint32_t d = 1; d < kIn; d <<= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+    if (kPerRow > 64) {
+        if ((tid & 63u) == 0) l_wave[0][tid >> 6] = ref;
+        __syncthreads();
+        for (uint32_t w = 0; w < kPerRow / 64; ++w) ref = fmaxf(ref, l_wave[0][r * (kPerRow / 64) + w]);
+    }
+    const float at = ref == -kInf ? 0.f : ref;
+#pragma unroll
+    for (uint32_t j = 0; j < kHeld; ++j) {
+        const uint32_t p = i + j * kPerRow;
+        if (p >= parts) break;
+        const float f = ml[j].y == 0.f ? 0.f : exp2_(ml[j].x - at);
+        l_share[r * parts + p] = ml[j].y == 0.f ? -1.f : f;                 // -1: nothing attended, what lies there is no number of this call
+        sum += f * ml[j].y;
+    }
+    for (uint32_t p = i + kHeld * kPerRow; p < parts; p += kPerRow) {
+        const float2 y = a.part_ml[p * rows + near];
+        const float f = y.y == 0.f ? 0.f : exp2_(y.x - at);
+        l_share[r * parts + p] = y.y == 0.f ? -1.f : f;
+        sum += f * y.y;
+    }
+    for (uint32_t d = 1; d < kIn; d <<= 1) sum += __shfl_xor(sum, d);
+    if (kPerRow > 64 && (tid & 63u) == 0) l_wave[1][tid >> 6] = sum;
+    __syncthreads();
+    if (kPerRow > 64) {
+        sum = 0.f;
+        for (uint32_t w = 0; w < kPerRow / 64; ++w) sum += l_wave[1][r * (kPerRow / 64) + w];
+    }
     f32x4 y{};
-    if (live) {
+    if (x * 4 < a.head_dim) {
+        const float *from = a.part_o + near * a.head_dim + x * 4;
+        const size_t step = rows * a.head_dim;
+#pragma unroll 4
         for (uint32_t p = way; p < parts; p += kWays) {
-            const float2 ml = a.part_ml[p * rows + row];
-            if (ml.y == 0.f) continue;
-            f32x4 v{};
-            if (x * 4 < a.head_dim) v = *(const f32x4 *)(a.part_o + (p * rows + row) * a.head_dim + x * 4);
-            const float next = fmaxf(ref, ml.x), at = next == -kInf ? 0.f : next, f = exp2_(ref - at), g = exp2_(ml.x - at);
-            y = y * f + v * g;
-            sum = sum * f + ml.y * g;
-            ref = next;
+            const f32x4 v = *(const f32x4 *)(from + p * step);
+            const float f = l_share[r * parts + p];
+            if (f != -1.f) y += f * v;
         }
     }
     if constexpr (kWays > 1) {
-        __shared__ f32x4 l_y[kThreads];
-        __shared__ float2 l_ml[kThreads];
+        __shared__ f32x4 l_y[kJoin];
         l_y[tid] = y;
-        l_ml[tid] = make_float2(ref, sum);
         __syncthreads();
         if (way) return;
 #pragma unroll
-        for (int w = 1; w < kWays; ++w) {
-            const float2 ml = l_ml[tid + w * kLanes];
-            if (ml.y == 0.f) continue;
-            const f32x4 v = l_y[tid + w * kLanes];
-            const float next = fmaxf(ref, ml.x), at = next == -kInf ? 0.f : next, f = exp2_(ref - at), g = exp2_(ml.x - at);
-            y = y * f + v * g;
-            sum = sum * f + ml.y * g;
-            ref = next;
-        }
+        for (int w = 1; w < kWays; ++w) y += l_y[tid + w * kLanes];
     }
     if (!live) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -712,7 +751,7 @@ template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(k
         for (int j = 0; j < 4; ++j) z[j] = (T)(y[j] * inv);
         *(t4 *)(a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head + x * 8) = z;
     }
-    if (a.lse && x == 0) a.lse[row] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+    if (a.lse && i == 0) a.lse[row] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
 __global__ void clear_kernel(uint32_t *p) { *p = 0u; }
@@ -721,16 +760,23 @@ __global__ void clear_kernel(uint32_t *p) { *p = 0u; }
 
 uint32_t div_up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-// How many chunks a stretch of `keys` keys is cut into, where one chunk gives `tiles` work-groups and `others` run beside them: the
-// fewest rounds of work-groups, weighed with what each chunk costs by itself (its start and end; its part, written and read again).
-uint32_t choose_chunks(uint64_t tiles, uint32_t keys, uint32_t step, uint32_t slots, uint64_t most) {
+// How many chunks a stretch of `keys` keys is cut into, where one chunk gives `tiles` work-groups: the least of an estimate in
+// microseconds.  A step of a wide work-group (64 keys) takes 1.33 us alone on its CU and 1.9 beside another at 128 values
+// a head; one of a narrow one (128 keys) 2.2, or what reading takes at 5.4 TB/s for all work-groups together; 4 us go to a
+// round's start and end; each part of `rows` rows is written and read at 4 TB/s.  (Measured: 4,096 rows, 8,192 keys, 32 tiles:
+// 4 / 8 / 12 / 16 chunks 55 / 39 / 43 / 49 us; 16,384 rows, 32,768 keys, 128 tiles: 2 / 3 / 4 / 5 / 6 chunks 373 / 342 / 311 / 347 / 323;
+// 128 rows, 200,003 keys, 8 tiles: 16 / 32 / 64 / 128 chunks 197 / 159 / 168 / 186.)
+uint32_t choose_chunks(uint64_t tiles, uint32_t keys, bool wide, uint64_t rows, uint32_t head_dim, uint32_t cus, uint64_t most) {
+    const uint32_t step = wide ? kWideKeys : kNarrowKeys * kWaves, limit = div_up(keys, step), slots = cus * (head_dim <= 128 ? 2 : 1);
+    const double size = head_dim / 128.0, part = rows * (head_dim * 8.0 + 16.0) / 4e6;
     uint32_t best = 1;
     double least = 0;
-    const uint32_t limit = div_up(keys, step);
-    for (uint32_t s = 1; s <= limit && s <= most && s <= 1024; ++s) {
-        const uint32_t chunk = div_up(div_up(keys, s), step) * step;
-        if (s > 1 && div_up(keys, chunk) != s) continue;
-        const double rounds = (double)((tiles * s + slots - 1) / slots), cost = rounds * (chunk + 192.0) + 24.0 * s;
+    for (uint32_t s = 1; s <= limit && s <= most && s < kMaxParts / 2; ++s) {
+        const uint32_t chunk = div_up(limit, s);       // in steps
+        if (s > 1 && div_up(limit, chunk) != s) continue;
+        const double n = (double)(tiles * s), beside = n < slots ? n : slots, all = n <= slots ? 1.0 : (n / slots + std::ceil(n / slots)) / 2;
+        const double one = wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(2.2, beside * 0.0121 * size);
+        const double cost = all * (chunk * one + 4.0) + s * part;
         if (s == 1 || cost < least) {
             best = s;
             least = cost;
@@ -767,9 +813,13 @@ template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, 
     if (a.direct) return hipSuccess;
     constexpr int kLanes = DT == 1 ? 8 : DT == 2 ? 16 : DT <= 4 ? 32 : 64;
     const size_t rows = (size_t)a.n_tokens * a.q_heads;
-    // few rows of many parts: the parts are read side by side
-    if (parts >= 8) hipLaunchKernelGGL((join_kernel<T, kLanes, 4>), dim3(div_up(rows, kThreads / (kLanes * 4))), dim3(kThreads), 0, st, a, parts);
-    else hipLaunchKernelGGL((join_kernel<T, kLanes, 1>), dim3(div_up(rows, kThreads / kLanes)), dim3(kThreads), 0, st, a, parts);
+    auto join = [&](auto ways) {
+        constexpr int kWays = decltype(ways)::value, kRows = kJoin / (kLanes * kWays);
+        hipLaunchKernelGGL((join_kernel<T, kLanes, kWays>), dim3(div_up(rows, kRows)), dim3(kJoin), kRows * parts * sizeof(float), st, a, parts);
+    };
+    // few rows: more lanes to a row, which read its parts side by side
+    if (rows * kLanes < 16384 && parts >= 4) join(std::integral_constant<int, kJoin / kLanes>());
+    else join(std::integral_constant<int, 1>());
     return hipGetLastError();
 }
 
@@ -916,7 +966,6 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     a.c = r.scale * 1.4426950408889634f;
 
     const uint64_t rows = (uint64_t)r.n_tokens * r.q_heads, part_limit = s->part_rows / rows;
-    const uint32_t slots = s->cus * (r.head_dim <= 128 ? 2 : 1);
     // own tokens: one part at least, so that every row has one
     const uint64_t own_rows = (uint64_t)a.max_new * a.ratio;
     uint32_t own_keys = r.max_len ? r.max_len : 1;
@@ -924,13 +973,13 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     if (own_rows > kNarrowRows) {
         a.own_mode = kOwnWide;
         a.own_tiles = div_up(own_rows, kWideRows);
-        a.own_chunks = choose_chunks(requests_heads * a.own_tiles, own_keys, kWideKeys, slots, part_limit / 2);
+        a.own_chunks = choose_chunks(requests_heads * a.own_tiles, own_keys, true, rows, r.head_dim, s->cus, part_limit / 2);
         a.own_chunk = div_up(div_up(own_keys, a.own_chunks), kWideKeys) * kWideKeys;
     } else {
         a.own_mode = own_keys <= 2 * kNarrowKeys * kWaves ? kOwnSolo : kOwnSplit;
         a.own_tiles = 1;
         const uint32_t step = a.own_mode == kOwnSolo ? kNarrowKeys : kNarrowKeys * kWaves;
-        a.own_chunks = a.own_mode == kOwnSolo ? 1 : choose_chunks(requests_heads, own_keys, step, slots, part_limit / 2);
+        a.own_chunks = a.own_mode == kOwnSolo ? 1 : choose_chunks(requests_heads, own_keys, false, rows, r.head_dim, s->cus, part_limit / 2);
         a.own_chunk = div_up(div_up(own_keys, a.own_chunks), step) * step;
     }
     if (a.own_tiles == 0) a.own_tiles = 1;
@@ -941,7 +990,7 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
         a.history_wide = group_rows > kNarrowRows;
         a.history_tiles = div_up(group_rows, a.history_wide ? kWideRows : kNarrowRows);
         const uint32_t step = a.history_wide ? kWideKeys : kNarrowKeys * kWaves;
-        a.history_chunks = choose_chunks((uint64_t)a.history_tiles * r.n_groups * r.kv_heads, r.max_prefix, step, slots, part_limit - a.own_chunks);
+        a.history_chunks = choose_chunks((uint64_t)a.history_tiles * r.n_groups * r.kv_heads, r.max_prefix, a.history_wide, rows, r.head_dim, s->cus, part_limit - a.own_chunks);
         a.history_chunk = div_up(div_up(r.max_prefix, a.history_chunks), step) * step;
         const uint64_t combos = (uint64_t)r.n_groups * r.kv_heads * a.history_chunks;
         SEQ_REQUIRE(combos < (1u << 30), "too many groups, heads and chunks for one launch");
