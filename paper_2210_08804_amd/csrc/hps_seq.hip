@@ -18,23 +18,31 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 // ---- extend and release -------------------------------------------------------------------
 //
 // Everything follows from two exclusive sums over the requests: of their new tokens, and of their new blocks.  A
-// work-group takes a chunk of 4,096 requests, adds up what all requests in front of it have (nobody waits for anybody:
-// the lengths are few and in the caches, and reading them again costs less than a second launch or a chain of
+// work-group takes a chunk of requests, four to a thread, adds up what all requests in front of it have (nobody waits for
+// anybody: the lengths are few and in the caches, and reading them again costs less than a second launch or a chain of
 // work-groups), scans its own into LDS, and writes its share of the chunk's tokens and blocks, each found by a binary
-// search in LDS.
-constexpr uint32_t kThreads = 1024, kChunk = 4096, kPer = kChunk / kThreads, kWaves = kThreads / 64;
+// search in LDS; some of its waves see to the blocks while the others see to the tokens.  Bound by the chain of round trips
+// (arguments, lengths, table or free list).
+constexpr uint32_t kPer = 4;                           // requests of a thread
 constexpr uint32_t kMaxSum = 0x7FFFFFFFu;
 
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
-
-struct Sums {                                          // saturating sums are associative, so they scan like any other
-    uint32_t tokens, blocks, over;
-    __device__ __forceinline__ void add(const Sums &o) {
-        tokens = add_sat(tokens, o.tokens);
-        blocks = add_sat(blocks, o.blocks);
-        over = add_sat(over, o.over);
-    }
-};
+template <int kCtrl, int kRows = 0xf> __device__ __forceinline__ uint32_t moved(uint32_t x) {     // 0 where nothing comes from
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xf, false);
+}
+// Inclusive sums over 16 lanes, over a wave; saturating sums are associative, so they scan like any other.
+__device__ __forceinline__ uint32_t scan16(uint32_t x) {
+    x = add_sat(x, moved<0x111>(x));                   // one lane on, two, four, eight
+    x = add_sat(x, moved<0x112>(x));
+    x = add_sat(x, moved<0x114>(x));
+    return add_sat(x, moved<0x118>(x));
+}
+__device__ __forceinline__ uint32_t scan64(uint32_t x) {
+    x = scan16(x);
+    x = add_sat(x, moved<0x142, 0xa>(x));              // the last lane of 16 to the next 16, of 32 to the next 32
+    return add_sat(x, moved<0x143, 0xc>(x));
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
 // One request: its kept tokens, and what it adds.
 struct Request {
@@ -47,35 +55,10 @@ struct Request {
         kept = (past + round) >> sh;
         blocks = ((past + fit + round) >> sh) - kept;
     }
-    __device__ __forceinline__ Sums sums() const { return {fresh, blocks, fresh - fit}; }
 };
 
-// Exclusive scan over the work-group; `total` receives the sum of all.
-__device__ __forceinline__ Sums scan(Sums mine, Sums *l_wave, Sums &total) {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    Sums inc = mine;
-    for (uint32_t d = 1; d < 64; d <<= 1) {
-        Sums o{(uint32_t)__shfl_up((int)inc.tokens, d), (uint32_t)__shfl_up((int)inc.blocks, d), (uint32_t)__shfl_up((int)inc.over, d)};
-        if (lane >= d) inc.add(o);
-    }
-    if (lane == 63) l_wave[wave] = inc;
-    Sums exc{(uint32_t)__shfl_up((int)inc.tokens, 1), (uint32_t)__shfl_up((int)inc.blocks, 1), (uint32_t)__shfl_up((int)inc.over, 1)};
-    if (lane == 0) exc = {0, 0, 0};
-    __syncthreads();
-    Sums before{0, 0, 0};
-    total = {0, 0, 0};
-    for (uint32_t w = 0; w < blockDim.x / 64; ++w) {
-        if (w == wave) before = total;
-        total.add(l_wave[w]);
-    }
-    before.add(exc);
-    __syncthreads();
-    return before;
-}
-
-// The last i < n with first[i] <= x, where first[0] <= x < first[n].
-__device__ __forceinline__ uint32_t find(const uint32_t *first, uint32_t n, uint32_t x) {
-    uint32_t lo = 0, hi = n;
+// The last i in lo .. hi - 1 with first[i] <= x, where first[lo] <= x < first[hi].
+__device__ __forceinline__ uint32_t find(const uint32_t *first, uint32_t lo, uint32_t hi, uint32_t x) {
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) >> 1;
         if (first[mid] <= x) lo = mid; else hi = mid;
@@ -83,114 +66,172 @@ __device__ __forceinline__ uint32_t find(const uint32_t *first, uint32_t n, uint
     return lo;
 }
 
+// The same for a whole wave's x and n <= 4096 of them, in two looks.
+__device__ __forceinline__ uint32_t find_together(const uint32_t *first, uint32_t n, uint32_t x) {
+    const uint32_t lane = threadIdx.x & 63u, step = (n + 63) / 64;
+    const uint32_t lo = ((uint32_t)__popcll(__ballot(lane * step < n && first[lane * step] <= x)) - 1u) * step, i = lo + lane;
+    return lo + (uint32_t)__popcll(__ballot(lane < step && i < n && first[i] <= x)) - 1u;
+}
+
 struct ExtendArgs {
     hps_seq_extend_args_t a;
     uint32_t sh, cap;                                  // log2 of the block size; tokens that a table holds
 };
 
-__device__ __forceinline__ int32_t new_block(const ExtendArgs &e, uint32_t n_free, uint32_t k) {
-    const int32_t id = k < n_free ? e.a.free_blocks[n_free - 1u - k] : -1;
-    return (uint32_t)id < e.a.n_blocks ? id : -1;
+// The place in the free list of the call's k-th new block; null where the list has none.
+__device__ __forceinline__ const int32_t *new_block(const ExtendArgs &e, uint32_t n_free, uint32_t k) {
+    return k < n_free ? e.a.free_blocks + (n_free - 1u - k) : nullptr;
 }
 
-__global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs e) {
-    __shared__ uint32_t l_tok[kChunk + 1], l_blk[kChunk + 1];
-    __shared__ Sums l_wave[kWaves];
+template <uint32_t kThreads> __global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs e) {
+    constexpr uint32_t kChunk = kPer * kThreads, kWaves = kThreads / 64, kBlockWaves = kWaves / 4;
+    __shared__ uint32_t l_tok[kChunk + 1], l_blk[kChunk + 1], l_past[kChunk];
+    __shared__ uint32_t l_wave[4][16];                 // tokens and blocks of the chunk's waves; of what is in front of the chunk
+    __shared__ unsigned long long l_over;
     const hps_seq_extend_args_t &a = e.a;
-    const uint32_t tid = threadIdx.x, r0 = blockIdx.y * kChunk, mine = min(kChunk, a.n_requests - r0);
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, r0 = blockIdx.y * kChunk, mine = min(kChunk, a.n_requests - r0);
     const bool last_chunk = blockIdx.y == gridDim.y - 1;
-    const uint32_t n_free = (uint32_t)min(max(*a.n_free, 0), (int32_t)a.n_blocks);
+    const int32_t free_now = *a.n_free;
+    if (tid == 0) l_over = 0;
 
-    Sums front{0, 0, 0};
-    for (uint32_t r = tid; r < r0; r += kThreads) front.add(Request(a.past_lens[r], a.new_lens[r], e.cap, e.sh).sums());
-    Sums part[kPer], sum{0, 0, 0};
-    uint32_t past_fit[kPer];
+    uint32_t tok[kPer], blk[kPer], end[kPer], tokens = 0, blocks = 0, over = 0;
+    int32_t p[kPer], n[kPer];
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i) {
-        const uint32_t r = r0 + tid * kPer + i;
         const bool there = tid * kPer + i < mine;
-        const Request q(there ? a.past_lens[r] : 0, there ? a.new_lens[r] : 0, e.cap, e.sh);
-        part[i] = q.sums();
-        past_fit[i] = q.past + q.fit;
-        sum.add(part[i]);
+        p[i] = there ? a.past_lens[r0 + tid * kPer + i] : 0;
+        n[i] = there ? a.new_lens[r0 + tid * kPer + i] : 0;
     }
-    Sums total, at = scan(sum, l_wave, total);
+    uint32_t front_tokens = 0, front_blocks = 0;
+    for (uint32_t r = tid; r < r0; r += kThreads) {
+        const Request q(a.past_lens[r], a.new_lens[r], e.cap, e.sh);
+        front_tokens = add_sat(front_tokens, q.fresh);
+        front_blocks = add_sat(front_blocks, q.blocks);
+        over = add_sat(over, q.fresh - q.fit);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) {
+        const Request q(p[i], n[i], e.cap, e.sh);
+        tok[i] = tokens;
+        blk[i] = blocks;
+        end[i] = q.past + q.fit;
+        tokens = add_sat(tokens, q.fresh);
+        blocks = add_sat(blocks, q.blocks);
+        over = add_sat(over, q.fresh - q.fit);
+        if (tid * kPer + i < mine) l_past[tid * kPer + i] = q.past;
+    }
+    const uint32_t inc_tokens = scan64(tokens), inc_blocks = scan64(blocks);
+    if (lane == 63) {
+        l_wave[0][wave] = inc_tokens;
+        l_wave[1][wave] = inc_blocks;
+    }
     if (r0) {                                          // uniform
-        Sums all;
-        (void)scan(front, l_wave, all);
-        at.add(all);
-        total.add(all);
+        front_tokens = scan64(front_tokens);
+        front_blocks = scan64(front_blocks);
+        if (lane == 63) {
+            l_wave[2][wave] = front_tokens;
+            l_wave[3][wave] = front_blocks;
+        }
     }
+    __syncthreads();
+    if (over) atomicAdd(&l_over, (unsigned long long)over);                 // seldom: a table too short
+    uint32_t sums[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[i] = scan16(lane < kWaves && (i < 2 || r0) ? l_wave[i][lane] : 0);
+    const uint32_t base_tokens = lane_of(sums[2], kWaves - 1), base_blocks = lane_of(sums[3], kWaves - 1);
+    const uint32_t all_tokens = add_sat(base_tokens, lane_of(sums[0], kWaves - 1)), all_blocks = add_sat(base_blocks, lane_of(sums[1], kWaves - 1));
+    uint32_t at_tokens = base_tokens, at_blocks = base_blocks;
+    const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)wave);
+    if (w) {
+        at_tokens = add_sat(at_tokens, lane_of(sums[0], (int)w - 1));
+        at_blocks = add_sat(at_blocks, lane_of(sums[1], (int)w - 1));
+    }
+    at_tokens = add_sat(at_tokens, moved<0x138>(inc_tokens));               // the lane below's
+    at_blocks = add_sat(at_blocks, moved<0x138>(inc_blocks));
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i) {
         const uint32_t j = tid * kPer + i;
         if (j < mine) {
-            l_tok[j] = at.tokens;
-            l_blk[j] = at.blocks;
+            l_tok[j] = add_sat(at_tokens, tok[i]);
+            l_blk[j] = add_sat(at_blocks, blk[i]);
             if (blockIdx.x == 0) {
-                a.token_offsets[r0 + j] = (int32_t)min(at.tokens, kMaxSum);
-                a.total_lens[r0 + j] = (int32_t)past_fit[i];
+                a.token_offsets[r0 + j] = (int32_t)min(add_sat(at_tokens, tok[i]), kMaxSum);
+                a.total_lens[r0 + j] = (int32_t)end[i];
             }
         }
-        at.add(part[i]);
     }
     if (tid == 0) {
-        l_tok[mine] = total.tokens;
-        l_blk[mine] = total.blocks;
-        if (last_chunk && blockIdx.x == 0) {
-            const uint32_t taken = min(total.blocks, n_free);
-            a.token_offsets[a.n_requests] = (int32_t)min(total.tokens, kMaxSum);
-            a.info[0] = (int32_t)(n_free - taken);
-            a.info[1] = (int32_t)min(total.tokens, kMaxSum);
-            a.info[2] = (int32_t)min(total.blocks - taken, kMaxSum);
-            a.info[3] = (int32_t)min(total.over, kMaxSum);
-        }
+        l_tok[mine] = all_tokens;
+        l_blk[mine] = all_blocks;
     }
+    const uint32_t n_free = (uint32_t)min(max(free_now, 0), (int32_t)a.n_blocks);
     __syncthreads();
-
-    const uint32_t stride = gridDim.x * kThreads, first = blockIdx.x * kThreads + tid;
-    for (uint64_t k = l_blk[0] + (uint64_t)first; k < l_blk[mine]; k += stride) {
-        const uint32_t i = find(l_blk, mine, (uint32_t)k), r = r0 + i;
-        const Request q(a.past_lens[r], a.new_lens[r], e.cap, e.sh);
-        a.block_table[(size_t)r * a.table_width + q.kept + ((uint32_t)k - l_blk[i])] = new_block(e, n_free, (uint32_t)k);
+    if (tid == 0 && last_chunk && blockIdx.x == 0) {
+        const uint32_t taken = min(all_blocks, n_free);
+        a.token_offsets[a.n_requests] = (int32_t)min(all_tokens, kMaxSum);
+        a.info[0] = (int32_t)(n_free - taken);
+        a.info[1] = (int32_t)min(all_tokens, kMaxSum);
+        a.info[2] = (int32_t)min(all_blocks - taken, kMaxSum);
+        a.info[3] = (int32_t)min(l_over, (unsigned long long)kMaxSum);
     }
-    // Tokens in fours, 16 bytes a store; the first and the last four of a chunk may belong to its neighbours in part.
+
+    const uint32_t round = (1u << e.sh) - 1u;
+    if (wave >= kWaves - kBlockWaves) {
+        constexpr uint32_t kFill = 64 * kBlockWaves;
+        for (uint64_t k = l_blk[0] + (uint64_t)(blockIdx.x * kFill + tid - (kThreads - kFill)); k < l_blk[mine]; k += gridDim.x * kFill) {
+            const uint32_t i = find(l_blk, 0, mine, (uint32_t)k), kept = (l_past[i] + round) >> e.sh;
+            const int32_t *from = new_block(e, n_free, (uint32_t)k);
+            const int32_t id = from ? *from : -1;
+            a.block_table[(size_t)(r0 + i) * a.table_width + kept + ((uint32_t)k - l_blk[i])] = (uint32_t)id < a.n_blocks ? id : -1;
+        }
+        return;
+    }
+    // Tokens in fours, 16 bytes a store; the first and the last four of a chunk may belong to its neighbours in part.  A wave's
+    // 256 tokens are of a few requests, which it finds together.
+    constexpr uint32_t kFill = 64 * (kWaves - kBlockWaves);
     const uint32_t t_begin = min(l_tok[0], a.max_tokens), t_end = min(l_tok[mine], a.max_tokens), t_all = last_chunk ? a.max_tokens : t_end;
     const bool wide = (((uintptr_t)a.slots | (uintptr_t)a.positions) & 15u) == 0;
-    for (uint64_t g = (t_begin >> 2) + (uint64_t)first; g * 4 < t_all; g += stride) {
-        i32x4 slot, pos;
-        uint32_t i = 0, off = 0, next = 0, last_j = 0xFFFFFFFFu;
-        int32_t id = -1, start = 0;
-        uint32_t past = 0, kept = 0;
+    for (uint64_t g0 = (t_begin >> 2) + (uint64_t)(blockIdx.x * kFill + 64 * w); g0 * 4 < t_all; g0 += gridDim.x * kFill) {        // uniform in a wave
+        const uint32_t g = (uint32_t)g0 + lane, t0 = max((uint32_t)g0 * 4, t_begin), t1 = min((uint32_t)g0 * 4 + 256, t_end);       // max_tokens < 2^31
+        uint32_t lo = 0, hi = 0;
+        if (t0 < t1) {
+            lo = find_together(l_tok, mine, t0);
+            hi = find_together(l_tok, mine, t1 - 1) + 1;
+        }
+        uint32_t own[4];
+        int32_t start[4], id[4];
+        uint32_t i = lo, next = 0;
 #pragma unroll
-        for (uint32_t c = 0; c < 4; ++c) {
-            const uint32_t t = (uint32_t)g * 4 + c;
-            slot[c] = pos[c] = -1;
+        for (uint32_t c = 0; c < 4; ++c) {             // all loads first
+            const uint32_t t = g * 4 + c;
+            own[c] = 0xFFFFFFFFu;
+            start[c] = 0;
+            id[c] = -1;
             if (t < t_begin || t >= t_end) continue;
             if (t >= next) {
-                i = find(l_tok, mine, t);
-                off = l_tok[i];
+                i = find(l_tok, i, hi, t);
                 next = l_tok[i + 1];
-                past = min((uint32_t)max(a.past_lens[r0 + i], 0), e.cap);
-                kept = (past + (1u << e.sh) - 1u) >> e.sh;
-                start = a.start ? a.start[r0 + i] : 0;
-                last_j = 0xFFFFFFFFu;
             }
-            const uint32_t own = past + (t - off), j = own >> e.sh;
-            pos[c] = (int32_t)min((int64_t)start + own, (int64_t)kMaxSum);
-            if (own >= e.cap) continue;
-            if (j != last_j) {
-                id = j < kept ? a.block_table[(size_t)(r0 + i) * a.table_width + j] : new_block(e, n_free, l_blk[i] + (j - kept));
-                last_j = j;
-            }
-            if ((uint32_t)id < a.n_blocks) slot[c] = (int32_t)(((uint32_t)id << e.sh) | (own & ((1u << e.sh) - 1u)));
+            const uint32_t past = l_past[i], kept = (past + round) >> e.sh, j = (past + (t - l_tok[i])) >> e.sh;
+            own[c] = past + (t - l_tok[i]);
+            if (a.start) start[c] = a.start[r0 + i];
+            const int32_t *from = own[c] >= e.cap ? nullptr : j < kept ? a.block_table + (size_t)(r0 + i) * a.table_width + j : new_block(e, n_free, l_blk[i] + (j - kept));
+            if (from) id[c] = *from;
+        }
+        i32x4 slot, pos;
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+            const uint32_t t = g * 4 + c;
+            const bool inside = t >= t_begin && t < t_end;
+            pos[c] = inside ? (int32_t)min((int64_t)start[c] + own[c], (int64_t)kMaxSum) : -1;
+            slot[c] = inside && (uint32_t)id[c] < a.n_blocks ? (int32_t)(((uint32_t)id[c] << e.sh) | (own[c] & round)) : -1;
         }
         if (wide && g * 4 >= t_begin && g * 4 + 4 <= t_all) {
             *(i32x4 *)(a.slots + g * 4) = slot;
             *(i32x4 *)(a.positions + g * 4) = pos;
         } else {
             for (uint32_t c = 0; c < 4; ++c) {
-                const uint32_t t = (uint32_t)g * 4 + c;
+                const uint32_t t = g * 4 + c;
                 if (t < t_begin || t >= t_all) continue;
                 a.slots[t] = slot[c];
                 a.positions[t] = pos[c];
@@ -209,16 +250,24 @@ struct ReleaseArgs {
 };
 
 // One work-group: requests end seldom, and the free list is one stack whose order the call fixes.
-__global__ void __launch_bounds__(kThreads) release_kernel(const ReleaseArgs a) {
-    __shared__ uint32_t l_blk[kChunk + 1];
-    __shared__ Sums l_wave[kWaves];
-    __shared__ uint32_t l_cnt[kWaves];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+constexpr uint32_t kReleaseThreads = 1024, kReleaseChunk = kPer * kReleaseThreads, kReleaseWaves = kReleaseThreads / 64;
+__global__ void __launch_bounds__(kReleaseThreads) release_kernel(const ReleaseArgs a) {
+    __shared__ uint32_t l_blk[kReleaseChunk + 1], l_wave[kReleaseWaves];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
     const uint32_t had = (uint32_t)min(max(*a.n_free, 0), (int32_t)a.n_blocks);
     uint32_t base = had, lost = 0;                     // the same in all threads
-    for (uint32_t r0 = 0; r0 < a.n_requests; r0 += kChunk) {
-        const uint32_t mine = min(kChunk, a.n_requests - r0);
-        uint32_t n[kPer], sum = 0;
+    // sum over the waves in front of this one, and over all, of what the waves' last lanes have
+    auto over_waves = [&](uint32_t mine, uint32_t &all) {
+        if (lane == 63) l_wave[wave] = mine;
+        __syncthreads();
+        const uint32_t sums = scan16(lane < kReleaseWaves ? l_wave[lane] : 0);
+        __syncthreads();
+        all = lane_of(sums, kReleaseWaves - 1);
+        return wave ? lane_of(sums, (int)wave - 1) : 0u;
+    };
+    for (uint32_t r0 = 0; r0 < a.n_requests; r0 += kReleaseChunk) {
+        const uint32_t mine = min(kReleaseChunk, a.n_requests - r0);
+        uint32_t n[kPer], sum = 0, total;
         for (uint32_t i = 0; i < kPer; ++i) {
             const uint32_t j = tid * kPer + i, r = r0 + j;
             n[i] = 0;
@@ -228,37 +277,31 @@ __global__ void __launch_bounds__(kThreads) release_kernel(const ReleaseArgs a) 
             }
             sum = add_sat(sum, n[i]);
         }
-        Sums total, at = scan({0, sum, 0}, l_wave, total);
+        const uint32_t inc = scan64(sum);
+        uint32_t at = add_sat(over_waves(inc, total), moved<0x138>(inc));
         for (uint32_t i = 0; i < kPer; ++i) {
-            if (tid * kPer + i < mine) l_blk[tid * kPer + i] = at.blocks;
-            at.blocks = add_sat(at.blocks, n[i]);
+            if (tid * kPer + i < mine) l_blk[tid * kPer + i] = at;
+            at = add_sat(at, n[i]);
         }
-        if (tid == 0) l_blk[mine] = total.blocks;
+        if (tid == 0) l_blk[mine] = total;
         __syncthreads();
-        for (uint64_t k0 = 0; k0 < total.blocks; k0 += kThreads) {
+        for (uint64_t k0 = 0; k0 < total; k0 += kReleaseThreads) {
             const uint32_t k = (uint32_t)k0 + tid;
             int32_t id = -1;
-            if (k0 + tid < total.blocks) {
-                const uint32_t i = find(l_blk, mine, k);
+            if (k0 + tid < total) {
+                const uint32_t i = find(l_blk, 0, mine, k);
                 int32_t *entry = a.table + (size_t)(r0 + i) * a.width + (k - l_blk[i]);
                 id = *entry;
                 *entry = -1;
             }
             const bool valid = (uint32_t)id < a.n_blocks;
             const uint64_t m = __ballot(valid);
-            if (lane == 0) l_cnt[wave] = (uint32_t)__popcll(m);
-            __syncthreads();
-            uint32_t at_wave = base, all = 0;
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                if (w < wave) at_wave += l_cnt[w];
-                all += l_cnt[w];
-            }
-            const uint32_t at_lane = at_wave + (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
-            if (valid && at_lane < a.n_blocks) a.free_blocks[at_lane] = id;
+            uint32_t all;
+            const uint32_t to = base + over_waves((uint32_t)__popcll(m), all) + (uint32_t)__popcll(m & ((1ull << lane) - 1ull));
+            if (valid && to < a.n_blocks) a.free_blocks[to] = id;
             const uint32_t room = a.n_blocks - base;
             lost = add_sat(lost, all - min(all, room));
             base += min(all, room);
-            __syncthreads();
         }
         __syncthreads();
     }
@@ -497,12 +540,17 @@ hps_status_t hps_seq_extend(const hps_seq_extend_args_t *args, void *stream) {
     SEQ_REQUIRE(a.n_free != a.info, "info must not be the array that n_free is read from");
     SEQ_REQUIRE(a.n_requests == 0 || (a.total_lens != a.past_lens && a.total_lens != a.new_lens), "total_lens must be an array of its own");
     ExtendArgs e{a, (uint32_t)__builtin_ctz(a.block_size), a.table_width * a.block_size};
-    const uint32_t chunks = a.n_requests ? (a.n_requests + kChunk - 1) / kChunk : 1;
-    // a work-group per 4,096 tokens, one store of each lane, and two work-groups per CU at most
-    uint32_t parts = (a.max_tokens + 4095u) / 4096u, most = 512u / chunks;
-    if (parts > most) parts = most;
-    if (parts < 1) parts = 1;
-    hipLaunchKernelGGL(extend_kernel, dim3(parts, chunks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), e);
+    auto launch = [&](auto threads) {
+        constexpr uint32_t kThreads = decltype(threads)::value, kChunk = kPer * kThreads;
+        const uint32_t chunks = a.n_requests ? (a.n_requests + kChunk - 1) / kChunk : 1;
+        // a store of each lane that sees to tokens, and one work-group per CU at most
+        uint32_t parts = (a.max_tokens + 3 * kThreads - 1) / (3 * kThreads), most = 256u / chunks;
+        if (parts > most) parts = most;
+        if (parts < 1) parts = 1;
+        hipLaunchKernelGGL((extend_kernel<kThreads>), dim3(parts, chunks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), e);
+    };
+    if (a.n_requests <= kPer * 256) launch(std::integral_constant<uint32_t, 256>());
+    else launch(std::integral_constant<uint32_t, 1024>());
     SEQ_TRY(hipGetLastError());
     return HPS_OK;
 }
@@ -519,7 +567,7 @@ hps_status_t hps_seq_release(int32_t *lens, const int32_t *finished, uint32_t n_
     SEQ_REQUIRE(n_requests == 0 || table_width == 0 || seq_words(block_table), "block_table must be a 4-byte aligned device pointer");
     const ReleaseArgs a{lens, finished, block_table, free_blocks, n_free, info, n_requests, (uint32_t)__builtin_ctz(block_size), table_width * block_size,
                         table_width, n_blocks};
-    hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kReleaseThreads), 0, static_cast<hipStream_t>(stream), a);
     SEQ_TRY(hipGetLastError());
     return HPS_OK;
 }
