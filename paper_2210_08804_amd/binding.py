@@ -516,19 +516,19 @@ def hps_seq_last_error() -> str:
     return load_library().hps_seq_last_error().decode()
 
 
-def _ints(t, name, shape=None):
-    """Address of a contiguous int32 array; 0 for None."""
+def _ints(t, name, n=None):
+    """Address of a contiguous int32 array, of n numbers where n is given; 0 for None."""
     if t is None:
         return 0
+    if t.is_cuda and t.dtype is _int32 and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
     if not t.is_cuda:
         raise TypeError(f"{name}: device tensor expected")
     if t.dtype is not _int32:
         raise TypeError(f"{name}: expected {_int32}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: contiguous tensor expected")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: expected {n} numbers, got {t.numel()}")
 
 
 def _word(t, name):
@@ -538,18 +538,18 @@ def _word(t, name):
     return _ints(t, name)
 
 
-def _heads(t, name, dtype, tokens, heads, dim):
+def _heads(t, name, dtype, shape):
     """(address, token stride, head stride) of a tensor [tokens, heads, dim] whose heads are each in one piece."""
+    if t.is_cuda and t.dtype is dtype and t.shape == shape:
+        st, sh, sd = t.stride()
+        if sd == 1 or shape[2] == 1:
+            return t.data_ptr(), st, sh
+        raise ValueError(f"{name}: the values of a head must be adjacent")
     if not t.is_cuda:
         raise TypeError(f"{name}: device tensor expected")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.shape != (tokens, heads, dim):
-        raise ValueError(f"{name}: expected shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
-    st, sh, sd = t.stride()
-    if sd != 1 and dim > 1:
-        raise ValueError(f"{name}: the values of a head must be adjacent")
-    return t.data_ptr(), st, sh
+    raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _pages(k, v, dtype):
@@ -558,14 +558,14 @@ def _pages(k, v, dtype):
         raise TypeError("k_pages, v_pages: device tensors expected")
     if k.dtype is not dtype or v.dtype is not dtype:
         raise TypeError(f"k_pages, v_pages: expected {dtype}, got {k.dtype} and {v.dtype}")
-    if k.dim() != 4 or k.shape != v.shape:
+    shape, stride = k.shape, k.stride()
+    if len(shape) != 4 or shape != v.shape:
         raise ValueError("k_pages, v_pages: expected two tensors [blocks, block size, heads, dim]")
-    stride = k.stride()
     if stride != v.stride():
         raise ValueError("k_pages and v_pages must have the same strides")
-    if stride[3] != 1 and k.shape[3] > 1:
+    if stride[3] != 1 and shape[3] > 1:
         raise ValueError("k_pages, v_pages: the values of a head must be adjacent")
-    return k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], k.shape[0], k.shape[1]
+    return k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], shape[0], shape[1]
 
 
 def _dtype_of(t):
@@ -581,7 +581,8 @@ def _rope_table_of(table):
         return 0, 0, 0
     if table.dim() != 3 or table.shape[2] != 2:
         raise ValueError("table: expected a tensor [positions, rot / 2, 2]")
-    return _ptr(table, _float32), table.shape[0], 2 * table.shape[1]
+    n, half, _ = table.shape
+    return _ptr(table, _float32), n, 2 * half
 
 
 def hps_seq_extend(past_lens, new_lens, block_size, free_blocks, n_free, block_table, token_offsets, total_lens, slots, positions, info,
@@ -593,9 +594,9 @@ def hps_seq_extend(past_lens, new_lens, block_size, free_blocks, n_free, block_t
         raise ValueError("block_table: expected a tensor [requests, width]")
     most, = slots.shape
     args = _SEQ_EXTEND.pack(
-        _ints(past_lens, "past_lens"), _ints(new_lens, "new_lens", (n,)), _ints(start, "start", (n,)), _ints(free_blocks, "free_blocks"),
-        _word(n_free, "n_free"), _ints(block_table, "block_table"), _ints(token_offsets, "token_offsets", (n + 1,)),
-        _ints(total_lens, "total_lens", (n,)), _ints(slots, "slots"), _ints(positions, "positions", (most,)), _ints(info, "info", (4,)),
+        _ints(past_lens, "past_lens"), _ints(new_lens, "new_lens", n), _ints(start, "start", n), _ints(free_blocks, "free_blocks"),
+        _word(n_free, "n_free"), _ints(block_table, "block_table"), _ints(token_offsets, "token_offsets", n + 1),
+        _ints(total_lens, "total_lens", n), _ints(slots, "slots"), _ints(positions, "positions", most), _ints(info, "info", 4),
         n, block_size, free_blocks.numel(), block_table.shape[1], most)
     status = (_lib or load_library()).hps_seq_extend(args, _stream(stream))
     if status:
@@ -608,8 +609,8 @@ def hps_seq_release(lens, finished, block_size, block_table, free_blocks, n_free
     if block_table.dim() != 2 or block_table.shape[0] != n:
         raise ValueError("block_table: expected a tensor [requests, width]")
     _check_seq(load_library().hps_seq_release(
-        _ints(lens, "lens"), _ints(finished, "finished", (n,)), n, block_size, _ints(block_table, "block_table"), block_table.shape[1],
-        _ints(free_blocks, "free_blocks"), free_blocks.numel(), _word(n_free, "n_free"), _ints(info, "info", (4,)), _stream(stream)))
+        _ints(lens, "lens"), _ints(finished, "finished", n), n, block_size, _ints(block_table, "block_table"), block_table.shape[1],
+        _ints(free_blocks, "free_blocks"), free_blocks.numel(), _word(n_free, "n_free"), _ints(info, "info", 4), _stream(stream)))
 
 
 def hps_seq_rope_table(table, base=10000.0, scale=HPS_SEQ_SCALE_NONE, factor=1.0, original=1.0, low=1.0, high=2.0, magnitude=1.0, stream=None) -> None:
@@ -620,15 +621,16 @@ def hps_seq_rope_table(table, base=10000.0, scale=HPS_SEQ_SCALE_NONE, factor=1.0
 
 def hps_seq_rope(q, q_out, positions, table, k=None, k_out=None, interleaved=False, inverse=False, stream=None) -> None:
     """q, q_out [tokens, heads, dim] (and k, k_out with heads of their own) turned by table[positions]; inverse: the gradient."""
-    T, H, D = q.shape
+    T, H, D = shape = q.shape
     dtype = q.dtype
     address, n, rot = _rope_table_of(table)
     none, hk = (0, 0, 0), 0
     if k is not None:
         hk = k.shape[1]
+        k_shape = (T, hk, D)
     args = _SEQ_ROPE.pack(
-        *_heads(q, "q", dtype, T, H, D), *(_heads(k, "k", dtype, T, hk, D) if k is not None else none), *_heads(q_out, "q_out", dtype, T, H, D),
-        *(_heads(k_out, "k_out", dtype, T, hk, D) if k is not None else none), _ints(positions, "positions", (T,)), address,
+        *_heads(q, "q", dtype, shape), *(_heads(k, "k", dtype, k_shape) if k is not None else none), *_heads(q_out, "q_out", dtype, shape),
+        *(_heads(k_out, "k_out", dtype, k_shape) if k is not None else none), _ints(positions, "positions", T), address,
         T, H, hk, D, rot, n, _dtype_of(q), bool(interleaved), bool(inverse))
     status = (_lib or load_library()).hps_seq_rope(args, _stream(stream))
     if status:
@@ -638,20 +640,21 @@ def hps_seq_rope(q, q_out, positions, table, k=None, k_out=None, interleaved=Fal
 def hps_seq_append(k, v, k_pages, v_pages, slots, q=None, q_out=None, positions=None, table=None, interleaved=False, stream=None) -> None:
     """Keys (turned, with a table) and values [tokens, kv heads, dim] to slots of pages [blocks, block size, kv heads, dim]; queries
     [tokens, heads, dim] turned into q_out."""
-    T, hk, D = k.shape
+    T, hk, D = k_shape = k.shape
     dtype = k.dtype
     address, n, rot = _rope_table_of(table)
     none, H = (0, 0, 0), 0
     if q is not None:
         H = q.shape[1]
+        shape = (T, H, D)
     pages = _pages(k_pages, v_pages, dtype)
     if k_pages.shape[2:] != (hk, D):
         raise ValueError("k_pages, v_pages: heads and dim differ from the keys'")
     if table is not None and positions is None:
         raise ValueError("positions: needed with a table")
     args = _SEQ_APPEND.pack(
-        *(_heads(q, "q", dtype, T, H, D) if q is not None else none), *(_heads(q_out, "q_out", dtype, T, H, D) if q is not None else none),
-        *_heads(k, "k", dtype, T, hk, D), *_heads(v, "v", dtype, T, hk, D), *pages, _ints(slots, "slots", (T,)), _ints(positions, "positions", (T,)), address,
+        *(_heads(q, "q", dtype, shape) if q is not None else none), *(_heads(q_out, "q_out", dtype, shape) if q is not None else none),
+        *_heads(k, "k", dtype, k_shape), *_heads(v, "v", dtype, k_shape), *pages, _ints(slots, "slots", T), _ints(positions, "positions", T), address,
         T, H, hk, D, rot, n, _dtype_of(k), bool(interleaved))
     status = (_lib or load_library()).hps_seq_append(args, _stream(stream))
     if status:
@@ -681,11 +684,11 @@ def hps_seq_attention(session, q, k_pages, v_pages, block_table, lens, token_off
     token_offsets int32 [requests + 1]; prefix_table int32 [groups, width], prefix_lens int32 [groups], group_offsets int32 [groups + 1]; lse float32
     [tokens, heads].  The bounds max_new, max_len, max_prefix and max_group are, where they are not given, the most that the shapes allow.
     scale: 1 / sqrt(dim) if None."""
-    T, H, D = q.shape
+    T, H, D = shape = q.shape
     dtype = q.dtype
     pages = _pages(k_pages, v_pages, dtype)
-    hk, block = k_pages.shape[2], pages[6]
-    if k_pages.shape[3] != D:
+    _, block, hk, dim = k_pages.shape
+    if dim != D:
         raise ValueError("k_pages, v_pages: dim differs from the queries'")
     n, = lens.shape
     if block_table.dim() != 2 or block_table.shape[0] != n:
@@ -699,9 +702,9 @@ def hps_seq_attention(session, q, k_pages, v_pages, block_table, lens, token_off
     if lse is not None and lse.shape != (T, H):
         raise ValueError(f"lse: expected shape {(T, H)}, got {tuple(lse.shape)}")
     args = _SEQ_ATTENTION.pack(
-        *_heads(q, "q", dtype, T, H, D), *_heads(out, "out", dtype, T, H, D), *pages, _ints(prefix_table, "prefix_table") if groups else 0,
-        _ints(prefix_lens, "prefix_lens") if groups else 0, _ints(group_offsets, "group_offsets", (groups + 1,)) if groups else 0,
-        _ints(block_table, "block_table"), _ints(lens, "lens"), _ints(token_offsets, "token_offsets", (n + 1,)), _ptr(lse, _float32) or 0,
+        *_heads(q, "q", dtype, shape), *_heads(out, "out", dtype, shape), *pages, _ints(prefix_table, "prefix_table") if groups else 0,
+        _ints(prefix_lens, "prefix_lens") if groups else 0, _ints(group_offsets, "group_offsets", groups + 1) if groups else 0,
+        _ints(block_table, "block_table"), _ints(lens, "lens"), _ints(token_offsets, "token_offsets", n + 1), _ptr(lse, _float32) or 0,
         T, n, groups, width, prefix_width, T if max_new is None else max_new, T if max_group is None else max_group,
         width * block if max_len is None else max_len, prefix_width * block if max_prefix is None else max_prefix, H, hk, D,
         _dtype_of(q), D ** -0.5 if scale is None else scale)
