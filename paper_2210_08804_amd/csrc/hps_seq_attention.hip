@@ -119,6 +119,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     static constexpr int kRow = DT <= 2 ? 128 : DT <= 4 ? 256 : 512;        // bytes of a row in LDS
     static constexpr int kChunks = kRow / 16, kSteps = 2 * DT;
+    static constexpr bool kFull = kExact && 64 * DT == kRow;                // every chunk of a row in LDS is one of the head's
     static constexpr int kLoads = 16 * kRow / 1024, kLoadRows = 1024 / kRow;        // wave loads of 16 rows, rows of one
     static constexpr uint32_t kLds = 256 * kRow;       // wide: 2 stages of 64 keys and values; narrow: 4 waves of 32
     static constexpr uint32_t kWaveLds = 64 * kRow;    // of a narrow wave
@@ -193,14 +194,14 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const uint32_t chunk = (kValues ? load_v : load_k) ^ sw<kValues>(i * kLoadRows) << 4;
-                if (kExact || chunk < 2 * a.head_dim) load_to_lds(base + (int64_t)(i * kLoadRows) * a.page_token, load_row + chunk, to + i * 1024);
+                if (kFull || chunk < 2 * a.head_dim) load_to_lds(base + (int64_t)(i * kLoadRows) * a.page_token, load_row + chunk, to + i * 1024);
             }
             return true;
         }
 #pragma unroll 1
         for (int i = 0; i < kLoads; ++i) {
             const uint32_t t = i * kLoadRows + lane / kChunks, chunk = (lane % kChunks) ^ sw<kValues>(t), key = at + t;
-            if (!kExact && chunk * 8 >= a.head_dim) continue;               // nothing ever lies there
+            if (!kFull && chunk * 8 >= a.head_dim) continue;               // nothing ever lies there
             const char *from = nullptr;
             if (key < it.end) {
                 const uint32_t b = (uint32_t)it.table[key >> a.sh];
@@ -289,9 +290,9 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     template <int kAt> __device__ __forceinline__ bool any_odd() const {
         constexpr uint32_t e = Type<T>::kExp;
         uint32_t odd = 0;
-#pragma unroll 1
-        for (uint32_t x = lane * 16; x < 32 * kRow; x += 64 * 16) {
-            const u32x4 y = *(lds_u32x4 *)((lds_char *)(uintptr_t)(here + x) + kAt);
+#pragma unroll
+        for (int i = 0; i < 2 * kLoads; ++i) {
+            const u32x4 y = *(lds_u32x4 *)((lds_char *)(uintptr_t)(here + lane * 16) + kAt + i * 1024);
 #pragma unroll
             for (int j = 0; j < 4; ++j) odd |= (uint32_t)((y[j] & e) == e) | (uint32_t)((y[j] >> 16 & e) == e);
         }
@@ -582,7 +583,7 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
     extern __shared__ __align__(16) char shared[];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_char *)shared;
-    if (!kExact || DT == 3) {                          // places of LDS rows that no load fills
+    if (!E::kFull) {                                   // places of LDS rows that no load fills
         for (uint32_t x = threadIdx.x * 16; x < E::kLds; x += kThreads * 16) *(u32x4 *)(shared + x) = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
@@ -799,12 +800,22 @@ struct hps_seq_attention_session {
 
 namespace {
 
+template <typename T, int DT, bool kExact> constexpr uint32_t kAttendLds = Engine<T, DT, kExact>::kLds + kWaves * 32 * sizeof(float2);
+
+// Kernels that use more LDS than 64 KiB have to be told so once a device.
+template <typename T, int DT> hipError_t allow_lds() {
+    static_assert(kAttendLds<T, DT, true> <= 160 * 1024, "LDS of a CU");
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, kAttendLds<T, DT, true>)) return e;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, kAttendLds<T, DT, false>);
+}
+template <typename T> hipError_t allow_lds() {
+    if (hipError_t e = allow_lds<T, 3>()) return e;
+    if (hipError_t e = allow_lds<T, 4>()) return e;
+    return allow_lds<T, 8>();
+}
+
 template <typename T, int DT, bool kExact> hipError_t launch_attend(const Args &a, uint32_t groups, hipStream_t st) {
-    constexpr uint32_t bytes = Engine<T, DT, kExact>::kLds + kWaves * 32 * sizeof(float2);
-    static_assert(bytes <= 160 * 1024, "LDS of a CU");
-    if (bytes > 64 * 1024)
-        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_kernel<T, DT, kExact>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
-    hipLaunchKernelGGL((attend_kernel<T, DT, kExact>), dim3(groups), dim3(kThreads), bytes, st, a);
+    hipLaunchKernelGGL((attend_kernel<T, DT, kExact>), dim3(groups), dim3(kThreads), (kAttendLds<T, DT, kExact>), st, a);
     return hipGetLastError();
 }
 
@@ -852,18 +863,22 @@ hps_status_t hps_seq_attention_create(size_t max_rows, uint32_t max_head_dim, hp
     hipError_t e = hipGetDevice(&s->device);
     if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, s->device);
     s->cus = cus > 0 ? (uint32_t)cus : 256u;
-    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->part_o), s->part_rows * s->max_head_dim * sizeof(float));
-    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->part_ml), s->part_rows * sizeof(float2));
-    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&s->flags), 256);
+    if (e == hipSuccess) e = allow_lds<_Float16>();
+    if (e == hipSuccess) e = allow_lds<__bf16>();
+    // one piece: values (a multiple of 32 bytes a row), references and sums, the flag word
+    const size_t o_bytes = s->part_rows * s->max_head_dim * sizeof(float), ml_bytes = s->part_rows * sizeof(float2);
+    char *piece = nullptr;
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&piece), o_bytes + ml_bytes + 256);
     if (e == hipSuccess) {
+        s->part_o = reinterpret_cast<float *>(piece);
+        s->part_ml = reinterpret_cast<float2 *>(piece + o_bytes);
+        s->flags = reinterpret_cast<uint32_t *>(piece + o_bytes + ml_bytes);
         hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(1), 0, 0, s->flags);
         e = hipGetLastError();
     }
     if (e == hipSuccess) e = hipStreamSynchronize(0);
     if (e != hipSuccess) {
-        (void)hipFree(s->part_o);
-        (void)hipFree(s->part_ml);
-        (void)hipFree(s->flags);
+        (void)hipFree(piece);
         delete s;
         (void)hipGetLastError();
         return hps_seq_fail(e == hipErrorOutOfMemory ? HPS_ERR_OOM : HPS_ERR_DEVICE, "hps_seq_attention_create: ", hipGetErrorString(e));
@@ -881,8 +896,6 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s) {
     SEQ_TRY(hipSetDevice(s->device));
     hipError_t e = hipDeviceSynchronize();
     (void)hipFree(s->part_o);
-    (void)hipFree(s->part_ml);
-    (void)hipFree(s->flags);
     s->magic = 0;
     delete s;
     (void)hipSetDevice(prev);
@@ -903,6 +916,9 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     SEQ_REQUIRE(s && s->magic == kMagic, "not a live attention session");
     SEQ_REQUIRE(args, "args must not be NULL");
     const hps_seq_attention_args_t &r = *args;
+    int device = -1;
+    SEQ_TRY(hipGetDevice(&device));
+    SEQ_REQUIRE(device == s->device, "the session is of another device than the current one");
     SEQ_REQUIRE(r.dtype == HPS_SEQ_F16 || r.dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F16 or HPS_SEQ_BF16");
     SEQ_REQUIRE(r.head_dim > 0 && r.head_dim % 8 == 0 && r.head_dim <= 256, "head_dim must be a multiple of 8 in 8 .. 256");
     SEQ_REQUIRE(r.head_dim <= s->max_head_dim, "head_dim exceeds the session's max_head_dim");
