@@ -828,8 +828,9 @@ template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, 
         constexpr int kWays = decltype(ways)::value, kRows = kJoin / (kLanes * kWays);
         hipLaunchKernelGGL((join_kernel<T, kLanes, kWays>), dim3(div_up(rows, kRows)), dim3(kJoin), kRows * parts * sizeof(float), st, a, parts);
     };
-    // few rows: more lanes to a row, which read its parts side by side
-    if (rows * kLanes < 16384 && parts >= 4) join(std::integral_constant<int, kJoin / kLanes>());
+    // Few rows: all lanes of a work-group to one, which read its parts side by side (a row each / several rows each, us of a whole
+    // call, 16 heads of 128: 1 token behind 1,000 keys 13.0 / 13.8, 4 behind 32,768 21.6 / 36.6, 64 37.0 / 45.1, 256 behind 1,000 25.1 / 22.3).
+    if (rows * kLanes <= 65536) join(std::integral_constant<int, kJoin / kLanes>());
     else join(std::integral_constant<int, 1>());
     return hipGetLastError();
 }
@@ -992,7 +993,10 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
         a.own_chunks = choose_chunks(requests_heads * a.own_tiles, own_keys, true, rows, r.head_dim, s->cus, part_limit / 2);
         a.own_chunk = div_up(div_up(own_keys, a.own_chunks), kWideKeys) * kWideKeys;
     } else {
-        a.own_mode = own_keys <= 2 * kNarrowKeys * kWaves ? kOwnSolo : kOwnSplit;
+        // A wave to a request where there are more requests than work-groups at a time, up to 512 keys (a wave / a work-group each, us, 4
+        // key heads of 128: 64 requests of 64 / 256 / 512 keys 14.6, 21.9, 32.4 / 13.9, 14.9, 19.9; 512 of 64 / 256 / 512 / 1,024 keys 26.2, 38.0,
+        // 63.2, 134.1 / 43.6, 50.6, 69.6, 129.2).
+        a.own_mode = requests_heads > 2 * s->cus && own_keys <= 512 ? kOwnSolo : kOwnSplit;
         a.own_tiles = 1;
         const uint32_t step = a.own_mode == kOwnSolo ? kNarrowKeys : kNarrowKeys * kWaves;
         a.own_chunks = a.own_mode == kOwnSolo ? 1 : choose_chunks(requests_heads, own_keys, false, rows, r.head_dim, s->cus, part_limit / 2);
@@ -1003,7 +1007,9 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     uint64_t history_groups = 0;
     if (r.n_groups && r.max_prefix && a.max_group) {
         const uint64_t group_rows = (uint64_t)a.max_group * a.ratio;
-        a.history_wide = group_rows > kNarrowRows;
+        // Up to 32 rows the waves share the keys; up to 64 too, in two work-groups, where reading a long history is what counts (waves share
+        // keys / rows, us: 64 rows behind 4,096 keys 16.1 / 15.4, behind 65,536 36.9 / 41.1; 96 rows 53.1 / 37.7).
+        a.history_wide = group_rows > (r.max_prefix >= 16384 ? 2 : 1) * kNarrowRows;
         a.history_tiles = div_up(group_rows, a.history_wide ? kWideRows : kNarrowRows);
         const uint32_t step = a.history_wide ? kWideKeys : kNarrowKeys * kWaves;
         a.history_chunks = choose_chunks((uint64_t)a.history_tiles * r.n_groups * r.kv_heads, r.max_prefix, a.history_wide, rows, r.head_dim, s->cus, part_limit - a.own_chunks);
