@@ -188,7 +188,7 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  * length that its table does not hold; a block number outside 0 .. n_blocks - 1 within a length raises
  * HPS_SEQ_FLAG_BLOCK and stands for a block of zeros.
  * dtype HPS_SEQ_F16 or HPS_SEQ_BF16; head_dim a multiple of 8 up to 256; q_heads a multiple of
- * kv_heads; all data and strides multiples of 16 bytes; scale finite and > 0.
+ * kv_heads; all data and strides multiples of 16 bytes, the pages' not negative; scale finite and > 0.
  */
 typedef struct {
     hps_seq_heads_t q, out;

@@ -39,9 +39,9 @@ constexpr float kInf = __builtin_inff();
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr uint32_t kWideRows = 128, kNarrowRows = 32;  // rows of a work-group
 constexpr uint32_t kWideKeys = 64, kNarrowKeys = 32;   // keys of a step: of the work-group, of a wave
-// A row's reference m need not be its maximum: it moves when a score is this far ahead (in powers of two), or weights sum to
-// Type::kMost, which is within the type's range.  Most steps need no rescaling then; precision is relative and the same.
-constexpr float kSlack = 8.f;
+// A row's reference m need not be its maximum: it moves when a score is kSlack ahead (in powers of two), or 16 weights of
+// a lane sum to kMost, far within both types' range.  Most steps need no rescaling then; precision is relative and the same.
+constexpr float kSlack = 8.f, kMost = 0x1p12f;
 
 struct Args {
     const char *q, *k, *v;
@@ -50,7 +50,8 @@ struct Args {
     float2 *part_ml;                                   // reference and sum of each part's row; sum 0: nothing attended
     uint32_t *flags;
     const int32_t *prefix_table, *prefix_lens, *group_offsets, *block_table, *lens, *token_offsets;
-    int64_t q_token, q_head, out_token, out_head, page_block, page_token, page_head;       // strides in bytes
+    int64_t q_token, q_head, out_token, out_head, page_head;            // strides in bytes
+    uint32_t page_block, page_token;
     uint32_t n_tokens, n_requests, n_groups, table_width, prefix_width, max_new, max_group, max_len, max_prefix;
     uint32_t q_heads, kv_heads, ratio, head_dim, n_blocks, sh;
     uint32_t history_groups, history_tiles, history_chunks, history_chunk, history_combos; // work-groups; row tiles; chunks, keys of one; (group, chunk, head)
@@ -65,13 +66,11 @@ template <> struct Type<__bf16> {
     typedef bf16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7F80u;
-    static constexpr float kMost = 0x1p40f;
 };
 template <> struct Type<_Float16> {
     typedef f16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7C00u;
-    static constexpr float kMost = 0x1p14f;
 };
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -153,7 +152,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         const uint32_t t = 4 * half + (g >> 2), r = lane / kChunks;
         v_row = lds + t * kRow;
         v_chunk = ((2 * ((lane >> 4) & 1u) + ((g & 3u) >> 1)) ^ sw_v(t)) << 4 | (g & 1u) << 3;
-        load_row = r * (uint32_t)a.page_token;
+        load_row = r * a.page_token;
         load_k = (lane % kChunks ^ sw_k(r)) << 4;
         load_v = (lane % kChunks ^ sw_v(r)) << 4;
         const uint32_t row = it.row0 + first_row + n, i = row / a.ratio;
@@ -190,11 +189,11 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     template <bool kValues> __device__ __forceinline__ bool load16(uint32_t at, int32_t id, uint32_t to) {
         const char *head = kValues ? v_head : k_head;
         if (__builtin_expect(at + 16 <= it.end && (uint32_t)id < a.n_blocks, 1)) {
-            const char *base = head + (int64_t)id * a.page_block + (int64_t)(at & ((1u << a.sh) - 1u)) * a.page_token;
+            const char *base = head + (uint64_t)(uint32_t)id * a.page_block + (uint64_t)(at & ((1u << a.sh) - 1u)) * a.page_token;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const uint32_t chunk = (kValues ? load_v : load_k) ^ sw<kValues>(i * kLoadRows) << 4;
-                if (kFull || chunk < 2 * a.head_dim) load_to_lds(base + (int64_t)(i * kLoadRows) * a.page_token, load_row + chunk, to + i * 1024);
+                if (kFull || chunk < 2 * a.head_dim) load_to_lds(base + (uint64_t)a.page_token * (i * kLoadRows), load_row + chunk, to + i * 1024);
             }
             return true;
         }
@@ -205,7 +204,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
             const char *from = nullptr;
             if (key < it.end) {
                 const uint32_t b = (uint32_t)it.table[key >> a.sh];
-                if (b < a.n_blocks) from = head + (int64_t)b * a.page_block + (int64_t)(key & ((1u << a.sh) - 1u)) * a.page_token + chunk * 16;
+                if (b < a.n_blocks) from = head + (uint64_t)b * a.page_block + (uint64_t)(key & ((1u << a.sh) - 1u)) * a.page_token + chunk * 16;
                 else atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
             }
             if (from) load_to_lds(from, to + i * 1024);
@@ -333,7 +332,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     // meeting a step.  The scores of the next 32 keys are formed beside the weights of these, so that a wave's matrix
     // instructions run while it computes exponentials: the keys of a step are 32 ahead of its values.
     // The inner loop has the steps of which every row sees all keys and whose reference can stay: weights may be large, they
-    // only must not overflow (Type::kMost), which their sum shows.  The others leave it for the end of the step.
+    // only must not overflow (kMost), which their sum shows.  The others leave it for the end of the step.
     __device__ __forceinline__ void wide() {
         const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit(), mine = 16 * wave;
         if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
@@ -377,7 +376,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 if (at + 64 > least) break;
                 t = scores<0>();
                 float sum = weights(s, w, m);       // infinite, or NaN, the first time: m is -inf
-                if (__ballot(!(sum < Type<T>::kMost))) {
+                if (__ballot(!(sum < kMost))) {
                     ahead = true;
                     break;
                 }
@@ -385,7 +384,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 add_values<kWideValues>(w);
                 s = scores<32 * kRow>();
                 sum = weights(t, w, m);
-                if (__ballot(!(sum < Type<T>::kMost))) {
+                if (__ballot(!(sum < kMost))) {
                     ahead = true;
                     left = 1;
                     const f32x16 x = s;
@@ -939,6 +938,7 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     SEQ_REQUIRE(r.pages.n_blocks == 0 || (r.pages.k && r.pages.v && seq_aligned(r.pages.k, 16) && seq_aligned(r.pages.v, 16)), "the pages must be device pointers, 16-byte aligned");
     SEQ_REQUIRE(multiple16(r.pages.block_stride) && multiple16(r.pages.token_stride) && multiple16(r.pages.head_stride), "the pages' strides must be multiples of 16 bytes");
     SEQ_REQUIRE(r.pages.token_stride >= 0 && r.pages.token_stride < (1 << 25), "the pages' token_stride must be in 0 .. 2^25 - 1");
+    SEQ_REQUIRE(r.pages.block_stride >= 0 && r.pages.block_stride < (1ll << 31), "the pages' block_stride must be in 0 .. 2^31 - 1");
     SEQ_REQUIRE(r.n_groups == 0 || (seq_words(r.prefix_lens) && seq_words(r.group_offsets) && (r.prefix_width == 0 || seq_words(r.prefix_table))),
                 "prefix_table, prefix_lens and group_offsets must be 4-byte aligned device pointers");
     SEQ_REQUIRE(r.lse == nullptr || seq_aligned(r.lse, 4), "lse must be 4-byte aligned");
@@ -962,8 +962,8 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     a.q_head = r.q.head_stride * 2;
     a.out_token = r.out.token_stride * 2;
     a.out_head = r.out.head_stride * 2;
-    a.page_block = r.pages.block_stride * 2;
-    a.page_token = r.pages.token_stride * 2;
+    a.page_block = (uint32_t)(r.pages.block_stride * 2);
+    a.page_token = (uint32_t)(r.pages.token_stride * 2);
     a.page_head = r.pages.head_stride * 2;
     a.n_tokens = r.n_tokens;
     a.n_requests = r.n_requests;
