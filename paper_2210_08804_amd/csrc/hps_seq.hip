@@ -348,9 +348,18 @@ struct RopeArgs {
 
 template <typename T, int E> struct alignas(E * sizeof(T) > 16 ? 16 : E * sizeof(T)) Vec { T v[E]; };
 
+// One pair, in 32 bits, rounded once; the products are written out, so that every shape of the kernel gives the same bits.
+template <typename T> __device__ __forceinline__ void turn(T &a, T &b, float c, float s) {
+    const float p = (float)a, q = (float)b, qs = q * s, qc = q * c;
+    a = (T)__builtin_fmaf(p, c, -qs);
+    b = (T)__builtin_fmaf(p, s, qc);
+}
+
 // One work-group per token.  A lane has two vectors of 16 bytes of a head (for halves: the two that hold E pairs), which
-// stay the same from head to head, so cosines and sines are read once for all of them; two heads are in flight at a time.
-// Bound by HBM: each input and output passes once.  E = 1 is for rows that are not in whole 16-byte vectors.
+// stay the same from head to head, so cosines and sines are read once for all of them.  Bound by HBM where tokens have many
+// heads (8,192 tokens of 48 heads of 128: 37.5 us, 5.4 TB/s while the pages are in the Infinity Cache, 50 us, 4.0 TB/s, otherwise),
+// else by the chain position, cosines, rows, store.  Two heads under way instead of one: 38.6 us, four 41.7; rows requested in front of
+// the position 41.1.  E = 1 is for rows that are not in whole 16-byte vectors (67.9 us).
 template <typename T, int E, bool kPages>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
     typedef Vec<T, E> V;
@@ -358,11 +367,6 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
     const uint32_t lane_head = tid / a.spans, s = tid - lane_head * a.spans;
     if (lane_head >= a.per_pass) return;
     const bool turns = a.table != nullptr;
-    const int32_t pos = turns ? a.positions[t] : 0;
-    if (pos < 0) return;
-    uint32_t slot = 0;
-    if (kPages) slot = (uint32_t)a.slots[t];
-    const bool stored = !kPages || slot < a.n_slots;
 
     // the two vectors (o0, o1, in values), and the pairs in them
     const bool within = a.interleaved && E > 1;        // pairs lie within a vector
@@ -376,6 +380,11 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
         o1 = s < split ? a.half + s * E : o0 + E;
     }
     const bool has0 = o0 < a.head_dim, has1 = o1 < a.head_dim;
+    const int32_t pos = turns ? a.positions[t] : 0;
+    uint32_t slot = 0;
+    if (kPages) slot = (uint32_t)a.slots[t];
+    if (pos < 0) return;
+    const bool stored = !kPages || slot < a.n_slots;
     const bool turn0 = turns && o0 < 2 * a.half, turn1 = turns && o1 < 2 * a.half;
     float cs[E], sn[E];                                // of the pairs: across the two vectors E, within them E / 2 each
 #pragma unroll
@@ -399,63 +408,39 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
         }
     }
 
-    constexpr int U = 2;
-    for (uint32_t h0 = lane_head; h0 < a.n_heads; h0 += U * a.per_pass) {
-        V x[U], y[U];
-        char *to[U];
-        bool turned[U], live[U];
+    for (uint32_t hh = lane_head; hh < a.n_heads; hh += a.per_pass) {
+        const int seg = hh < a.heads[0] ? 0 : hh < a.heads[0] + a.heads[1] ? 1 : 2;
+        if (seg > 0 && !stored) break;                 // keys and values come last
+        const uint32_t h = hh - (seg > 0 ? a.heads[0] : 0) - (seg > 1 ? a.heads[1] : 0);
+        const char *from = seg == 0 ? a.in[0] : seg == 1 ? a.in[1] : a.in[2];
+        const int64_t it = seg == 0 ? a.in_token[0] : seg == 1 ? a.in_token[1] : a.in_token[2];
+        const int64_t ih = seg == 0 ? a.in_head[0] : seg == 1 ? a.in_head[1] : a.in_head[2];
+        from += (int64_t)t * it + (int64_t)h * ih;
+        V x, y;
+        if (has0) x = *(const V *)(from + o0 * sizeof(T));
+        if (has1) y = *(const V *)(from + o1 * sizeof(T));
+        char *to = seg == 0 ? a.out[0] : seg == 1 ? a.out[1] : a.out[2];
+        const int64_t ot = seg == 0 ? a.out_token[0] : seg == 1 ? a.out_token[1] : a.out_token[2];
+        const int64_t oh = seg == 0 ? a.out_head[0] : seg == 1 ? a.out_head[1] : a.out_head[2];
+        if (kPages && seg > 0) to += (int64_t)(slot >> a.sh) * a.page_block + (int64_t)(slot & ((1u << a.sh) - 1u)) * ot;
+        else to += (int64_t)t * ot;
+        to += (int64_t)h * oh;
+        if (seg < 2 && turn0) {
+            if (within) {
+                if constexpr (E > 1) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t hh = h0 + u * a.per_pass;
-            const uint32_t seg = hh < a.heads[0] ? 0 : hh < a.heads[0] + a.heads[1] ? 1 : 2;
-            const uint32_t h = hh - (seg > 0 ? a.heads[0] : 0) - (seg > 1 ? a.heads[1] : 0);
-            live[u] = hh < a.n_heads && (seg == 0 || stored);
-            turned[u] = seg < 2;
-            to[u] = nullptr;
-            if (!live[u]) continue;
-            const char *from = (seg == 0 ? a.in[0] : seg == 1 ? a.in[1] : a.in[2]);
-            const int64_t it = seg == 0 ? a.in_token[0] : seg == 1 ? a.in_token[1] : a.in_token[2];
-            const int64_t ih = seg == 0 ? a.in_head[0] : seg == 1 ? a.in_head[1] : a.in_head[2];
-            from += (int64_t)t * it + (int64_t)h * ih;
-            char *dst = seg == 0 ? a.out[0] : seg == 1 ? a.out[1] : a.out[2];
-            const int64_t ot = seg == 0 ? a.out_token[0] : seg == 1 ? a.out_token[1] : a.out_token[2];
-            const int64_t oh = seg == 0 ? a.out_head[0] : seg == 1 ? a.out_head[1] : a.out_head[2];
-            if (kPages && seg > 0) dst += (int64_t)(slot >> a.sh) * a.page_block + (int64_t)(slot & ((1u << a.sh) - 1u)) * ot;
-            else dst += (int64_t)t * ot;
-            to[u] = dst + (int64_t)h * oh;
-            if (has0) x[u] = *(const V *)(from + o0 * sizeof(T));
-            if (has1) y[u] = *(const V *)(from + o1 * sizeof(T));
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!live[u]) continue;
-            if (turned[u] && turn0) {
-                if (within) {
-                    if constexpr (E > 1) {
-#pragma unroll
-                        for (int j = 0; j < E / 2; ++j) {
-                            const float p = (float)x[u].v[2 * j], q = (float)x[u].v[2 * j + 1];
-                            x[u].v[2 * j] = (T)(p * cs[j] - q * sn[j]);
-                            x[u].v[2 * j + 1] = (T)(p * sn[j] + q * cs[j]);
-                            if (turn1) {
-                                const float p1 = (float)y[u].v[2 * j], q1 = (float)y[u].v[2 * j + 1];
-                                y[u].v[2 * j] = (T)(p1 * cs[E / 2 + j] - q1 * sn[E / 2 + j]);
-                                y[u].v[2 * j + 1] = (T)(p1 * sn[E / 2 + j] + q1 * cs[E / 2 + j]);
-                            }
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float p = (float)x[u].v[j], q = (float)y[u].v[j];
-                        x[u].v[j] = (T)(p * cs[j] - q * sn[j]);
-                        y[u].v[j] = (T)(p * sn[j] + q * cs[j]);
+                    for (int j = 0; j < E / 2; ++j) {
+                        turn(x.v[2 * j], x.v[2 * j + 1], cs[j], sn[j]);
+                        if (turn1) turn(y.v[2 * j], y.v[2 * j + 1], cs[E / 2 + j], sn[E / 2 + j]);
                     }
                 }
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j) turn(x.v[j], y.v[j], cs[j], sn[j]);
             }
-            if (has0) *(V *)(to[u] + o0 * sizeof(T)) = x[u];
-            if (has1) *(V *)(to[u] + o1 * sizeof(T)) = y[u];
         }
+        if (has0) *(V *)(to + o0 * sizeof(T)) = x;
+        if (has1) *(V *)(to + o1 * sizeof(T)) = y;
     }
 }
 
