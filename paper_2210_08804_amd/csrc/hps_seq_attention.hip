@@ -333,6 +333,10 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     // instructions run while it computes exponentials: the keys of a step are 32 ahead of its values.
     // The inner loop has the steps of which every row sees all keys and whose reference can stay: weights may be large, they
     // only must not overflow (kMost), which their sum shows.  The others leave it for the end of the step.
+    // Bound by the matrix instructions and what they wait for: 512 requests of 32 / 8 heads of 128 behind 32,768 keys take 285 us in
+    // this kernel (964 TFLOP/s; matrix instructions alone 210, without loads 249, without exponentials 287).  The matrix pipes
+    // are busy 48 % of all cycles, LDS has no bank conflict, the clock is 1.86 to 2.0 GHz.  Two meetings a step 318 us instead of
+    // 307; eight waves to a work-group 292 instead of 299, but 42.5 instead of 40.2 for 256 requests behind 8,192 keys.
     __device__ __forceinline__ void wide() {
         const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit(), mine = 16 * wave;
         if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
@@ -421,7 +425,8 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     }
 
     // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon
-    // as the scores are there, the next values behind the product with these.
+    // as the scores are there, the next values behind the product with these.  Bound by HBM where histories are long (4 requests of
+    // 32 / 8 heads of 128 behind 200,003 keys: 149 us, 5.5 TB/s), else by the chain offsets, block, keys, scores, values.
     __device__ __forceinline__ void narrow(uint32_t from, uint32_t stride) {
         const uint32_t least = least_limit();
         if (from >= it.end) return;
@@ -666,7 +671,9 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
 
 // Joins the parts of a row.  A work-group has kRows rows, kLanes lanes with four values each of every kWays-th part.  First
 // every lane computes one part's share of one row (the references and sums of all parts are read side by side), then the
-// values are read, several parts under way at a time.  Bound by the round trips where rows are few, else by reading the parts.
+// values are read, several parts under way at a time.  Bound by the round trips where rows are few (64 rows: 4 us), else by
+// reading the parts (16,384 rows of 5 parts of 128 values: 10 us, 4.2 TB/s).  Done in the launch in front, by the work-group that ends
+// last, it costs more: with the fences that its reading needs 8 candidates behind 500 keys take 24 us instead of 14.
 constexpr int kJoin = 256, kMaxParts = 1024;
 template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kJoin) join_kernel(const Args a, uint32_t parts) {
     constexpr uint32_t kRows = kJoin / (kLanes * kWays), kPerRow = kJoin / kRows;

@@ -202,6 +202,19 @@ def test_extreme_scores():
     assert (out == 0).all() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("H,K,new", [(2, 2, 1), (16, 1, 9)])
+def test_large_values_behind_growing_scores(H, K, new):
+    """The sums are formed against a reference that may lie behind the largest score: they have room for values of 2^80."""
+    p = Problem(BF, 64, H, K, 16, [(3000, 1)], [(new + 40, new)], seed=4, scale=1.0)
+    p.q[:] = 1
+    for i in range(3000):                              # 0.05 a key: the weights pass every line at which the reference moves
+        p.k[int(p.prefix_table[0, i // 16]), i % 16] = i / 1280
+    p.v *= 2.0 ** 80
+    p.check()
+    p.v *= 2.0 ** -160                                 # and small ones are not lost
+    p.check()
+
+
 def test_histories_behind_four_gibibytes():
     """Blocks whose keys and values are more than 2^32 bytes from the first one."""
     K, D, block = 8, 128, 64
