@@ -607,7 +607,9 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
         }
         // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
         // side by side, one head's rows are in few of the L2's channels.
-        const uint32_t rest = combo / a.kv_heads, chunk = rest % a.history_chunks, g = rest / a.history_chunks;
+        // From group to group the chunks do: where histories end at different lengths, the last chunks have little to do, and must not
+        // all be one XCD's (26 groups of 187 to 3,000 keys, two heads of 64, 4 chunks 50.6 -> 42.8 us, 8 chunks 51.7 -> 48.6).
+        const uint32_t rest = combo / a.kv_heads, g = rest / a.history_chunks, chunk = (rest + g) % a.history_chunks;
         it.head = (combo + rest) % a.kv_heads;
         const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
         const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
