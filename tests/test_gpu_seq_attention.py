@@ -215,6 +215,23 @@ def test_large_values_behind_growing_scores(H, K, new):
     p.check()
 
 
+@pytest.mark.parametrize("H,K,new", [(2, 2, 1), (4, 4, 20), (16, 1, 20)])
+def test_odd_queries_spoil_their_own_rows_only(H, K, new):
+    """Queries that are no numbers, or infinite: every score of theirs is NaN or infinite, their neighbours' are as ever."""
+    for odd in (math.nan, math.inf):
+        p = Problem(BF, 64, H, K, 16, [(700, 2)], [(new + 40, new), (new, new)], seed=6)
+        p.q[0, 1], p.q[new, 0, 7] = odd, odd
+        if new > 1:
+            p.q[new - 1, H - 1, 63] = odd
+        for offsets in ([0, 2], [0, 0]):               # with and without the history
+            p.group_offsets = torch.tensor(offsets, dtype=torch.int32)
+            out, lse = p.run()
+            want, want_lse, bound, lse_bound = p.want()
+            # where all scores are minus infinity the result is just 0, and its bound, of infinite scores, no number
+            R.close(out, want, torch.where(torch.isnan(bound), 0.0, bound))
+            R.close(lse, want_lse, torch.where(torch.isnan(lse_bound), 0.0, lse_bound))
+
+
 def test_histories_behind_four_gibibytes():
     """Blocks whose keys and values are more than 2^32 bytes from the first one."""
     K, D, block = 8, 128, 64
