@@ -178,9 +178,10 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  * Query head h reads key/value head h / (q_heads / kv_heads).  out receives the result in the queries'
  * type, lse [n_tokens][q_heads] fp32 (or NULL) the logarithm of the sum of exponentials.  A row that
  * attends to nothing, or whose scores are all minus infinity, gets 0, and minus infinity in lse.  Rows of
- * tokens behind the last request's are not written.  What lies in masked places (behind a length, behind a query's
- * own place) has no part in the result, whatever its value.  Sums, maxima and weights are in 32 bits; weights are rounded to the
- * values' type for the product with the values, whose sums are formed before they are divided by the weights' (values up to
+ * tokens in front of the first request's or behind the last one's are not written.  What lies in masked
+ * places (behind a length, behind a query's own place) has no part in the result, whatever its value.  Sums,
+ * maxima and weights are in 32 bits; weights are rounded to the values' type for the product with the
+ * values, whose sums are formed before they are divided by the weights' (values up to
  * 2^80 in size are safe, whatever the scores).
  *
  * max_new, max_group, max_len, max_prefix bound the new tokens of a request, the new tokens of a

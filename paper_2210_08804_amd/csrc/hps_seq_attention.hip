@@ -684,7 +684,8 @@ template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(k
     const uint32_t tid = threadIdx.x, r = tid / kPerRow, i = tid % kPerRow, x = i % kLanes, way = i / kLanes;
     const size_t rows = (size_t)a.n_tokens * a.q_heads, row = (size_t)blockIdx.x * kRows + r, near = row < rows ? row : rows - 1;
     const uint32_t t = (uint32_t)(near / a.q_heads), h = (uint32_t)(near - (size_t)t * a.q_heads);
-    const bool live = row < rows && (int32_t)t < scalar(a.token_offsets, a.n_requests);
+    // only rows of requests have parts of this call; others are not the call's to write
+    const bool live = row < rows && (int32_t)t >= scalar(a.token_offsets, 0) && (int32_t)t < scalar(a.token_offsets, a.n_requests);
     float ref = -kInf, sum = 0.f;
     constexpr uint32_t kEach = (kMaxParts + kPerRow - 1) / kPerRow;
     float2 ml[kEach > 4 ? 4 : kEach];

@@ -364,3 +364,28 @@ def test_graph_replays_on_new_lengths():
         call()
         assert torch.equal(got, out)                   # the same call gives the same bits
     B.hps_seq_attention_destroy(s)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+@pytest.mark.parametrize("prefix", [0, 90, 5000])
+def test_rows_in_front_of_the_first_request_are_left_alone(new, prefix):
+    """A batch in two calls over the same queries and outputs: the second one's offsets begin where the first one's end.  In between the
+    session serves another one."""
+    p = Problem(BF, 64, 4, 2, 16, [(prefix, 2), (prefix // 2, 3)], [(new, new), (40 + new, 1), (new, new), (70, 2), (3, 1)], tail=2, seed=new)
+    k, v = p.pages()
+    T, first = p.q.shape[0], 2
+    q, table, lens, offsets, ptable, plens = (x.cuda() for x in (p.q, p.block_table, p.lens, p.offsets, p.prefix_table, p.prefix_lens))
+    out, lse = torch.full((T, 4, 64), 9.0, dtype=BF, device="cuda"), torch.full((T, 4), 9.0, device="cuda")
+    s = B.hps_seq_attention_create(T * 4, 64)
+    for r, g, n in ((slice(0, first), slice(0, 1), 2), (slice(first, None), slice(1, None), 3)):
+        B.hps_seq_attention(s, q, k, v, table[r], lens[r], offsets[r.start:][:n + 1], out, prefix_table=ptable[g], prefix_lens=plens[g],
+                            group_offsets=torch.tensor([0, n], dtype=torch.int32, device="cuda"), lse=lse, **p.bounds)
+        B.hps_seq_attention(s, -2 * q, k, v, table, lens, offsets, torch.empty_like(q), prefix_table=ptable, prefix_lens=plens, group_offsets=p.group_offsets.cuda(), **p.bounds)
+    torch.cuda.synchronize()
+    assert B.hps_seq_attention_flags(s) == 0
+    B.hps_seq_attention_destroy(s)
+    want, want_lse, bound, lse_bound = p.want()
+    n = int(p.offsets[-1])
+    R.close(out[:n].cpu(), want[:n], bound[:n])
+    R.close(lse[:n].cpu(), want_lse[:n], lse_bound[:n])
+    assert (out[n:] == 9).all() and (lse[n:] == 9).all()
