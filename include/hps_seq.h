@@ -175,6 +175,8 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  *     group_offsets[g + 1] (groups are runs of requests; a request of no group has no history), and
  *   - the request's own tokens 0 .. lens[r] - n + i, listed in row r of block_table (its new tokens are the
  *     last n of them: append before attending).
+ * Offsets may go beyond n_tokens, as those of hps_seq_extend do beyond its max_tokens: the tokens there have no
+ * query and no row, and count among the n.
  * Query head h reads key/value head h / (q_heads / kv_heads).  out receives the result in the queries'
  * type, lse [n_tokens][q_heads] fp32 (or NULL) the logarithm of the sum of exponentials.  A row that
  * attends to nothing, or whose scores are all minus infinity, gets 0, and minus infinity in lse.  Rows of

@@ -648,7 +648,8 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
         const uint32_t len = length(a, scalar(a.lens, r), a.table_width, a.max_len);
         it.table = a.block_table + (size_t)r * a.table_width;
         it.first = chunk * a.own_chunk;
-        const int32_t from = (int32_t)len - (int32_t)n + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
+        // places by all of the request's new tokens: queries may end inside it
+        const int32_t from = (int32_t)len - (scalar(a.token_offsets, r + 1) - (int32_t)t0) + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
         it.causal_from = n > 1 ? from : kAll;
         it.end = min((uint32_t)max(last, 0), it.first + a.own_chunk);
         it.part = a.history_chunks + chunk;

@@ -389,3 +389,16 @@ def test_rows_in_front_of_the_first_request_are_left_alone(new, prefix):
     R.close(out[:n].cpu(), want[:n], bound[:n])
     R.close(lse[:n].cpu(), want_lse[:n], lse_bound[:n])
     assert (out[n:] == 9).all() and (lse[n:] == 9).all()
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_tokens_behind_the_last_query(new):
+    """Offsets may count more tokens than there are queries for: the others' places in their requests stay what they are."""
+    p = Problem(BF, 64, 4, 2, 16, [(40, 2)], [(new, new), (50 + new, 2 * new)], seed=new)
+    want, want_lse, bound, lse_bound = p.want()
+    T = new + max(1, new // 2)
+    p.q = p.q[:T]
+    out, lse = p.run()
+    assert p.flags == 0
+    R.close(out, want[:T], bound[:T])
+    R.close(lse, want_lse[:T], lse_bound[:T])
