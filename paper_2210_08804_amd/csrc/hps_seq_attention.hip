@@ -499,7 +499,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 typedef T t4 __attribute__((ext_vector_type(4)));
                 t4 y;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = (T)(x[j] * f);
+                for (int j = 0; j < 4; ++j) y[j] = f == 0.f ? (T)0.f : (T)(x[j] * f);      // nothing attended: 0, though weights of 0 met values that are not finite
                 *(t4 *)(to + dim * 2) = y;
             } else {
                 *(f32x4 *)(to + dim * 4) = x;

@@ -402,3 +402,17 @@ def test_tokens_behind_the_last_query(new):
     assert p.flags == 0
     R.close(out, want[:T], bound[:T])
     R.close(lse, want_lse[:T], lse_bound[:T])
+
+
+@pytest.mark.parametrize("H,K,requests", [(4, 2, [(5, 1), (40, 2)]), (16, 1, [(60, 9), (9, 9)]), (2, 2, [(33, 1)] * 300), (2, 2, [(700, 1), (2000, 2)])])
+def test_scores_of_minus_infinity_and_infinite_values(H, K, requests):
+    """Rows whose scores are all minus infinity get 0, whatever the values and however the keys are cut."""
+    for groups in ([], [(100, len(requests))]):
+        p = Problem(BF, 64, H, K, 16, groups, requests)
+        p.q[:] = 1
+        for t, n in [(p.block_table[r], int(n)) for r, n in enumerate(p.lens)] + [(p.prefix_table[g], int(n)) for g, n in enumerate(p.prefix_lens)]:
+            place = torch.arange(n)
+            p.k[t.long()[place // 16], place % 16] = -torch.finfo(BF).max
+            p.v[t.long()[place // 16], place % 16] = math.inf
+        out, lse = p.run()
+        assert (out == 0).all() and (lse == -math.inf).all()
