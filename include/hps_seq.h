@@ -183,8 +183,9 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  * tokens in front of the first request's or behind the last one's are not written.  What lies in masked
  * places (behind a length, behind a query's own place) has no part in the result, whatever its value.  Sums,
  * maxima and weights are in 32 bits; weights are rounded to the values' type for the product with the
- * values, whose sums are formed before they are divided by the weights' (values up to
- * 2^80 in size are safe, whatever the scores).
+ * values (f16 has no more than 11 bits of those above 2^-22 of a row's largest, fewer below, and none below
+ * 2^-33), whose sums are formed before they are divided by the weights' (values up to 2^80 in size are
+ * safe, whatever the scores).
  *
  * max_new, max_group, max_len, max_prefix bound the new tokens of a request, the new tokens of a
  * group, lens and prefix_lens: the host sizes the launch by them (the device reads the lengths

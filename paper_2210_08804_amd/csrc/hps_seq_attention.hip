@@ -39,9 +39,12 @@ constexpr float kInf = __builtin_inff();
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr uint32_t kWideRows = 128, kNarrowRows = 32;  // rows of a work-group
 constexpr uint32_t kWideKeys = 64, kNarrowKeys = 32;   // keys of a step: of the work-group, of a wave
-// A row's reference m need not be its maximum: it moves when a score is kSlack ahead (in powers of two), or 16 weights of
-// a lane sum to kMost, far within both types' range.  Most steps need no rescaling then; precision is relative and the same.
-constexpr float kSlack = 8.f, kMost = 0x1p12f;
+// A row's reference m need not be its maximum.  Where it moves it goes to kBelow below the largest score (in powers of two), and it
+// moves when a score is kSlack ahead of it, or 16 weights of a lane sum to kMost, far within the type's range: most steps need
+// no rescaling then.  bf16 has the exponents of 32 bits, so its weights lose the same few bits wherever the reference is.  f16 has
+// none below 2^-14 and loses weights of 2^-25 whole, which a long history has many of behind one large weight: its reference stays 8
+// below the largest score, which leaves weights of 2^-22 of the largest their bits (15,000 keys of which 31 in 32 have a weight of
+// 2^-26: with the largest score for a reference all of those were lost, now they are 1 % off at most).
 
 struct Args {
     const char *q, *k, *v;
@@ -66,11 +69,13 @@ template <> struct Type<__bf16> {
     typedef bf16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7F80u;
+    static constexpr float kBelow = 0.f, kSlack = 8.f, kMost = 0x1p12f;
 };
 template <> struct Type<_Float16> {
     typedef f16x8 frag;
     static __device__ __forceinline__ f32x16 mfma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExp = 0x7C00u;
+    static constexpr float kBelow = 8.f, kSlack = 15.f, kMost = 0x1p15f;    // weights stay below 2^15, f16 ends at 2^16
 };
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -246,9 +251,9 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         return both_max(top) * a.c;
     }
-    // Moves the reference to the largest score so far, and what was summed with it.
+    // Moves the reference to the largest score so far (or kBelow below it), and what was summed with it.
     __device__ __forceinline__ void move(float top) {
-        const float next = fmaxf(m, top), ref = next == -kInf ? 0.f : next, f = exp2_(m - ref);
+        const float next = fmaxf(m, top - Type<T>::kBelow), ref = next == -kInf ? 0.f : next, f = exp2_(m - ref);
         l *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
@@ -380,7 +385,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 if (at + 64 > least) break;
                 t = scores<0>();
                 float sum = weights(s, w, m);       // infinite, or NaN, the first time: m is -inf
-                if (__ballot(!(sum < kMost))) {
+                if (__ballot(!(sum < Type<T>::kMost))) {
                     ahead = true;
                     break;
                 }
@@ -388,7 +393,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 add_values<kWideValues>(w);
                 s = scores<32 * kRow>();
                 sum = weights(t, w, m);
-                if (__ballot(!(sum < kMost))) {
+                if (__ballot(!(sum < Type<T>::kMost))) {
                     ahead = true;
                     left = 1;
                     const f32x16 x = s;
@@ -418,7 +423,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
         uint32_t seen = 0xFFFFu;
         if (hidden) seen = hide(s, at);
         const float top = largest(s);
-        if (__ballot(top > m + kSlack)) move(top);
+        if (__ballot(top > m + Type<T>::kSlack)) move(top);
         l += weights(s, w, reference());
         if (hidden && it.causal_from != kAll) add_values_hidden<kAt>(w, seen);
         else add_values<kAt>(w);
@@ -467,7 +472,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
                 full = at + 32 <= least;
                 if (!full) break;
                 top = largest(s);
-                if (__ballot(top > m + kSlack)) break;                      // also the first time: m is -inf
+                if (__ballot(top > m + Type<T>::kSlack)) break;                      // also the first time: m is -inf
                 l += weights(s, w, reference());
                 wait_values();
                 add_values<kNarrowValues>(w);

@@ -416,3 +416,25 @@ def test_scores_of_minus_infinity_and_infinite_values(H, K, requests):
             p.v[t.long()[place // 16], place % 16] = math.inf
         out, lse = p.run()
         assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("H,K,new", [(1, 1, 1), (16, 1, 3)])
+@pytest.mark.parametrize("shared", [True, False])
+def test_small_weights_beside_large_ones(H, K, new, shared, dtype):
+    """A key of weight 1 and 31 of weight 2^-26, over and over: small weights are not lost where they are rounded for the product."""
+    n = 15000
+    p = Problem(dtype, 64, H, K, 16, [(n, 1)] if shared else [], [(new if shared else n + new, new)], seed=8, scale=1.0)
+    p.q[:], p.k[:], p.v[:] = 1, -18 / 64, p.v.nan_to_num().abs() * 1024
+    first = p.prefix_table[0, :n // 16:2] if shared else p.block_table[0, :n // 16:2]
+    p.k[first.long(), 0], p.v[first.long(), 0] = 0, 0
+    out, lse = p.run()
+    want, want_lse, _, lse_bound = p.want()
+    # every weight is rounded relative to itself, and f16's to steps of 2^-32 of the largest (2^-24 where that is 2^8 at least); the result to its
+    # type; scores and sums as ever
+    e = 18 * 72 * 2.0 ** -24 + 2.0 ** -21
+    steps = (n + new) * 2.0 ** -33 * float(p.v.abs().max()) / len(first) if dtype is HF else 0
+    bound = 2.02 * R.ROUND[dtype] * want + want * (2 * e + (n + 64) * 2.0 ** -24) + steps + R.TINY[dtype]
+    assert 4 * float(bound.max()) < float(want.min())
+    R.close(out, want, bound)
+    R.close(lse, want_lse, lse_bound)
