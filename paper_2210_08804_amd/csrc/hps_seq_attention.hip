@@ -770,6 +770,17 @@ template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(k
     if (a.lse && i == 0) a.lse[row] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
+// Where a bound of 0 keeps all histories out of the launch: whether there are any all the same.
+__global__ void __launch_bounds__(kThreads) check_kernel(const Args a) {
+    const uint32_t g = blockIdx.x * kThreads + threadIdx.x;
+    if (g >= a.n_groups) return;
+    const uint32_t r0 = clamp_to(a.group_offsets[g], a.n_requests), r1 = clamp_to(a.group_offsets[g + 1], a.n_requests);
+    const uint32_t t0 = clamp_to(a.token_offsets[r0], a.n_tokens), t1 = clamp_to(a.token_offsets[r1], a.n_tokens);
+    if (t1 <= t0) return;
+    if (t1 - t0 > a.max_group) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+    length(a, a.prefix_lens[g], a.prefix_width, a.max_prefix);
+}
+
 __global__ void clear_kernel(uint32_t *p) { *p = 0u; }
 
 // ---- host ---------------------------------------------------------------------------------
@@ -1042,6 +1053,10 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     a.direct = parts == 1;
     const uint32_t groups = (uint32_t)(history_groups + own_groups);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (r.n_groups && !history_groups) {
+        hipLaunchKernelGGL(check_kernel, dim3(div_up(r.n_groups, kThreads)), dim3(kThreads), 0, st, a);
+        SEQ_TRY(hipGetLastError());
+    }
     SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, groups, parts, st) : launch<__bf16>(a, groups, parts, st));
     return HPS_OK;
 }

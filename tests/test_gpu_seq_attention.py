@@ -438,3 +438,24 @@ def test_small_weights_beside_large_ones(H, K, new, shared, dtype):
     assert 4 * float(bound.max()) < float(want.min())
     R.close(out, want, bound)
     R.close(lse, want_lse, lse_bound)
+
+
+def test_lengths_are_checked_where_no_history_is_attended():
+    """A bound of 0 leaves the histories out of the launch, and tells where there are any all the same."""
+    p = Problem(BF, 64, 4, 2, 16, [(100, 2), (3, 1)], [(5, 1), (40, 2), (1, 1)])
+    good = dict(max_new=2, max_len=40, max_prefix=100, max_group=3)
+    for bad in (dict(max_prefix=0), dict(max_group=0), dict(max_prefix=0, max_group=0)):
+        p.bounds = {**good, **bad}
+        p.run()
+        assert p.flags == B.HPS_SEQ_FLAG_LENGTH, bad
+    p.group_offsets = torch.tensor([0, 0, 0], dtype=torch.int32)             # histories of nobody: no new tokens to a group
+    p.bounds = {**good, "max_group": 0}
+    p.check()
+    p = Problem(BF, 64, 4, 2, 16, [(0, 2), (0, 1)], [(5, 1), (40, 2), (1, 1)], loose=1)
+    p.check()                                          # histories of no tokens, bounded by 0: nothing to tell
+    groups = 1500                                      # more groups than work-groups
+    p = Problem(BF, 64, 1, 1, 16, [(0, 0)] * groups + [(0, 1)], [(5, 1)], loose=1)
+    p.check()
+    p.prefix_lens[groups] = 1
+    p.run()
+    assert p.flags == B.HPS_SEQ_FLAG_LENGTH
