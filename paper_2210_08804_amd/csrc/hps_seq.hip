@@ -347,6 +347,7 @@ struct RopeArgs {
     uint32_t heads[3], n_heads;                                         // of each, of all
     uint32_t head_dim, half, max_pos;                                   // half = rot_dim / 2
     uint32_t spans, per_pass, n_slots, sh;                              // spans: pairs of vectors of a head; per_pass: heads side by side
+    uint32_t first_token;                                               // of this launch
     int32_t interleaved;
     float sign;
 };
@@ -368,7 +369,7 @@ template <typename T> __device__ __forceinline__ void turn(T &a, T &b, float c, 
 template <typename T, int E, bool kPages>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
     typedef Vec<T, E> V;
-    const uint32_t t = blockIdx.x, tid = threadIdx.x;
+    const uint32_t t = a.first_token + blockIdx.x, tid = threadIdx.x;
     const uint32_t lane_head = tid / a.spans, s = tid - lane_head * a.spans;
     if (lane_head >= a.per_pass) return;
     const bool turns = a.table != nullptr;
@@ -463,9 +464,11 @@ hipError_t launch_rope(RopeArgs &a, uint32_t n_tokens, uint32_t rot_dim, hipStre
     uint32_t threads = (a.n_heads * a.spans + 63) / 64 * 64;
     if (threads > 256) threads = 256;
     a.per_pass = threads / a.spans;
-    if (whole) hipLaunchKernelGGL((rope_kernel<T, E, kPages>), dim3(n_tokens), dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL((rope_kernel<T, 1, kPages>), dim3(n_tokens), dim3(threads), 0, st, a);
-    return hipGetLastError();
+    return seq_launches(n_tokens, [&](uint32_t first, uint32_t n) {
+        a.first_token = first;
+        if (whole) hipLaunchKernelGGL((rope_kernel<T, E, kPages>), dim3(n), dim3(threads), 0, st, a);
+        else hipLaunchKernelGGL((rope_kernel<T, 1, kPages>), dim3(n), dim3(threads), 0, st, a);
+    });
 }
 
 template <bool kPages> hipError_t launch_rope(RopeArgs &a, int dtype, uint32_t n_tokens, uint32_t rot_dim, hipStream_t st) {

@@ -59,6 +59,7 @@ struct Args {
     uint32_t q_heads, kv_heads, ratio, head_dim, n_blocks, sh;
     uint32_t history_groups, history_tiles, history_chunks, history_chunk, history_combos; // work-groups; row tiles; chunks, keys of one; (group, chunk, head)
     uint32_t own_tiles, own_chunks, own_chunk, own_items;
+    uint32_t first_group;                              // of this launch
     int32_t history_wide, own_mode, direct;            // direct: one part only, results go straight out
     float c;                                           // scale * log2(e)
 };
@@ -596,19 +597,20 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
         for (uint32_t x = threadIdx.x * 16; x < E::kLds; x += kThreads * 16) *(u32x4 *)(shared + x) = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
+    const uint32_t group = a.first_group + blockIdx.x;
     Item it;
     bool is_wide, solo = false;
-    if (blockIdx.x < a.history_groups) {
+    if (group < a.history_groups) {
         // Work-groups of one (group, chunk, head) read the same keys: they go to one XCD (workgroups are dealt to the eight in turn).
         uint32_t combo, tile;
         if (a.history_combos >= 8) {
-            const uint32_t y = blockIdx.x >> 3;
-            combo = (blockIdx.x & 7u) + 8 * (y / a.history_tiles);
+            const uint32_t y = group >> 3;
+            combo = (group & 7u) + 8 * (y / a.history_tiles);
             tile = y % a.history_tiles;
             if (combo >= a.history_combos) return;
         } else {
-            combo = blockIdx.x % a.history_combos;
-            tile = blockIdx.x / a.history_combos;
+            combo = group % a.history_combos;
+            tile = group / a.history_combos;
         }
         // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
         // side by side, one head's rows are in few of the L2's channels.
@@ -631,7 +633,7 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
         it.causal_from = kAll;
         it.part = chunk;
     } else {
-        uint32_t x = blockIdx.x - a.history_groups;
+        uint32_t x = group - a.history_groups;
         is_wide = a.own_mode == kOwnWide;
         solo = a.own_mode == kOwnSolo;
         if (solo) {
@@ -683,12 +685,12 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
 // reading the parts (16,384 rows of 5 parts of 128 values: 10 us, 4.2 TB/s).  Done in the launch in front, by the work-group that ends
 // last, it costs more: with the fences that its reading needs 8 candidates behind 500 keys take 24 us instead of 14.
 constexpr int kJoin = 256, kMaxParts = 1024;
-template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kJoin) join_kernel(const Args a, uint32_t parts) {
+template <typename T, int kLanes, int kWays> __global__ void __launch_bounds__(kJoin) join_kernel(const Args a, uint32_t parts, uint32_t first_group) {
     constexpr uint32_t kRows = kJoin / (kLanes * kWays), kPerRow = kJoin / kRows;
     extern __shared__ __align__(16) char shared[];
     float *l_share = (float *)shared;                  // [kRows][parts]
     const uint32_t tid = threadIdx.x, r = tid / kPerRow, i = tid % kPerRow, x = i % kLanes, way = i / kLanes;
-    const size_t rows = (size_t)a.n_tokens * a.q_heads, row = (size_t)blockIdx.x * kRows + r, near = row < rows ? row : rows - 1;
+    const size_t rows = (size_t)a.n_tokens * a.q_heads, row = ((size_t)first_group + blockIdx.x) * kRows + r, near = row < rows ? row : rows - 1;
     const uint32_t t = (uint32_t)(near / a.q_heads), h = (uint32_t)(near - (size_t)t * a.q_heads);
     // only rows of requests have parts of this call; others are not the call's to write
     const bool live = row < rows && (int32_t)t >= scalar(a.token_offsets, 0) && (int32_t)t < scalar(a.token_offsets, a.n_requests);
@@ -840,28 +842,30 @@ template <typename T> hipError_t allow_lds() {
     return allow_lds<T, 8>();
 }
 
-template <typename T, int DT, bool kExact> hipError_t launch_attend(const Args &a, uint32_t groups, hipStream_t st) {
-    hipLaunchKernelGGL((attend_kernel<T, DT, kExact>), dim3(groups), dim3(kThreads), (kAttendLds<T, DT, kExact>), st, a);
-    return hipGetLastError();
+template <typename T, int DT, bool kExact> hipError_t launch_attend(Args &a, uint32_t groups, hipStream_t st) {
+    return seq_launches(groups, [&](uint32_t first, uint32_t n) {
+        a.first_group = first;
+        hipLaunchKernelGGL((attend_kernel<T, DT, kExact>), dim3(n), dim3(kThreads), (kAttendLds<T, DT, kExact>), st, a);
+    });
 }
 
-template <typename T, int DT> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
+template <typename T, int DT> hipError_t launch(Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
     if (hipError_t e = a.head_dim == 32 * DT ? launch_attend<T, DT, true>(a, groups, st) : launch_attend<T, DT, false>(a, groups, st)) return e;
     if (a.direct) return hipSuccess;
     constexpr int kLanes = DT == 1 ? 8 : DT == 2 ? 16 : DT <= 4 ? 32 : 64;
     const size_t rows = (size_t)a.n_tokens * a.q_heads;
     auto join = [&](auto ways) {
         constexpr int kWays = decltype(ways)::value, kRows = kJoin / (kLanes * kWays);
-        hipLaunchKernelGGL((join_kernel<T, kLanes, kWays>), dim3(div_up(rows, kRows)), dim3(kJoin), kRows * parts * sizeof(float), st, a, parts);
+        return seq_launches(div_up(rows, kRows), [&](uint32_t first, uint32_t n) {
+            hipLaunchKernelGGL((join_kernel<T, kLanes, kWays>), dim3(n), dim3(kJoin), kRows * parts * sizeof(float), st, a, parts, first);
+        });
     };
     // Few rows: all lanes of a work-group to one, which read its parts side by side (a row each / several rows each, us of a whole
     // call, 16 heads of 128: 1 token behind 1,000 keys 13.0 / 13.8, 4 behind 32,768 21.6 / 36.6, 64 37.0 / 45.1, 256 behind 1,000 25.1 / 22.3).
-    if (rows * kLanes <= 65536) join(std::integral_constant<int, kJoin / kLanes>());
-    else join(std::integral_constant<int, 1>());
-    return hipGetLastError();
+    return rows * kLanes <= 65536 ? join(std::integral_constant<int, kJoin / kLanes>()) : join(std::integral_constant<int, 1>());
 }
 
-template <typename T> hipError_t launch(const Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
+template <typename T> hipError_t launch(Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {
     if (a.head_dim <= 32) return launch<T, 1>(a, groups, parts, st);
     if (a.head_dim <= 64) return launch<T, 2>(a, groups, parts, st);
     if (a.head_dim <= 96) return launch<T, 3>(a, groups, parts, st);

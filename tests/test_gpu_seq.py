@@ -313,3 +313,29 @@ def test_a_graph_of_a_step_is_replayed_on_new_lengths():
         for s, ts in seen.items():
             if s >= 0 and len(ts) == 1:
                 assert torch.equal(got[s], kv[ts[0], K:].cpu())
+
+
+@pytest.mark.parametrize("pages", [False, True])
+def test_more_tokens_than_one_launch_takes(pages):
+    """2^24 tokens of 256 threads each: 2^32 threads.  All but a few tokens are passed over."""
+    T, H, D = (1 << 24) + 5, 256 if not pages else 252, 2
+    torch.cuda.empty_cache()
+    at = torch.tensor([0, 77, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, (1 << 24) - 1, 1 << 24, T - 1])
+    g = torch.Generator().manual_seed(3)
+    x, positions, table = torch.randn(len(at), H, D, generator=g).half(), torch.randint(0, 50, (len(at),), generator=g).int(), cos_sin(50, D)
+    rows, every = torch.empty(T, H, D, dtype=torch.float16, device="cuda"), i32(T, fill=-1)
+    rows[at.cuda()], every[at.cuda()] = x.cuda(), positions.cuda()
+    want, _ = R.rope(x, positions, table, False, False)
+    if pages:
+        kv = torch.randn(T, 2, 1, D, device="cuda").half()
+        kp, vp = torch.zeros(1, 16, 1, D, device="cuda").half(), torch.zeros(1, 16, 1, D, device="cuda").half()
+        slots = i32(T, fill=-1)
+        slots[at.cuda()] = torch.arange(len(at), dtype=torch.int32, device="cuda") + 3
+        B.hps_seq_append(kv[:, 0], kv[:, 1], kp, vp, slots, q=rows, q_out=rows, positions=every, table=table.cuda())
+        k = kv[at.cuda(), 0].cpu()
+        want_k, _ = R.rope(k, positions, table, False, False)
+        R.close(kp[0, 3:3 + len(at)].cpu(), want_k, R.rope_bound(k, want_k, torch.float16))
+        assert torch.equal(vp[0, 3:3 + len(at)], kv[at.cuda(), 1])
+    else:
+        B.hps_seq_rope(rows, rows, every, table.cuda())
+    R.close(rows[at.cuda()].cpu(), want, R.rope_bound(x, want, torch.float16))

@@ -459,3 +459,47 @@ def test_lengths_are_checked_where_no_history_is_attended():
     p.prefix_lens[groups] = 1
     p.run()
     assert p.flags == B.HPS_SEQ_FLAG_LENGTH
+
+
+def test_more_work_groups_than_one_launch_takes():
+    """Many requests of a token each with the bounds that the shapes give: 2^24 tiles, as many as a launch has no room for."""
+    n, H, K, D, L, block = 8192, 32, 8, 64, 3, 4
+    g = torch.Generator(device="cuda").manual_seed(1)
+    normal = lambda *s: torch.randn(*s, device="cuda", generator=g).to(BF)  # noqa: E731
+    q, k, v = normal(n, H, D), normal(n, block, K, D), normal(n, block, K, D)
+    table = torch.randperm(n, device="cuda", generator=g).int().view(n, 1)
+    lens, offsets = torch.full((n,), L, dtype=torch.int32, device="cuda"), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    out, s = torch.full_like(q, 9), B.hps_seq_attention_create(n * H, D)
+    B.hps_seq_attention(s, q, k, v, table, lens, offsets, out)
+    torch.cuda.synchronize()
+    assert B.hps_seq_attention_flags(s) == 0
+    B.hps_seq_attention_destroy(s)
+    kk, vv = (x[table[:, 0].long(), :L].double().permute(0, 2, 1, 3)[:, :, None] for x in (k, v))          # [n, K, 1, L, D]
+    qq = q.double().view(n, K, H // K, 1, D)
+    p = ((qq * kk).sum(-1) * D ** -0.5).softmax(-1)[..., None]
+    want, mass = ((p * x).sum(-2).view(n, H, D) for x in (vv, vv.abs()))
+    # scores of 64 products of values up to 6 in 32 bits, weights and results rounded to the type
+    e = 64 * 36 * D ** -0.5 * (D + 8) * 2.0 ** -24 + 2.0 ** -21
+    R.close(out.cpu(), want.cpu(), (R.ROUND[BF] * 1.01 * (want.abs() + mass) + mass * (2 * e + (L + 64) * 2.0 ** -24) + 1e-30).cpu())
+
+
+def test_more_rows_than_one_join_takes():
+    """2^29 rows, of which one request has 65,536: the others are left alone."""
+    T, H, D, block = 8193, 65536, 8, 2
+    torch.cuda.empty_cache()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn(3, block, H, D, device="cuda", generator=g).half() for _ in range(2))
+    q, out = torch.empty(T, H, D, dtype=HF, device="cuda"), torch.empty(T, H, D, dtype=HF, device="cuda").fill_(9)
+    q[:1] = torch.randn(1, H, D, device="cuda", generator=g)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    s = B.hps_seq_attention_create(T * H, D)
+    B.hps_seq_attention(s, q, k, v, i32(0).view(1, 1), i32(1), i32(0, 1), out, prefix_table=i32(2, 1).view(1, 2), prefix_lens=i32(3), group_offsets=i32(0, 1), max_new=1, max_group=1)
+    torch.cuda.synchronize()
+    assert B.hps_seq_attention_flags(s) == 0
+    B.hps_seq_attention_destroy(s)
+    assert all(bool((x == 9).all()) for x in out[1:].split(512))
+    kk, vv = (torch.stack((x[2, 0], x[2, 1], x[1, 0], x[0, 0]), 1).double() for x in (k, v))        # [H, 4, D]
+    p = ((q[0].double()[:, None] * kk).sum(-1) * D ** -0.5).softmax(-1)[..., None]
+    want, mass = (p * vv).sum(1), (p * vv.abs()).sum(1)
+    e = 8 * 36 * D ** -0.5 * (D + 8) * 2.0 ** -24 + 2.0 ** -21
+    R.close(out[0].cpu(), want.cpu(), (R.ROUND[HF] * 1.01 * (want.abs() + mass) + mass * (2 * e + 68 * 2.0 ** -24) + 4 * R.TINY[HF] * vv.abs().amax(1) + R.TINY[HF]).cpu())
