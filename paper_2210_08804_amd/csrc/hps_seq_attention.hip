@@ -862,7 +862,8 @@ template <typename T, int DT> hipError_t launch(Args &a, uint32_t groups, uint32
     };
     // Few rows: all lanes of a work-group to one, which read its parts side by side (a row each / several rows each, us of a whole
     // call, 16 heads of 128: 1 token behind 1,000 keys 13.0 / 13.8, 4 behind 32,768 21.6 / 36.6, 64 37.0 / 45.1, 256 behind 1,000 25.1 / 22.3).
-    return rows * kLanes <= 65536 ? join(std::integral_constant<int, kJoin / kLanes>()) : join(std::integral_constant<int, 1>());
+    // Many parts too: a launch has 64 KiB of LDS unasked, and several rows of heads up to 32 would want more beyond 512.
+    return rows * kLanes <= 65536 || kJoin / kLanes * parts * sizeof(float) > 65536 - 512 ? join(std::integral_constant<int, kJoin / kLanes>()) : join(std::integral_constant<int, 1>());
 }
 
 template <typename T> hipError_t launch(Args &a, uint32_t groups, uint32_t parts, hipStream_t st) {

@@ -503,3 +503,13 @@ def test_more_rows_than_one_join_takes():
     want, mass = (p * vv).sum(1), (p * vv.abs()).sum(1)
     e = 8 * 36 * D ** -0.5 * (D + 8) * 2.0 ** -24 + 2.0 ** -21
     R.close(out[0].cpu(), want.cpu(), (R.ROUND[HF] * 1.01 * (want.abs() + mass) + mass * (2 * e + 68 * 2.0 ** -24) + 4 * R.TINY[HF] * vv.abs().amax(1) + R.TINY[HF]).cpu())
+
+
+def test_many_parts_of_many_rows():
+    """Over 512 parts, of more rows than a work-group each: what the join keeps of them in LDS."""
+    T, D, block, n = 8200, 8, 1024, 1 << 20
+    p = Problem(HF, D, 1, 1, block, [(n, 1)], [(n, 1)], tail=T - 1)
+    p.bounds["max_group"] = 1
+    s = B.hps_seq_attention_create(2_000_000, D)       # a session for larger calls: room for parts
+    p.check(session=s)
+    B.hps_seq_attention_destroy(s)
