@@ -96,10 +96,14 @@ __device__ __forceinline__ float both_sum(float x) {
 // lanes that are switched off leave their place in LDS alone.  (Not the builtin: the compiler then waits for every such
 // load in front of any read of LDS, and the next step's loads are what is to stay in flight.)
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    uint32_t kept;                                     // m0 is the compiler's: it gets it back (which costs no time beside the load)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(to), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    uint32_t kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(to), "v"(from) : "memory");
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
