@@ -626,6 +626,8 @@ def hps_seq_rope(q, q_out, positions, table, k=None, k_out=None, interleaved=Fal
     address, n, rot = _rope_table_of(table)
     none, hk = (0, 0, 0), 0
     if k is not None:
+        if k_out is None:
+            raise ValueError("k_out: needed with k")
         hk = k.shape[1]
         k_shape = (T, hk, D)
     args = _SEQ_ROPE.pack(
@@ -645,6 +647,8 @@ def hps_seq_append(k, v, k_pages, v_pages, slots, q=None, q_out=None, positions=
     address, n, rot = _rope_table_of(table)
     none, H = (0, 0, 0), 0
     if q is not None:
+        if q_out is None:
+            raise ValueError("q_out: needed with q")
         H = q.shape[1]
         shape = (T, H, D)
     pages = _pages(k_pages, v_pages, dtype)

@@ -122,3 +122,12 @@ def test_the_binding_refuses_what_it_cannot_describe():
         B.hps_seq_attention(None, x, x.view(1, 4, 2, 64), x.view(1, 4, 2, 64), i.view(4, 1), i, torch.zeros(5, dtype=torch.int32), x)
     with pytest.raises(ValueError, match="requests, width"):
         B.hps_seq_extend(i, i, 16, i, i, i, torch.zeros(5, dtype=torch.int32), i, i, i, i)
+
+
+def test_outputs_that_are_missing_are_named():
+    x, i = torch.zeros(4, 2, 64), torch.zeros(4, dtype=torch.int32)
+    pages = x.view(1, 4, 2, 64)
+    with pytest.raises(ValueError, match="k_out: needed with k"):
+        B.hps_seq_rope(x, x, i, None, k=x)
+    with pytest.raises(ValueError, match="q_out: needed with q"):
+        B.hps_seq_append(x, x, pages, pages, i, q=x)
