@@ -62,7 +62,10 @@ extern "C" {
  * The new n_free is info[0], so a call may be given the previous call's info as n_free (another array
  * than its own info).  Lacking blocks: the table entry is -1 and so are the slots of its tokens.  A
  * request holds at most table_width * block_size tokens: total_lens stops there and slots are -1
- * beyond.  Tokens beyond max_tokens are counted, and not written.  Sums stop at 2^31 - 1.
+ * beyond.  (hps_seq_attention takes a request's new tokens for the last of its length, so where tokens did not fit -
+ * info[3] != 0, total_lens[r] < past + new - all rows of that request's new tokens are undefined in it, those of
+ * tokens that did fit among them.  Other requests are as ever.)  Tokens beyond max_tokens are counted, and not
+ * written.  Sums stop at 2^31 - 1.
  * n_requests == 0 is allowed.
  */
 typedef struct {
@@ -174,7 +177,7 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  *   - the prefix_lens[g] tokens listed in row g of prefix_table, if group_offsets[g] <= r <
  *     group_offsets[g + 1] (groups are runs of requests; a request of no group has no history), and
  *   - the request's own tokens 0 .. lens[r] - n + i, listed in row r of block_table (its new tokens are the
- *     last n of them: append before attending).
+ *     last n of them: append before attending; a length that hps_seq_extend had to cut does not fit this).
  * Offsets may go beyond n_tokens, as those of hps_seq_extend do beyond its max_tokens: the tokens there have no
  * query and no row, and count among the n.
  * Query head h reads key/value head h / (q_heads / kv_heads).  out receives the result in the queries'
@@ -183,8 +186,8 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  * tokens in front of the first request's or behind the last one's are not written.  What lies in masked
  * places (behind a length, behind a query's own place) has no part in the result, whatever its value.  Sums,
  * maxima and weights are in 32 bits; weights are rounded to the values' type for the product with the
- * values (f16 has no more than 11 bits of those above 2^-22 of a row's largest, fewer below, and none below
- * 2^-33), whose sums are formed before they are divided by the weights' (values up to 2^80 in size are
+ * values (in f16 those above 2^-22 of a row's largest keep 11 bits, smaller ones fewer, and those below 2^-33
+ * none), whose sums are formed before they are divided by the weights' (values up to 2^80 in size are
  * safe, whatever the scores).
  *
  * max_new, max_group, max_len, max_prefix bound the new tokens of a request, the new tokens of a

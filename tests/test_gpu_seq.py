@@ -339,3 +339,33 @@ def test_more_tokens_than_one_launch_takes(pages):
     else:
         B.hps_seq_rope(rows, rows, every, table.cuda())
     R.close(rows[at.cuda()].cpu(), want, R.rope_bound(x, want, torch.float16))
+
+
+def test_a_request_that_outgrows_its_table_spoils_no_other():
+    """Steps of a request whose table becomes full, and is too short then, between two others: extend, append, attention."""
+    block, width, H, K, D, dtype = 4, 3, 4, 2, 64, torch.bfloat16
+    g = torch.Generator().manual_seed(9)
+    pages = [torch.zeros(20, block, K, D, dtype=dtype, device="cuda") for _ in range(2)]
+    free, info, lens = torch.randperm(20, generator=g).int().cuda(), i32(4, fill=20), i32(3, fill=0)
+    table, s = i32(3, width, fill=-1), B.hps_seq_attention_create(64, D)
+    seen = [[] for _ in range(3)]
+    for new, fits in (([2, 7, 1], True), ([3, 5, 4], True), ([1, 3, 2], False)):     # the second one has 7, 12, 15 of 12
+        T = sum(new)
+        offsets, other, slots, positions, after = i32(4), i32(3), i32(T), i32(T), i32(4)
+        B.hps_seq_extend(lens, i32(3).copy_(torch.tensor(new)), block, free, info[:1], table, offsets, other, slots, positions, after)
+        lens, info = other, after
+        x = torch.randn(T, H + 2 * K, D, generator=g).to(dtype)
+        d, at = x.cuda(), [0, *np.cumsum(new)]
+        out = torch.full((T, H, D), 9.0, dtype=dtype, device="cuda")
+        B.hps_seq_append(d[:, H:H + K], d[:, H + K:], *pages, slots)
+        B.hps_seq_attention(s, d[:, :H].contiguous(), *pages, table, lens, offsets, out)
+        assert int(info[3]) == (0 if fits else 3) and B.hps_seq_attention_flags(s) == 0
+        for r in range(3):
+            seen[r].append(x[at[r]:at[r + 1], H:])
+            if r == 1 and not fits:
+                continue
+            kv = torch.cat(seen[r])
+            n = kv.shape[0]
+            want, _, bound, _ = R.attention(x[at[r]:at[r + 1], :H], kv[None, :, :K], kv[None, :, K:], torch.zeros(1, 1, dtype=torch.int32), [n], [0, new[r]], D ** -0.5)
+            R.close(out[at[r]:at[r + 1]].cpu(), want, bound)
+    B.hps_seq_attention_destroy(s)
