@@ -192,9 +192,12 @@ hps_status_t hps_seq_attention_destroy(hps_seq_attention_t *s);
  *
  * max_new, max_group, max_len, max_prefix bound the new tokens of a request, the new tokens of a
  * group, lens and prefix_lens: the host sizes the launch by them (the device reads the lengths
- * themselves).  A longer one raises HPS_SEQ_FLAG_LENGTH and the rows concerned are undefined, and so does a
+ * themselves), so bounds near the lengths pay: work-groups without rows come and go, but there are n_requests times
+ * as many as max_new would fill (512 requests of a token, 32 / 8 heads: 18 us with max_new 1, 204 with 512; 8,192 requests
+ * 163 us with 1, 18 ms with 8,192).  A longer one raises HPS_SEQ_FLAG_LENGTH and the rows concerned are undefined, and so does a
  * length that its table does not hold; a block number outside 0 .. n_blocks - 1 within a length raises
  * HPS_SEQ_FLAG_BLOCK and stands for a block of zeros.
+ * Blocks of 16 tokens and more are read two to five times as fast as smaller ones.
  * dtype HPS_SEQ_F16 or HPS_SEQ_BF16; head_dim a multiple of 8 up to 256; q_heads a multiple of
  * kv_heads; all data and strides multiples of 16 bytes, the pages' not negative; scale finite and > 0.
  */

@@ -686,7 +686,8 @@ def hps_seq_attention(session, q, k_pages, v_pages, block_table, lens, token_off
                       lse=None, scale=None, max_new=None, max_len=None, max_prefix=None, max_group=None, stream=None) -> None:
     """q, out [tokens, heads, dim]; pages [blocks, block size, kv heads, dim]; block_table int32 [requests, width], lens int32 [requests],
     token_offsets int32 [requests + 1]; prefix_table int32 [groups, width], prefix_lens int32 [groups], group_offsets int32 [groups + 1]; lse float32
-    [tokens, heads].  The bounds max_new, max_len, max_prefix and max_group are, where they are not given, the most that the shapes allow.
+    [tokens, heads].  The bounds max_new, max_len, max_prefix and max_group are, where they are not given, the most that the shapes allow:
+    right for any lengths, and slow for many requests of few tokens, which max_new and max_group should be given for.
     scale: 1 / sqrt(dim) if None."""
     T, H, D = shape = q.shape
     dtype = q.dtype

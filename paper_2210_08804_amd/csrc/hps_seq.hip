@@ -22,7 +22,8 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 // work-groups), scans its own into LDS, and writes its share of the chunk's tokens and blocks, each found by a binary
 // search in LDS; some of its waves see to the blocks while the others see to the tokens.  Bound by the chain of round trips
 // (arguments, lengths, table or free list): 64 requests of a token each 5.8 us, 8,192 requests with a million tokens 12 us (9 MB,
-// which a copy moves in 2).
+// which a copy moves in 2).  What reading the lengths again costs grows with the square of the requests: 65,536 of a token each 22 us,
+// 262,144 62, a million 323.
 constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64;                // of a work-group (256 threads: the same times)
 constexpr uint32_t kPer = 4, kChunk = kPer * kThreads; // requests of a thread, of a work-group
 constexpr uint32_t kMaxSum = 0x7FFFFFFFu;
@@ -250,9 +251,9 @@ struct ReleaseArgs {
     uint32_t n_requests, sh, cap, width, n_blocks;
 };
 
-// One work-group: requests end seldom, and the free list is one stack whose order the call fixes.  Bound by the round trips of a
-// thousand blocks at a time, some 1.4 us: 64 requests of which 8 end with 63 blocks each 5.3 us, 8,192 of which 1,024 end with ten 18 us
-// (all 8,192: 118 us).
+// One work-group: the free list is one stack whose order the call fixes.  Bound by the round trips of a thousand blocks at a time, some
+// 1.4 us: 64 requests of which 8 end with 63 blocks each 5.3 us, 1,040 that all end with a block each (candidates that were scored) 6, 8,192
+// with a block each 14, with ten each 115.
 __global__ void __launch_bounds__(kThreads) release_kernel(const ReleaseArgs a) {
     __shared__ uint32_t l_blk[kChunk + 1], l_wave[kWaves];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));

@@ -195,7 +195,8 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
 
     // Rows of 16 keys (or values) from token `at` on to LDS.  Whole ones of a block: returns true, the loads are under way,
     // kLoads of them.  At the end of the keys, for small blocks and for a block number that is none: each lane by itself,
-    // zeros in the place of what is not there.
+    // zeros in the place of what is not there.  (Blocks of fewer than 16 tokens always come this way, and wait for it: 256 requests behind
+    // 8,192 keys 83 us instead of 38, 4 behind 200,003 718 instead of 156.)
     template <bool kValues> __device__ __forceinline__ bool load16(uint32_t at, int32_t id, uint32_t to) {
         const char *head = kValues ? v_head : k_head;
         if (__builtin_expect(at + 16 <= it.end && (uint32_t)id < a.n_blocks, 1)) {
@@ -343,10 +344,10 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
     // instructions run while it computes exponentials: the keys of a step are 32 ahead of its values.
     // The inner loop has the steps of which every row sees all keys and whose reference can stay: weights may be large, they
     // only must not overflow (kMost), which their sum shows.  The others leave it for the end of the step.
-    // Bound by the matrix instructions and what they wait for: 512 requests of 32 / 8 heads of 128 behind 32,768 keys take 285 us in
-    // this kernel (964 TFLOP/s; matrix instructions alone 210, without loads 249, without exponentials 287).  The matrix pipes
-    // are busy 48 % of all cycles, LDS has no bank conflict, the clock is 1.86 to 2.0 GHz.  Two meetings a step 318 us instead of
-    // 307; eight waves to a work-group 292 instead of 299, but 42.5 instead of 40.2 for 256 requests behind 8,192 keys.
+    // Bound by the matrix instructions and what they wait for: 512 requests of 32 / 8 heads of 128 behind 32,768 keys take 285 to
+    // 298 us in this kernel by device (964 to 924 TFLOP/s; of 307 at the time matrix instructions alone took 210, all but the loads 249, all
+    // but the exponentials 287).  The matrix pipes are busy 48 % of all cycles, LDS 24 % without a bank conflict (waves wait 3 % of
+    // their time to issue to it), the clock is 1.86 to 2.0 GHz.  Two meetings a step 318 us instead of 307; eight waves to a work-group 292 instead of 299, but 42.5 instead of 40.2 for 256 requests behind 8,192 keys.
     __device__ __forceinline__ void wide() {
         const uint32_t wave = uniform(threadIdx.x >> 6), least = least_limit(), mine = 16 * wave;
         if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
@@ -436,7 +437,7 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
 
     // One wave, 32 rows, every `stride`-th 32 keys from `from` on, in its own part of LDS: the next keys are fetched as soon
     // as the scores are there, the next values behind the product with these.  Bound by HBM where histories are long (4 requests of
-    // 32 / 8 heads of 128 behind 200,003 keys: 149 us, 5.5 TB/s), else by the chain offsets, block, keys, scores, values.
+    // 32 / 8 heads of 128 behind 200,003 keys: 146 to 153 us, 5.4 to 5.6 TB/s; a kernel that only reads as much takes 153 to 160), else by the chain offsets, block, keys, scores, values.
     __device__ __forceinline__ void narrow(uint32_t from, uint32_t stride) {
         const uint32_t least = least_limit();
         if (from >= it.end) return;
