@@ -10,6 +10,11 @@
  *   hps_seq_append      the same, with keys and values written to their pages
  *   hps_seq_attention   attention of every request's new tokens over the history that its group
  *                       shares (read once for all of them) and over the request's own tokens
+ *   hps_seq_norm_rope   queries and keys divided by their root mean square, head by head, weighted and
+ *                       turned in one pass; hps_seq_norm_rope_grad its gradients
+ *   hps_seq_append_packed, hps_seq_read_packed
+ *                       pages that hold keys and values in 4 bits: written (queries and keys normed and
+ *                       turned on the way) and read back
  *
  * Pages: keys and values of tokens live in `n_blocks` blocks of `block_size` tokens (a power of two up to
  * 1024), one array each; a request's table lists its blocks in order, so token p of a request is
@@ -225,6 +230,94 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
 #define HPS_SEQ_FLAG_LENGTH 1u
 #define HPS_SEQ_FLAG_BLOCK  2u
 hps_status_t hps_seq_attention_flags(hps_seq_attention_t *s, uint32_t *flags, int clear);
+
+/* ---- norms of heads ------------------------------------------------------------------------ */
+
+/*
+ * Every head x of queries and keys becomes turn(w * x / sqrt(mean(x^2) + eps)): its root mean square over all
+ * head_dim <= 512 values, a weight for each value (fp32 [head_dim], the tensor's own; NULL = ones), and the turning of
+ * hps_seq_rope with its conventions (a token with a negative position is passed over; turned values are NaN at
+ * positions of max_pos or more).  table NULL: nothing is turned and positions is not read.  Arithmetic is in 32 bits,
+ * rounded once; a head whose squares sum to more than 32 bits hold comes out as 0.  A tensor of 0 heads may have
+ * NULL data; an output may be its input, exactly.  eps finite and >= 0.
+ */
+typedef struct {
+    hps_seq_heads_t q, k, q_out, k_out;
+    const float   *q_weight, *k_weight;
+    const int32_t *positions;           /* [n_tokens] */
+    const float   *table;
+    double   eps;
+    uint32_t n_tokens, q_heads, k_heads, head_dim, rot_dim, max_pos;
+    int32_t  dtype, interleaved;
+} hps_seq_norm_args_t;
+
+hps_status_t hps_seq_norm_rope(const hps_seq_norm_args_t *args, void *stream);
+
+#define HPS_SEQ_NORM_PARTS 1024u        /* most partial sums of a weight's gradient */
+
+/*
+ * Gradients of hps_seq_norm_rope.  args->q and k are what it was given, q_out and k_out the gradients of its
+ * outputs (read here).  q_grad and k_grad receive those of its inputs, in the tensors' type (each may be the
+ * matching input or output gradient, exactly); q_weight_grad and k_weight_grad [head_dim] fp32 those of the weights,
+ * summed over all tokens and heads (overwritten; NULL: not wanted; 0 for a tensor without heads or tokens).  Sums are
+ * in 32 bits and in an order that depends on the sizes alone.  Tokens that are passed over have no part in the
+ * sums, and their rows of q_grad and k_grad are not written.  parts: scratch memory of 2 * HPS_SEQ_NORM_PARTS * head_dim
+ * floats, needed where a weight's gradient is; calls that share it must not overlap (replays of captured graphs included).
+ */
+hps_status_t hps_seq_norm_rope_grad(const hps_seq_norm_args_t *args, const hps_seq_heads_t *q_grad, const hps_seq_heads_t *k_grad,
+                                    float *q_weight_grad, float *k_weight_grad, float *parts, void *stream);
+
+/* ---- pages in 4 bits ----------------------------------------------------------------------- */
+
+/*
+ * Packed pages hold a value as s * v: v one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (a code of 4 bits: sign, two
+ * bits of exponent, one of mantissa, that is 0 .. 7 in this order and 8 more for a negative), s = 2^(b - 127) shared by the
+ * values 32 i .. 32 i + 31 of a head, b a byte.  A group whose b is above 252 (where it is read as f16: above 140) stands for
+ * 32 values that are no numbers.  With h = head_dim / 32 the tile of a block and a head is hps_seq_packed_bytes() =
+ * block_size * head_dim * 17 / 16 bytes:
+ *   codes of keys     value d of place p in byte p * head_dim / 2 + d / 2, the low half for even d
+ *   codes of values   from block_size * head_dim / 2 on: value d of place p in byte
+ *                     p / 8 * 4 * head_dim + d / (2 h) * 8 h + p % 8 * h + d % (2 h) / 2, the low half for even d: eight places'
+ *                     values side by side, which is how the product with the weights takes them
+ *   scales of keys    from block_size * head_dim on: p * h + d / 32
+ *   scales of values  from block_size * (head_dim + h) on: p / 8 * 8 h + d / 32 * 8 + p % 8
+ * head_dim is 32, 64, 96, 128 or 256, block_size a power of two in 16 .. 1024.
+ */
+typedef struct {
+    uint8_t *data;                      /* tile of (block, head): data + block * block_stride + head * head_stride */
+    int64_t  block_stride, head_stride; /* in bytes, multiples of 16, not negative */
+    uint32_t n_blocks, block_size;
+} hps_seq_packed_t;
+
+size_t hps_seq_packed_bytes(uint32_t block_size, uint32_t head_dim);        /* 0 for sizes that packed pages do not have */
+
+/*
+ * hps_seq_append to packed pages.  norm != 0: queries and keys are normed first as in hps_seq_norm_rope (weights NULL =
+ * ones).  Queries go to q_out in their type.  Of 32 values that share a scale the largest in size, a, sets it: s is the
+ * least power of two with a <= 7 s, kept within 2^-126 .. 2^125 (dtype f16: 2^-23 .. 2^13, which reads back as f16); codes are the
+ * nearest, of two the even one, and end at 6.  Where one of the 32 is infinite or NaN all become NaN.  Keys are normed and
+ * turned in 64 bits in front of that rounding, and rounded to nothing else on the way.  Slots and positions as in
+ * hps_seq_append: a token whose slot is none has its query turned and nothing stored, slots of one call must be different, and
+ * a token with a negative position is passed over where there is a table.
+ */
+typedef struct {
+    hps_seq_heads_t q, q_out, k, v;
+    hps_seq_packed_t pages;
+    const int32_t *slots, *positions;   /* [n_tokens] */
+    const float   *table, *q_weight, *k_weight;
+    double   eps;
+    uint32_t n_tokens, q_heads, kv_heads, head_dim, rot_dim, max_pos;
+    int32_t  dtype, interleaved, norm;
+} hps_seq_append_packed_args_t;
+
+hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, void *stream);
+
+/*
+ * What packed pages hold: keys and values of slots[i] become token i of k_out and v_out (either may have NULL data), as
+ * HPS_SEQ_F32, _F16 or _BF16.  A slot may come several times; a token whose slot is none is left as it was.
+ */
+hps_status_t hps_seq_read_packed(const hps_seq_packed_t *pages, const int32_t *slots, uint32_t n_tokens, uint32_t kv_heads, uint32_t head_dim,
+                                 const hps_seq_heads_t *k_out, const hps_seq_heads_t *v_out, int dtype, void *stream);
 
 const char *hps_seq_last_error(void);
 

@@ -40,6 +40,7 @@ EXPORTS = (
     "hps_membench_gather", "hps_membench_gather_half", "hps_membench_copy",
     "hps_seq_extend", "hps_seq_release", "hps_seq_rope_table", "hps_seq_rope", "hps_seq_append",
     "hps_seq_attention_create", "hps_seq_attention_destroy", "hps_seq_attention", "hps_seq_attention_flags",
+    "hps_seq_norm_rope", "hps_seq_norm_rope_grad", "hps_seq_packed_bytes", "hps_seq_append_packed", "hps_seq_read_packed",
     "hps_seq_last_error",
 )
 
@@ -73,6 +74,7 @@ def load_library():
     lib.hps_lookup_last_error.argtypes = []
     lib.hps_dedup_last_error.restype = C.c_char_p
     lib.hps_dedup_last_error.argtypes = []
+    lib.hps_seq_packed_bytes.restype, lib.hps_seq_packed_bytes.argtypes = C.c_size_t, [C.c_uint32, C.c_uint32]
     lib.hps_seq_last_error.restype = C.c_char_p
     lib.hps_seq_last_error.argtypes = []
     sigs = {
@@ -115,6 +117,10 @@ def load_library():
         "hps_seq_attention_destroy": [vp],
         "hps_seq_attention": [vp, vp, vp],
         "hps_seq_attention_flags": [vp, C.POINTER(u32), C.c_int],
+        "hps_seq_norm_rope": [vp, vp],
+        "hps_seq_norm_rope_grad": [vp, vp, vp, vp, vp, vp, vp],
+        "hps_seq_append_packed": [vp, vp],
+        "hps_seq_read_packed": [vp, vp, u32, u32, u32, vp, vp, C.c_int, vp],
         "hps_cache_destroy": [vp],
         "hps_cache_query": [vp, vp, sz, vp, vp, vp, vp, vp],
         "hps_cache_insert": [vp, vp, vp, sz, vp],
@@ -498,6 +504,7 @@ def hps_hostmap_fetch(m, keys, dim: int):
 HPS_SEQ_F32, HPS_SEQ_F16, HPS_SEQ_BF16 = 0, 1, 2
 HPS_SEQ_SCALE_NONE, HPS_SEQ_SCALE_LINEAR, HPS_SEQ_SCALE_PARTS = 0, 1, 2
 HPS_SEQ_FLAG_LENGTH, HPS_SEQ_FLAG_BLOCK = 1, 2
+HPS_SEQ_NORM_PARTS = 1024
 
 _SEQ_DTYPES = {torch.float32: HPS_SEQ_F32, torch.float16: HPS_SEQ_F16, torch.bfloat16: HPS_SEQ_BF16}
 # The argument structures of hps_seq.h, packed in native layout: a pointer or a 64-bit stride per P and q.
@@ -505,6 +512,10 @@ _SEQ_EXTEND = struct.Struct("@11P5I0P")
 _SEQ_ROPE = struct.Struct("@PqqPqqPqqPqqPP6I3i0P")
 _SEQ_APPEND = struct.Struct("@PqqPqqPqqPqqPPqqqIIPPP6I2i0P")
 _SEQ_ATTENTION = struct.Struct("@PqqPqqPPqqqII7P12Iif0P")
+_SEQ_HEADS = struct.Struct("@Pqq0P")
+_SEQ_NORM = struct.Struct("@PqqPqqPqqPqqPPPPd6I2i0P")
+_SEQ_PACKED = struct.Struct("@PqqII0P")
+_SEQ_APPEND_PACKED = struct.Struct("@PqqPqqPqqPqqPqqII5Pd6I3i0P")
 
 
 def _check_seq(status):
@@ -714,5 +725,137 @@ def hps_seq_attention(session, q, k_pages, v_pages, block_table, lens, token_off
         width * block if max_len is None else max_len, prefix_width * block if max_prefix is None else max_prefix, H, hk, D,
         _dtype_of(q), D ** -0.5 if scale is None else scale)
     status = (_lib or load_library()).hps_seq_attention(session, args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, where the call would run."""
+    device = _device() if _is_initialized() else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors of the current device, {device}, expected: one is on {t.device}")
+
+
+def _weight(t, name, n):
+    """Address of a contiguous float32 array of n numbers; 0 for None."""
+    if t is None:
+        return 0
+    if t.numel() != n:
+        raise ValueError(f"{name}: expected {n} numbers, got {t.numel()}")
+    return _ptr(t, _float32)
+
+
+def _norm_args(q, q_out, q_weight, k, k_out, k_weight, positions, table, eps, interleaved):
+    """(the packed structure of the norm calls, shape of q, shape of k)"""
+    T, H, D = shape = q.shape
+    dtype = q.dtype
+    address, n, rot = _rope_table_of(table)
+    if table is not None and positions is None:
+        raise ValueError("positions: needed with a table")
+    none, hk, k_shape = (0, 0, 0), 0, None
+    if k is not None:
+        if k_out is None:
+            raise ValueError("k_out: needed with k")
+        hk = k.shape[1]
+        k_shape = (T, hk, D)
+    return _SEQ_NORM.pack(
+        *_heads(q, "q", dtype, shape), *(_heads(k, "k", dtype, k_shape) if k is not None else none), *_heads(q_out, "q_out", dtype, shape),
+        *(_heads(k_out, "k_out", dtype, k_shape) if k is not None else none), _weight(q_weight, "q_weight", D), _weight(k_weight, "k_weight", D),
+        _ints(positions, "positions", T), address, eps, T, H, hk, D, rot, n, _dtype_of(q), bool(interleaved)), shape, k_shape
+
+
+def hps_seq_norm_rope(q, q_out, q_weight=None, k=None, k_out=None, k_weight=None, positions=None, table=None, eps=1e-6, interleaved=False, stream=None) -> None:
+    """Heads of q [tokens, heads, dim] (and k, with heads of its own) over their root mean square, times a weight float32 [dim] (None: ones), turned by
+    table[positions] (None: not turned)."""
+    args, _, _ = _norm_args(q, q_out, q_weight, k, k_out, k_weight, positions, table, eps, interleaved)
+    _here(q, q_out, q_weight, k, k_out, k_weight, positions, table)
+    status = (_lib or load_library()).hps_seq_norm_rope(args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_norm_rope_grad(q, q_out_grad, q_grad, q_weight=None, q_weight_grad=None, k=None, k_out_grad=None, k_grad=None, k_weight=None, k_weight_grad=None,
+                           positions=None, table=None, eps=1e-6, interleaved=False, parts=None, stream=None) -> None:
+    """Gradients of hps_seq_norm_rope with respect to q, k and their weights, from those of its outputs.  parts: scratch, float32 [HPS_SEQ_NORM_PARTS * 2 * dim] at
+    least, needed with a weight's gradient."""
+    args, shape, k_shape = _norm_args(q, q_out_grad, q_weight, k, k_out_grad, k_weight, positions, table, eps, interleaved)
+    D = shape[2]
+    wanted = q_weight_grad is not None or k_weight_grad is not None
+    if wanted and (parts is None or parts.numel() < HPS_SEQ_NORM_PARTS * 2 * D):
+        raise ValueError(f"parts: {HPS_SEQ_NORM_PARTS * 2 * D} numbers needed")
+    if k is not None and k_grad is None:
+        raise ValueError("k_grad: needed with k")
+    _here(q, q_out_grad, q_grad, q_weight, q_weight_grad, k, k_out_grad, k_grad, k_weight, k_weight_grad, positions, table, parts)
+    status = (_lib or load_library()).hps_seq_norm_rope_grad(
+        args, _SEQ_HEADS.pack(*_heads(q_grad, "q_grad", q.dtype, shape)), _SEQ_HEADS.pack(*_heads(k_grad, "k_grad", q.dtype, k_shape)) if k is not None else None,
+        _weight(q_weight_grad, "q_weight_grad", D), _weight(k_weight_grad, "k_weight_grad", D), _ptr(parts, _float32) if wanted else 0, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_packed_bytes(block_size: int, head_dim: int) -> int:
+    """Bytes of a block's tile of one head; 0 for sizes that packed pages do not have."""
+    return load_library().hps_seq_packed_bytes(block_size, head_dim)
+
+
+def _packed_pages(pages, dim):
+    """(address, block stride, head stride, blocks, block size) of packed pages uint8 [blocks, kv heads, bytes of a tile]."""
+    if not pages.is_cuda:
+        raise TypeError("pages: device tensor expected")
+    if pages.dtype is not torch.uint8:
+        raise TypeError(f"pages: expected {torch.uint8}, got {pages.dtype}")
+    if pages.dim() != 3:
+        raise ValueError("pages: expected a tensor [blocks, kv heads, bytes]")
+    n, _, size = pages.shape
+    sb, sh, one = pages.stride()
+    if one != 1:
+        raise ValueError("pages: the bytes of a tile must be adjacent")
+    block = size * 16 // (17 * dim)
+    if block * dim * 17 != size * 16:
+        raise ValueError(f"pages: {size} bytes are no tile of heads of {dim}")
+    return pages.data_ptr(), sb, sh, n, block
+
+
+def hps_seq_append_packed(k, v, pages, slots, q=None, q_out=None, positions=None, table=None, interleaved=False, norm=False, q_weight=None, k_weight=None,
+                          eps=1e-6, stream=None) -> None:
+    """Keys (normed where norm is set, turned with a table) and values [tokens, kv heads, dim] to slots of packed pages uint8 [blocks, kv heads,
+    hps_seq_packed_bytes(block size, dim)]; queries [tokens, heads, dim] normed and turned into q_out."""
+    T, hk, D = k_shape = k.shape
+    dtype = k.dtype
+    address, n, rot = _rope_table_of(table)
+    none, H = (0, 0, 0), 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q_out: needed with q")
+        H = q.shape[1]
+        shape = (T, H, D)
+    packed = _packed_pages(pages, D)
+    if pages.shape[1] != hk:
+        raise ValueError("pages: heads differ from the keys'")
+    if table is not None and positions is None:
+        raise ValueError("positions: needed with a table")
+    args = _SEQ_APPEND_PACKED.pack(
+        *(_heads(q, "q", dtype, shape) if q is not None else none), *(_heads(q_out, "q_out", dtype, shape) if q is not None else none),
+        *_heads(k, "k", dtype, k_shape), *_heads(v, "v", dtype, k_shape), *packed, _ints(slots, "slots", T), _ints(positions, "positions", T), address,
+        _weight(q_weight, "q_weight", D), _weight(k_weight, "k_weight", D), eps, T, H, hk, D, rot, n, _dtype_of(k), bool(interleaved), bool(norm))
+    _here(k, v, pages, slots, q, q_out, positions, table, q_weight, k_weight)
+    status = (_lib or load_library()).hps_seq_append_packed(args, _stream(stream))
+    if status:
+        _check_seq(status)
+
+
+def hps_seq_read_packed(pages, slots, k_out=None, v_out=None, stream=None) -> None:
+    """What packed pages hold in slots: k_out and v_out [tokens, kv heads, dim], either may be None, float32, float16 or bfloat16."""
+    like = k_out if k_out is not None else v_out
+    if like is None:
+        raise ValueError("k_out or v_out: one is needed")
+    T, hk, D = shape = like.shape
+    packed = _packed_pages(pages, D)
+    if pages.shape[1] != hk:
+        raise ValueError("pages: heads differ from the outputs'")
+    k, v = (_SEQ_HEADS.pack(*(_heads(t, name, like.dtype, shape) if t is not None else (0, 0, 0))) for t, name in ((k_out, "k_out"), (v_out, "v_out")))
+    _here(pages, slots, k_out, v_out)
+    status = (_lib or load_library()).hps_seq_read_packed(_SEQ_PACKED.pack(*packed), _ints(slots, "slots", T), T, hk, D, k, v, _dtype_of(like), _stream(stream))
     if status:
         _check_seq(status)

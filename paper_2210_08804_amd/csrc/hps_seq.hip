@@ -480,18 +480,6 @@ template <bool kPages> hipError_t launch_rope(RopeArgs &a, int dtype, uint32_t n
 
 int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
 
-hps_status_t check_rope(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens) {
-    SEQ_REQUIRE(dtype == HPS_SEQ_F32 || dtype == HPS_SEQ_F16 || dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F32, HPS_SEQ_F16 or HPS_SEQ_BF16");
-    SEQ_REQUIRE(head_dim > 0 && head_dim <= 512, "head_dim must be in 1 .. 512");
-    SEQ_REQUIRE(n_tokens < (1u << 31), "n_tokens must be < 2^31");
-    if (!table) return HPS_OK;
-    SEQ_REQUIRE(rot_dim % 2 == 0 && rot_dim > 0 && rot_dim <= head_dim, "rot_dim must be even and in 2 .. head_dim");
-    SEQ_REQUIRE(max_pos > 0 && max_pos <= (1u << 31), "max_pos must be in 1 .. 2^31");
-    SEQ_REQUIRE(seq_aligned(table, 8), "table must be 8-byte aligned");
-    SEQ_REQUIRE(n_tokens == 0 || seq_words(positions), "positions must be a 4-byte aligned device pointer");
-    return HPS_OK;
-}
-
 // Puts an array of heads into the arguments' place i; false if it is not there or not aligned to its values.
 bool put(RopeArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, int size) {
     a.heads[i] = heads;
@@ -505,6 +493,18 @@ bool put(RopeArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hp
 }
 
 }  // namespace
+
+hps_status_t seq_check_rope(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens) {
+    SEQ_REQUIRE(dtype == HPS_SEQ_F32 || dtype == HPS_SEQ_F16 || dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F32, HPS_SEQ_F16 or HPS_SEQ_BF16");
+    SEQ_REQUIRE(head_dim > 0 && head_dim <= 512, "head_dim must be in 1 .. 512");
+    SEQ_REQUIRE(n_tokens < (1u << 31), "n_tokens must be < 2^31");
+    if (!table) return HPS_OK;
+    SEQ_REQUIRE(rot_dim % 2 == 0 && rot_dim > 0 && rot_dim <= head_dim, "rot_dim must be even and in 2 .. head_dim");
+    SEQ_REQUIRE(max_pos > 0 && max_pos <= (1u << 31), "max_pos must be in 1 .. 2^31");
+    SEQ_REQUIRE(seq_aligned(table, 8), "table must be 8-byte aligned");
+    SEQ_REQUIRE(n_tokens == 0 || seq_words(positions), "positions must be a 4-byte aligned device pointer");
+    return HPS_OK;
+}
 
 hps_status_t hps_seq_fail(hps_status_t code, const char *what, const char *more) {
     snprintf(g_err, sizeof(g_err), "%s%s", what, more);
@@ -584,7 +584,7 @@ hps_status_t hps_seq_rope(const hps_seq_rope_args_t *args, void *stream) {
     SEQ_REQUIRE(args, "args must not be NULL");
     const hps_seq_rope_args_t &r = *args;
     SEQ_REQUIRE(r.table, "table must not be NULL");
-    if (hps_status_t st = check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
+    if (hps_status_t st = seq_check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
     SEQ_REQUIRE((uint64_t)r.q_heads + r.k_heads <= 65536, "at most 65536 heads");
     if (r.n_tokens == 0 || r.q_heads + r.k_heads == 0) return HPS_OK;
     RopeArgs a{};
@@ -604,7 +604,7 @@ hps_status_t hps_seq_rope(const hps_seq_rope_args_t *args, void *stream) {
 hps_status_t hps_seq_append(const hps_seq_append_args_t *args, void *stream) {
     SEQ_REQUIRE(args, "args must not be NULL");
     const hps_seq_append_args_t &r = *args;
-    if (hps_status_t st = check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
+    if (hps_status_t st = seq_check_rope(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens)) return st;
     SEQ_REQUIRE(seq_block_size(r.pages.block_size), "block_size must be a power of two in 1 .. 1024");
     SEQ_REQUIRE((uint64_t)r.pages.n_blocks * r.pages.block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
     SEQ_REQUIRE(r.kv_heads > 0 && (uint64_t)r.q_heads + 2ull * r.kv_heads <= 65536, "kv_heads must be > 0, and at most 65536 heads in all");

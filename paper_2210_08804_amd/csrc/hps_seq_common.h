@@ -8,8 +8,12 @@
 
 #include "hps_seq.h"
 
+#define SEQ_HIDDEN __attribute__((visibility("hidden")))
+
 // Stores the message of hps_seq_last_error() (no allocation, so nothing can be thrown) and returns `code`.
-__attribute__((visibility("hidden"))) hps_status_t hps_seq_fail(hps_status_t code, const char *what, const char *more = "");
+SEQ_HIDDEN hps_status_t hps_seq_fail(hps_status_t code, const char *what, const char *more = "");
+// What all calls with rotary positions ask of their arguments.
+SEQ_HIDDEN hps_status_t seq_check_rope(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens);
 
 #define SEQ_TRY(expr)                                                                                                          \
     do {                                                                                                                       \

@@ -1,0 +1,199 @@
+// Norms of heads with the rotation in the same pass: what the norm kernels and the kernel that appends to packed pages share.
+// Not part of the C ABI, and not exported.
+#ifndef HPS_SEQ_NORM_H
+#define HPS_SEQ_NORM_H
+
+#include "hps_seq_common.h"
+
+// One tensor of heads, and how work-groups share it.
+struct NormTensor {
+    const char *in, *back;                             // back: gradients of the outputs
+    char *out;
+    const float *weight;
+    int64_t in_token, in_head, back_token, back_head, out_token, out_head;  // strides in bytes
+    uint32_t heads, heads_beside, tokens_beside, groups;                    // side by side in a work-group; work-groups
+};
+
+struct NormArgs {
+    NormTensor x[2];                                   // queries, keys
+    const int32_t *positions;
+    const float *table;
+    float *parts, *weight_grad[2];
+    float eps, per_value;                              // 1 / head_dim
+    uint32_t n_tokens, head_dim, half, max_pos, lane_bits;                  // half = rot_dim / 2; lanes of a head: 1 << lane_bits
+    uint32_t first_group;                              // of this launch
+    int32_t interleaved, norm;
+};
+
+constexpr uint32_t kNormThreads = 256;
+
+template <typename T, int E> struct alignas(E * sizeof(T) > 16 ? 16 : E * sizeof(T)) NormVec { T v[E]; };
+
+// Sum over the 1 << bits lanes that hold a head; every lane gets it, the same bits.
+template <int kCtrl> __device__ __forceinline__ float norm_dpp(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float norm_sum(float x, uint32_t bits) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    if (bits > 0) x += norm_dpp<0xB1>(x);              // lane ^ 1
+    if (bits > 1) x += norm_dpp<0x4E>(x);              // lane ^ 2
+    if (bits > 2) x += norm_dpp<0x141>(x);             // 7 - lane of 8, whose quads are alike by now
+    if (bits > 3) x += norm_dpp<0x140>(x);             // 15 - lane of 16
+    if (bits > 4) {
+        const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r.x) + __uint_as_float(r.y);
+    }
+    if (bits > 5) {
+        const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r.x) + __uint_as_float(r.y);
+    }
+    return x;
+}
+
+// The values that lane `l` of a head has: kPer spans of two vectors of E, for halves the two that hold E pairs.
+template <typename T, int E> struct NormSpan {
+    typedef NormVec<T, E> V;
+    uint32_t o0, o1;                                   // the two vectors, in values
+    bool has0, has1, turn0, turn1;
+    float cs[E], sn[E];                                // of the pairs: across the two vectors E, within them E / 2 each
+    float w[2 * E];
+
+    __device__ __forceinline__ void place(const NormArgs &a, uint32_t s) {
+        if (a.interleaved) {
+            o0 = 2 * s * E;
+            o1 = o0 + E;
+        } else {
+            const uint32_t split = a.half / E;         // behind the pairs, two neighbours to a span
+            o0 = s < split ? s * E : 2 * a.half + 2 * (s - split) * E;
+            o1 = s < split ? a.half + s * E : o0 + E;
+        }
+        has0 = o0 < a.head_dim;
+        has1 = o1 < a.head_dim;
+        turn0 = a.table && o0 < 2 * a.half;
+        turn1 = a.table && o1 < 2 * a.half;
+    }
+    __device__ __forceinline__ bool within(const NormArgs &a) const { return a.interleaved && E > 1; }
+    __device__ __forceinline__ void weights(const float *weight) {
+#pragma unroll
+        for (int j = 0; j < 2 * E; ++j) w[j] = 1.f;
+        if (!weight) return;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if (has0) w[j] = weight[o0 + j];
+            if (has1) w[E + j] = weight[o1 + j];
+        }
+    }
+    __device__ __forceinline__ void angles(const NormArgs &a, uint32_t s, int32_t pos, float sign) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) cs[j] = sn[j] = 0.f;
+        if (!turn0) return;
+        if ((uint32_t)pos >= a.max_pos) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) cs[j] = sn[j] = __builtin_nanf("");
+            return;
+        }
+        const float2 *row = (const float2 *)a.table + (size_t)pos * a.half;
+        const uint32_t pair = within(a) ? s * E : a.interleaved ? s : o0, n = within(a) && !turn1 ? E / 2 : E;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if ((uint32_t)j < n) {
+                const float2 f = row[pair + j];
+                cs[j] = f.x;
+                sn[j] = f.y * sign;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const char *from, float (&x)[2 * E]) const {
+        V u{}, v{};
+        if (has0) u = *(const V *)(from + o0 * sizeof(T));
+        if (has1) v = *(const V *)(from + o1 * sizeof(T));
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            x[j] = (float)u.v[j];
+            x[E + j] = (float)v.v[j];
+        }
+    }
+    __device__ __forceinline__ void store(char *to, const float (&x)[2 * E]) const {
+        V u, v;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            u.v[j] = (T)x[j];
+            v.v[j] = (T)x[E + j];
+        }
+        if (has0) *(V *)(to + o0 * sizeof(T)) = u;
+        if (has1) *(V *)(to + o1 * sizeof(T)) = v;
+    }
+    static __device__ __forceinline__ void pair(float &p, float &q, float c, float s) {
+        const float qs = q * s, qc = q * c, u = __builtin_fmaf(p, c, -qs), v = __builtin_fmaf(p, s, qc);
+        p = u;
+        q = v;
+    }
+    __device__ __forceinline__ void turn(const NormArgs &a, float (&x)[2 * E]) const {
+        if (!turn0) return;
+        if (within(a)) {
+            if constexpr (E > 1) {
+#pragma unroll
+                for (int j = 0; j < E / 2; ++j) {
+                    pair(x[2 * j], x[2 * j + 1], cs[j], sn[j]);
+                    if (turn1) pair(x[E + 2 * j], x[E + 2 * j + 1], cs[E / 2 + j], sn[E / 2 + j]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) pair(x[j], x[E + j], cs[j], sn[j]);
+        }
+    }
+};
+
+// A work-group's heads of one tensor: y = turn(w x / sqrt(mean(x^2) + eps)).  A lane's place in its head stays the same from head to
+// head, so weights, cosines and sines are read once.  E = 1 is for rows that are not in whole 16-byte vectors.
+template <typename T, int E> __device__ __forceinline__ void norm_forward(const NormArgs &a, const NormTensor &g, uint32_t group) {
+    constexpr int kPer = E == 1 ? 4 : 1;
+    const uint32_t l = threadIdx.x & ((1u << a.lane_bits) - 1u), row = threadIdx.x >> a.lane_bits;
+    const uint32_t beside = row / g.heads_beside, t = group * g.tokens_beside + beside;
+    if (beside >= g.tokens_beside || t >= a.n_tokens) return;               // all lanes of a head, or none
+    const int32_t pos = a.table ? a.positions[t] : 0;
+    if (pos < 0) return;
+    NormSpan<T, E> sp[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const uint32_t s = l + ((uint32_t)i << a.lane_bits);
+        sp[i].place(a, s);
+        sp[i].weights(a.norm ? g.weight : nullptr);
+        sp[i].angles(a, s, pos, 1.f);
+    }
+    const char *from = g.in + (int64_t)t * g.in_token;
+    char *to = g.out + (int64_t)t * g.out_token;
+    for (uint32_t h = row % g.heads_beside; h < g.heads; h += g.heads_beside) {
+        float x[kPer][2 * E], r = 1.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sp[i].load(from + (int64_t)h * g.in_head, x[i]);
+        if (a.norm) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                for (int j = 0; j < 2 * E; ++j) sum = __builtin_fmaf(x[i][j], x[i][j], sum);
+            r = 1.f / __builtin_sqrtf(__builtin_fmaf(norm_sum(sum, a.lane_bits), a.per_value, a.eps));
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (a.norm)
+#pragma unroll
+                for (int j = 0; j < 2 * E; ++j) x[i][j] = x[i][j] * r * sp[i].w[j];
+            sp[i].turn(a, x[i]);
+            sp[i].store(to + (int64_t)h * g.out_head, x[i]);
+        }
+    }
+}
+
+// Puts a tensor's heads into place i.  false if it is not there or not aligned to its values.
+SEQ_HIDDEN bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, const hps_seq_heads_t *back, int size);
+// Whether every row starts on 16 bytes and no vector holds pairs of two kinds; sets the lanes of a head for either.
+SEQ_HIDDEN bool norm_whole(NormArgs &a, uint32_t rot_dim, int size);
+// Shares a tensor's rows between work-groups, which take several tokens where there are enough of them.
+SEQ_HIDDEN void norm_share(NormArgs &a, int i, uint32_t most_groups);
+SEQ_HIDDEN hps_status_t norm_check(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens, double eps,
+                        const float *q_weight, const float *k_weight);
+
+#endif  // HPS_SEQ_NORM_H

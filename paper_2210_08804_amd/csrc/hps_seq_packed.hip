@@ -1,0 +1,414 @@
+// Keys and values of new tokens to pages that hold them in 4 bits, and back (hps_seq.h), for gfx950.
+#include <hip/hip_runtime.h>
+
+#include "hps_seq_norm.h"
+#include "hps_seq_packed.h"
+
+namespace {
+
+// Where a token's values lie in its tile.
+struct Tile {
+    uint32_t dim, groups, block;
+    __device__ __forceinline__ uint32_t key(uint32_t place, uint32_t d) const { return place * (dim / 2) + d / 2; }
+    __device__ __forceinline__ uint32_t key_scale(uint32_t place, uint32_t d) const { return block * dim + place * groups + d / 32; }
+    // of values d, d + 1, d even
+    __device__ __forceinline__ uint32_t value(uint32_t place, uint32_t d) const {
+        return block * (dim / 2) + place / 8 * (4 * dim) + d / (2 * groups) * (8 * groups) + place % 8 * groups + d % (2 * groups) / 2;
+    }
+    __device__ __forceinline__ uint32_t value_scale(uint32_t place, uint32_t d) const { return block * (dim + groups) + (place / 8 * groups + d / 32) * 8 + place % 8; }
+};
+
+struct PackedArgs {
+    NormArgs norm;                                     // of the queries
+    const char *k, *v;
+    int64_t k_token, k_head, v_token, v_head;          // strides in bytes
+    char *k_out, *v_out;                               // of a reading
+    uint8_t *pages;
+    int64_t page_block, page_head;
+    const int32_t *slots;
+    const float *k_weight;
+    double eps;
+    uint32_t kv_heads, n_slots, sh, lane_bits, heads_each, head_groups;     // lanes of a head: 1 << lane_bits, 8 values each; heads of a work-group
+    uint32_t first_group, kv_groups;
+    Tile tile;
+    int32_t whole;                                     // rows of 16-byte vectors, and a vector's partners in one
+};
+
+constexpr uint32_t kThreads = 256;
+
+template <int kCtrl> __device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false); }
+template <int kCtrl> __device__ __forceinline__ double moved(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)moved<kCtrl>((uint32_t)(u >> 32)) << 32 | moved<kCtrl>((uint32_t)u));
+}
+// Over the four lanes that hold 32 neighbours.
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+    x = max(x, moved<0xB1>(x));
+    return max(x, moved<0x4E>(x));
+}
+// Over the 1 << bits lanes, four at least, that hold a head; every lane gets it, the same bits.
+__device__ __forceinline__ double head_sum(double x, uint32_t bits) {
+    x += moved<0xB1>(x);
+    x += moved<0x4E>(x);
+    if (bits > 2) x += moved<0x141>(x);                // 7 - lane of 8, whose quads are alike by now
+    if (bits > 3) x += moved<0x140>(x);                // 15 - lane of 16
+    if (bits > 4) x += __shfl_xor(x, 16);
+    return x;
+}
+
+template <typename T> struct alignas(16) Eight { T v[8]; };
+template <typename T> __device__ __forceinline__ Eight<T> load8(const char *from, bool whole) {
+    Eight<T> x;
+    if (whole) x = *(const Eight<T> *)from;
+    else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.v[j] = ((const T *)from)[j];
+    return x;
+}
+
+// The scale byte of 32 values, of which the largest in size has the leading word `top` in 64 bits (its last bit set where the rest of
+// the number is not 0): the least power of two s with a <= 7 s, 7 being 1.75 * 2^2.
+template <typename T> __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
+    if (top >= 0x7FF00000u) return 255u;               // infinite or NaN
+    const int b = (int)(top >> 20) - 1023 - 2 + ((top & 0xFFFFFu) > 0xC0000u) + 127;
+    return (uint32_t)min(max(b, kPackedLeast<T>), (int)kPackedMost<T>);
+}
+
+// Eight values' codes.  The conversion takes 32 bits, rounds to the nearest, of two to the even code, and ends at 6.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float s) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+}
+
+// Eight codes of values: runs of `groups` bytes, 8 * groups apart.
+__device__ __forceinline__ void put_values(uint8_t *to, const Tile &tile, uint32_t place, uint32_t d, uint32_t codes) {
+    if ((tile.groups & 3u) == 0) {
+        *(uint32_t *)(to + tile.value(place, d)) = codes;
+    } else if (tile.groups == 2) {
+        *(uint16_t *)(to + tile.value(place, d)) = (uint16_t)codes;
+        *(uint16_t *)(to + tile.value(place, d + 4)) = (uint16_t)(codes >> 16);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) to[tile.value(place, d + 2 * j)] = (uint8_t)(codes >> 8 * j);
+    }
+}
+__device__ __forceinline__ uint32_t get_values(const uint8_t *from, const Tile &tile, uint32_t place, uint32_t d) {
+    if ((tile.groups & 3u) == 0) return *(const uint32_t *)(from + tile.value(place, d));
+    if (tile.groups == 2) return *(const uint16_t *)(from + tile.value(place, d)) | (uint32_t)*(const uint16_t *)(from + tile.value(place, d + 4)) << 16;
+    uint32_t codes = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) codes |= (uint32_t)from[tile.value(place, d + 2 * j)] << 8 * j;
+    return codes;
+}
+
+// A lane's place: one of a work-group's rows, half of which are keys', half values', of as many tokens.
+struct Place {
+    uint32_t d, token, head0, heads;
+    bool values, live;
+    __device__ __forceinline__ Place(const PackedArgs &a, uint32_t group) {
+        const uint32_t row = threadIdx.x >> a.lane_bits, tokens = (kThreads >> a.lane_bits) / 2, chunk = group / a.head_groups;
+        d = (threadIdx.x & ((1u << a.lane_bits) - 1u)) * 8;
+        values = row >= tokens;
+        token = chunk * tokens + (values ? row - tokens : row);
+        head0 = group % a.head_groups * a.heads_each;
+        heads = min(head0 + a.heads_each, a.kv_heads);
+        live = token < a.norm.n_tokens;
+    }
+};
+
+// A lane's eight keys in 64 bits, normed and turned.  Codes are steps of up to half a value's size, so a difference in the last bit of a
+// sum can change a key by as much: in 64 bits that does not happen, and it costs nothing here (its operations run at the rate of
+// 32 bits on this device).
+template <typename T> struct Keys {
+    float cs[8], sn[8], w[8], wp[8];                   // of the lane's values and of their partners in the turning
+    uint32_t d;
+    bool in, turns;
+    __device__ __forceinline__ uint32_t partner(const NormArgs &n, uint32_t x) const { return n.interleaved ? x ^ 1u : x < n.half ? x + n.half : x - n.half; }
+    __device__ __forceinline__ Keys(const PackedArgs &a, uint32_t first, int32_t pos) : d(first) {
+        const NormArgs &n = a.norm;
+        in = d < n.head_dim;
+        turns = n.table && in && d < 2 * n.half;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            cs[j] = 1.f;
+            sn[j] = 0.f;
+            w[j] = wp[j] = 1.f;
+            if (!in) continue;
+            if (n.norm && a.k_weight) w[j] = wp[j] = a.k_weight[d + j];
+            if (!turns || d + j >= 2 * n.half) continue;
+            if (n.norm && a.k_weight) wp[j] = a.k_weight[partner(n, d + j)];
+            float2 f = make_float2(__builtin_nanf(""), __builtin_nanf(""));
+            if ((uint32_t)pos < n.max_pos) f = ((const float2 *)n.table)[(size_t)pos * n.half + (n.interleaved ? (d + j) / 2 : (d + j) % n.half)];
+            cs[j] = f.x;
+            sn[j] = (n.interleaved ? ((d + j) & 1u) == 0 : d + j < n.half) ? -f.y : f.y;          // a cos - b sin, b cos + a sin
+        }
+    }
+    __device__ __forceinline__ void values(const PackedArgs &a, const char *from, double (&y)[8]) const {
+        const NormArgs &n = a.norm;
+        T x[8], p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = p[j] = (T)0.f;
+        if (in) {
+            const Eight<T> u = load8<T>(from + d * sizeof(T), a.whole);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = p[j] = u.v[j];
+            if (turns) {
+                if (n.interleaved) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = x[j ^ 1];
+                } else if (a.whole) {
+                    const Eight<T> v = load8<T>(from + partner(n, d) * sizeof(T), true);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = v.v[j];
+                } else {
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j)
+                        if (d + j < 2 * n.half) p[j] = ((const T *)from)[partner(n, d + j)];
+                }
+            }
+        }
+        double r = 1.0;
+        if (n.norm) {
+            double sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)(float)x[j], (double)(float)x[j], sum);
+            r = 1.0 / __builtin_sqrt(head_sum(sum, a.lane_bits) / (double)n.head_dim + a.eps);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            double z = (double)(float)x[j], zp = (double)(float)p[j];
+            if (n.norm) {
+                z = z * r * (double)w[j];
+                zp = zp * r * (double)wp[j];
+            }
+            y[j] = turns && d + j < 2 * n.half ? __builtin_fma(z, (double)cs[j], zp * (double)sn[j]) : z;
+        }
+    }
+};
+
+// Work-groups of the launch: the queries' first (as in the norm kernels), then those of keys and values.  Bound by HBM where there are many
+// tokens, else by the chain slot, position, row, largest value, store.
+template <typename T, int E> __global__ void __launch_bounds__(kThreads) append_kernel(const PackedArgs a) {
+    uint32_t group = a.first_group + blockIdx.x;
+    if (group < a.norm.x[0].groups) return norm_forward<T, E>(a.norm, a.norm.x[0], group);
+    const Place at(a, group - a.norm.x[0].groups);
+    if (!at.live) return;
+    const int32_t pos = a.norm.table ? a.norm.positions[at.token] : 0;
+    const uint32_t slot = (uint32_t)a.slots[at.token];
+    if (pos < 0 || slot >= a.n_slots) return;          // all lanes of a row
+    const uint32_t place = slot & (a.tile.block - 1u);
+    uint8_t *const block = a.pages + (int64_t)(slot >> a.sh) * a.page_block;
+    if (at.values) {
+        for (uint32_t h = at.head0; h < at.heads; ++h) {
+            const char *from = a.v + (int64_t)at.token * a.v_token + (int64_t)h * a.v_head;
+            uint8_t *to = block + (int64_t)h * a.page_head;
+            float x[8];
+            uint32_t top = 0;
+            if (at.d < a.tile.dim) {
+                const Eight<T> u = load8<T>(from + at.d * sizeof(T), a.whole);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = (float)u.v[j];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+            }
+            top = group_max(top);
+            if (at.d >= a.tile.dim) continue;
+            // the same number's leading word in 64 bits; numbers below 2^-126 get the least scale either way
+            const uint32_t b = top >= 0x7F800000u ? 255u : scale_of<T>((top >> 3) + ((1023u - 127u) << 20) | ((top & 7u) != 0));
+            put_values(to, a.tile, place, at.d, codes_of(x, __uint_as_float(b << 23)));
+            if ((at.d & 31u) == 0) to[a.tile.value_scale(place, at.d)] = (uint8_t)b;
+        }
+        return;
+    }
+    const Keys<T> keys(a, at.d, pos);
+    for (uint32_t h = at.head0; h < at.heads; ++h) {
+        uint8_t *to = block + (int64_t)h * a.page_head;
+        double y[8];
+        keys.values(a, a.k + (int64_t)at.token * a.k_token + (int64_t)h * a.k_head, y);
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint64_t u = __builtin_bit_cast(uint64_t, y[j]);
+            top = max(top, ((uint32_t)(u >> 32) & 0x7FFFFFFFu) | ((uint32_t)u != 0));
+        }
+        top = group_max(top);
+        if (at.d >= a.tile.dim) continue;
+        const uint32_t b = scale_of<T>(top);
+        // rounded here, in 64 bits, to what the conversion then takes as it is
+        const double inverse = __builtin_bit_cast(double, (uint64_t)(1023u + 127u - b) << 52);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double v = __builtin_fabs(y[j]) * inverse;
+            const double step = v < 2.0 ? 0.5 : v < 4.0 ? 1.0 : 2.0, back = v < 2.0 ? 2.0 : v < 4.0 ? 1.0 : 0.5;
+            x[j] = (float)__builtin_copysign(__builtin_rint(v * back) * step, y[j]);
+        }
+        *(uint32_t *)(to + a.tile.key(place, at.d)) = codes_of(x, 1.f);
+        if ((at.d & 31u) == 0) to[a.tile.key_scale(place, at.d)] = (uint8_t)b;
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const PackedArgs a) {
+    const Place at(a, a.first_group + blockIdx.x);
+    if (!at.live || at.d >= a.tile.dim) return;
+    const uint32_t slot = (uint32_t)a.slots[at.token], place = slot & (a.tile.block - 1u);
+    char *out = at.values ? a.v_out : a.k_out;
+    if (slot >= a.n_slots || !out) return;
+    out += (int64_t)at.token * (at.values ? a.v_token : a.k_token) + at.d * sizeof(T);
+    const uint8_t *const block = a.pages + (int64_t)(slot >> a.sh) * a.page_block;
+    for (uint32_t h = at.head0; h < at.heads; ++h) {
+        const uint8_t *from = block + (int64_t)h * a.page_head;
+        const uint32_t codes = at.values ? get_values(from, a.tile, place, at.d) : *(const uint32_t *)(from + a.tile.key(place, at.d));
+        const float s = packed_scale<T>(from[at.values ? a.tile.value_scale(place, at.d) : a.tile.key_scale(place, at.d)]);
+        typedef typename Packed<T>::pair pair;
+        const pair p[4] = {Packed<T>::template values<0>(codes, s), Packed<T>::template values<1>(codes, s), Packed<T>::template values<2>(codes, s), Packed<T>::template values<3>(codes, s)};
+        Eight<T> x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.v[j] = p[j / 2][j % 2];
+        char *to = out + (int64_t)h * (at.values ? a.v_head : a.k_head);
+        if (a.whole) *(Eight<T> *)to = x;
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ((T *)to)[j] = x.v[j];
+    }
+}
+
+int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
+
+// Lanes, and the heads that a work-group goes through: all where there are tokens enough to fill the device, else one.
+void share(PackedArgs &a, uint32_t n_tokens) {
+    a.lane_bits = 2;
+    while ((8u << a.lane_bits) < a.tile.dim) ++a.lane_bits;
+    const uint32_t tokens = (kThreads >> a.lane_bits) / 2, chunks = (n_tokens + tokens - 1) / tokens;
+    a.heads_each = chunks >= 1024 ? a.kv_heads : 1;
+    a.head_groups = (a.kv_heads + a.heads_each - 1) / a.heads_each;
+}
+
+void put_pages(PackedArgs &a, const hps_seq_packed_t &p, uint32_t head_dim) {
+    a.pages = p.data;
+    a.page_block = p.block_stride;
+    a.page_head = p.head_stride;
+    a.n_slots = p.n_blocks * p.block_size;
+    a.sh = (uint32_t)__builtin_ctz(p.block_size);
+    a.tile = Tile{head_dim, head_dim / 32, p.block_size};
+}
+
+template <typename T> hipError_t launch_append(PackedArgs &a, bool whole, hipStream_t st) {
+    return seq_launches((uint64_t)a.norm.x[0].groups + a.kv_groups, [&](uint32_t first, uint32_t n) {
+        a.first_group = first;
+        if (whole) hipLaunchKernelGGL((append_kernel<T, 16 / sizeof(T)>), dim3(n), dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((append_kernel<T, 1>), dim3(n), dim3(kThreads), 0, st, a);
+    });
+}
+
+template <typename T> hipError_t launch_read(PackedArgs &a, hipStream_t st) {
+    return seq_launches(a.kv_groups, [&](uint32_t first, uint32_t n) {
+        a.first_group = first;
+        hipLaunchKernelGGL((read_kernel<T>), dim3(n), dim3(kThreads), 0, st, a);
+    });
+}
+
+bool heads16(const void *p, int64_t token, int64_t head) { return seq_aligned(p, 16) && ((token | head) & 15) == 0; }
+
+}  // namespace
+
+hps_status_t seq_check_packed(const hps_seq_packed_t &p, uint32_t head_dim) {
+    SEQ_REQUIRE(seq_packed_dim(head_dim), "head_dim must be 32, 64, 96, 128 or 256");
+    SEQ_REQUIRE(seq_packed_block(p.block_size), "block_size must be a power of two in 16 .. 1024");
+    SEQ_REQUIRE((uint64_t)p.n_blocks * p.block_size < (1ull << 31), "n_blocks * block_size must be < 2^31");
+    SEQ_REQUIRE(p.n_blocks == 0 || (p.data && seq_aligned(p.data, 16)), "the pages must be a device pointer, 16-byte aligned");
+    SEQ_REQUIRE(p.block_stride >= 0 && p.head_stride >= 0 && ((p.block_stride | p.head_stride) & 15) == 0, "the pages' strides must be multiples of 16 bytes and not negative");
+    return HPS_OK;
+}
+
+extern "C" {
+
+size_t hps_seq_packed_bytes(uint32_t block_size, uint32_t head_dim) {
+    return seq_packed_block(block_size) && seq_packed_dim(head_dim) ? (size_t)block_size * head_dim / 16 * 17 : 0;
+}
+
+hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, void *stream) {
+    SEQ_REQUIRE(args, "args must not be NULL");
+    const hps_seq_append_packed_args_t &r = *args;
+    if (hps_status_t st = norm_check(r.dtype, r.head_dim, r.rot_dim, r.table, r.positions, r.max_pos, r.n_tokens, r.norm ? r.eps : 0.0, r.q_weight, r.k_weight)) return st;
+    if (hps_status_t st = seq_check_packed(r.pages, r.head_dim)) return st;
+    SEQ_REQUIRE(r.kv_heads > 0 && (uint64_t)r.q_heads + 2ull * r.kv_heads <= 65536, "kv_heads must be > 0, and at most 65536 heads in all");
+    if (r.n_tokens == 0) return HPS_OK;
+    SEQ_REQUIRE(seq_words(r.slots), "slots must be a 4-byte aligned device pointer");
+    const int size = size_of(r.dtype);
+    PackedArgs a{};
+    NormArgs &n = a.norm;
+    n.positions = r.positions;
+    n.table = r.table;
+    n.x[0].weight = r.q_weight;
+    n.eps = (float)r.eps;
+    n.per_value = 1.f / (float)r.head_dim;
+    n.n_tokens = r.n_tokens;
+    n.head_dim = r.head_dim;
+    n.half = r.table ? r.rot_dim / 2 : 0;
+    n.max_pos = r.max_pos;
+    n.interleaved = r.table && r.interleaved;
+    n.norm = r.norm != 0;
+    SEQ_REQUIRE(norm_put(n, 0, r.q_heads, r.q, r.q_out, nullptr, size) && r.k.data && r.v.data && seq_aligned(r.k.data, size) && seq_aligned(r.v.data, size),
+                "q, q_out, k and v must be device pointers aligned to their type");
+    const bool whole = norm_whole(n, 2 * n.half, size);
+    norm_share(n, 0, 0xFFFFFFFFu);
+    a.k = static_cast<const char *>(r.k.data);
+    a.v = static_cast<const char *>(r.v.data);
+    a.k_token = r.k.token_stride * size;
+    a.k_head = r.k.head_stride * size;
+    a.v_token = r.v.token_stride * size;
+    a.v_head = r.v.head_stride * size;
+    a.slots = r.slots;
+    a.k_weight = r.k_weight;
+    a.eps = r.eps;
+    a.kv_heads = r.kv_heads;
+    put_pages(a, r.pages, r.head_dim);
+    a.whole = heads16(a.k, a.k_token, a.k_head) && heads16(a.v, a.v_token, a.v_head) && (n.interleaved || n.half % 8 == 0);
+    share(a, r.n_tokens);
+    const uint32_t tokens = (kThreads >> a.lane_bits) / 2;
+    const uint64_t kv_groups = a.n_slots ? (uint64_t)((r.n_tokens + tokens - 1) / tokens) * a.head_groups : 0;
+    SEQ_REQUIRE(kv_groups + n.x[0].groups < (1ull << 32), "too many tokens and heads for one call");
+    a.kv_groups = (uint32_t)kv_groups;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    SEQ_TRY(r.dtype == HPS_SEQ_F32 ? launch_append<float>(a, whole, st) : r.dtype == HPS_SEQ_F16 ? launch_append<_Float16>(a, whole, st) : launch_append<__bf16>(a, whole, st));
+    return HPS_OK;
+}
+
+hps_status_t hps_seq_read_packed(const hps_seq_packed_t *pages, const int32_t *slots, uint32_t n_tokens, uint32_t kv_heads, uint32_t head_dim,
+                                 const hps_seq_heads_t *k_out, const hps_seq_heads_t *v_out, int dtype, void *stream) {
+    SEQ_REQUIRE(pages && k_out && v_out, "pages, k_out and v_out must not be NULL");
+    SEQ_REQUIRE(dtype == HPS_SEQ_F32 || dtype == HPS_SEQ_F16 || dtype == HPS_SEQ_BF16, "dtype must be HPS_SEQ_F32, HPS_SEQ_F16 or HPS_SEQ_BF16");
+    if (hps_status_t st = seq_check_packed(*pages, head_dim)) return st;
+    SEQ_REQUIRE(n_tokens < (1u << 31), "n_tokens must be < 2^31");
+    SEQ_REQUIRE(kv_heads > 0 && kv_heads <= 65536, "kv_heads must be in 1 .. 65536");
+    if (n_tokens == 0 || pages->n_blocks == 0 || (!k_out->data && !v_out->data)) return HPS_OK;
+    const int size = size_of(dtype);
+    SEQ_REQUIRE(seq_words(slots), "slots must be a 4-byte aligned device pointer");
+    SEQ_REQUIRE(seq_aligned(k_out->data, size) && seq_aligned(v_out->data, size), "k_out and v_out must be aligned to their type");
+    PackedArgs a{};
+    a.norm.n_tokens = n_tokens;
+    a.k_out = static_cast<char *>(k_out->data);
+    a.v_out = static_cast<char *>(v_out->data);
+    a.k_token = k_out->token_stride * size;
+    a.k_head = k_out->head_stride * size;
+    a.v_token = v_out->token_stride * size;
+    a.v_head = v_out->head_stride * size;
+    a.slots = slots;
+    a.kv_heads = kv_heads;
+    put_pages(a, *pages, head_dim);
+    a.whole = heads16(a.k_out, a.k_token, a.k_head) && heads16(a.v_out, a.v_token, a.v_head);
+    share(a, n_tokens);
+    const uint32_t tokens = (kThreads >> a.lane_bits) / 2;
+    const uint64_t groups = (uint64_t)((n_tokens + tokens - 1) / tokens) * a.head_groups;
+    SEQ_REQUIRE(groups < (1ull << 32), "too many tokens and heads for one call");
+    a.kv_groups = (uint32_t)groups;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    SEQ_TRY(dtype == HPS_SEQ_F32 ? launch_read<float>(a, st) : dtype == HPS_SEQ_F16 ? launch_read<_Float16>(a, st) : launch_read<__bf16>(a, st));
+    return HPS_OK;
+}
+
+}  // extern "C"
