@@ -12,9 +12,9 @@
  *                       shares (read once for all of them) and over the request's own tokens
  *   hps_seq_norm_rope   queries and keys divided by their root mean square, head by head, weighted and
  *                       turned in one pass; hps_seq_norm_rope_grad its gradients
- *   hps_seq_append_packed, hps_seq_read_packed
+ *   hps_seq_append_packed, hps_seq_read_packed, hps_seq_attention_packed
  *                       pages that hold keys and values in 4 bits: written (queries and keys normed and
- *                       turned on the way) and read back
+ *                       turned on the way), read back, attended
  *
  * Pages: keys and values of tokens live in `n_blocks` blocks of `block_size` tokens (a power of two up to
  * 1024), one array each; a request's table lists its blocks in order, so token p of a request is
@@ -318,6 +318,31 @@ hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, voi
  */
 hps_status_t hps_seq_read_packed(const hps_seq_packed_t *pages, const int32_t *slots, uint32_t n_tokens, uint32_t kv_heads, uint32_t head_dim,
                                  const hps_seq_heads_t *k_out, const hps_seq_heads_t *v_out, int dtype, void *stream);
+
+/*
+ * hps_seq_attention over packed pages: the same rows, lengths, bounds, masks, flags and sessions (one session serves
+ * both calls, in turn).  Keys and values are what hps_seq_read_packed gives in the queries' type, HPS_SEQ_F16 or HPS_SEQ_BF16; a
+ * group of values that are no numbers makes those 32 values of every row that sees it NaN.  head_dim and block_size as packed
+ * pages have them; out and q as in hps_seq_attention.
+ */
+typedef struct {
+    hps_seq_heads_t q, out;
+    hps_seq_packed_t pages;
+    const int32_t *prefix_table;        /* [n_groups][prefix_width] */
+    const int32_t *prefix_lens;         /* [n_groups] */
+    const int32_t *group_offsets;       /* [n_groups + 1] */
+    const int32_t *block_table;         /* [n_requests][table_width] */
+    const int32_t *lens;                /* [n_requests] */
+    const int32_t *token_offsets;       /* [n_requests + 1] */
+    float   *lse;
+    uint32_t n_tokens, n_requests, n_groups, table_width, prefix_width;
+    uint32_t max_new, max_group, max_len, max_prefix;
+    uint32_t q_heads, kv_heads, head_dim;
+    int32_t  dtype;
+    float    scale;
+} hps_seq_attention_packed_args_t;
+
+hps_status_t hps_seq_attention_packed(hps_seq_attention_t *s, const hps_seq_attention_packed_args_t *args, void *stream);
 
 const char *hps_seq_last_error(void);
 

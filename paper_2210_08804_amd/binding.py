@@ -40,7 +40,7 @@ EXPORTS = (
     "hps_membench_gather", "hps_membench_gather_half", "hps_membench_copy",
     "hps_seq_extend", "hps_seq_release", "hps_seq_rope_table", "hps_seq_rope", "hps_seq_append",
     "hps_seq_attention_create", "hps_seq_attention_destroy", "hps_seq_attention", "hps_seq_attention_flags",
-    "hps_seq_norm_rope", "hps_seq_norm_rope_grad", "hps_seq_packed_bytes", "hps_seq_append_packed", "hps_seq_read_packed",
+    "hps_seq_norm_rope", "hps_seq_norm_rope_grad", "hps_seq_packed_bytes", "hps_seq_append_packed", "hps_seq_read_packed", "hps_seq_attention_packed",
     "hps_seq_last_error",
 )
 
@@ -120,6 +120,7 @@ def load_library():
         "hps_seq_norm_rope": [vp, vp],
         "hps_seq_norm_rope_grad": [vp, vp, vp, vp, vp, vp, vp],
         "hps_seq_append_packed": [vp, vp],
+        "hps_seq_attention_packed": [vp, vp, vp],
         "hps_seq_read_packed": [vp, vp, u32, u32, u32, vp, vp, C.c_int, vp],
         "hps_cache_destroy": [vp],
         "hps_cache_query": [vp, vp, sz, vp, vp, vp, vp, vp],
@@ -515,6 +516,7 @@ _SEQ_ATTENTION = struct.Struct("@PqqPqqPPqqqII7P12Iif0P")
 _SEQ_HEADS = struct.Struct("@Pqq0P")
 _SEQ_NORM = struct.Struct("@PqqPqqPqqPqqPPPPd6I2i0P")
 _SEQ_PACKED = struct.Struct("@PqqII0P")
+_SEQ_ATTENTION_PACKED = struct.Struct("@PqqPqqPqqII7P12Iif0P")
 _SEQ_APPEND_PACKED = struct.Struct("@PqqPqqPqqPqqPqqII5Pd6I3i0P")
 
 
@@ -750,9 +752,9 @@ def _norm_args(q, q_out, q_weight, k, k_out, k_weight, positions, table, eps, in
     """(the packed structure of the norm calls, shape of q, shape of k)"""
     T, H, D = shape = q.shape
     dtype = q.dtype
-    address, n, rot = _rope_table_of(table)
     if table is not None and positions is None:
         raise ValueError("positions: needed with a table")
+    address, n, rot = _rope_table_of(table)
     none, hk, k_shape = (0, 0, 0), 0, None
     if k is not None:
         if k_out is None:
@@ -823,6 +825,8 @@ def hps_seq_append_packed(k, v, pages, slots, q=None, q_out=None, positions=None
     hps_seq_packed_bytes(block size, dim)]; queries [tokens, heads, dim] normed and turned into q_out."""
     T, hk, D = k_shape = k.shape
     dtype = k.dtype
+    if table is not None and positions is None:
+        raise ValueError("positions: needed with a table")
     address, n, rot = _rope_table_of(table)
     none, H = (0, 0, 0), 0
     if q is not None:
@@ -833,8 +837,6 @@ def hps_seq_append_packed(k, v, pages, slots, q=None, q_out=None, positions=None
     packed = _packed_pages(pages, D)
     if pages.shape[1] != hk:
         raise ValueError("pages: heads differ from the keys'")
-    if table is not None and positions is None:
-        raise ValueError("positions: needed with a table")
     args = _SEQ_APPEND_PACKED.pack(
         *(_heads(q, "q", dtype, shape) if q is not None else none), *(_heads(q_out, "q_out", dtype, shape) if q is not None else none),
         *_heads(k, "k", dtype, k_shape), *_heads(v, "v", dtype, k_shape), *packed, _ints(slots, "slots", T), _ints(positions, "positions", T), address,
@@ -857,5 +859,35 @@ def hps_seq_read_packed(pages, slots, k_out=None, v_out=None, stream=None) -> No
     k, v = (_SEQ_HEADS.pack(*(_heads(t, name, like.dtype, shape) if t is not None else (0, 0, 0))) for t, name in ((k_out, "k_out"), (v_out, "v_out")))
     _here(pages, slots, k_out, v_out)
     status = (_lib or load_library()).hps_seq_read_packed(_SEQ_PACKED.pack(*packed), _ints(slots, "slots", T), T, hk, D, k, v, _dtype_of(like), _stream(stream))
+    if status:
+        _check_seq(status)
+
+def hps_seq_attention_packed(session, q, pages, block_table, lens, token_offsets, out, prefix_table=None, prefix_lens=None, group_offsets=None,
+                             lse=None, scale=None, max_new=None, max_len=None, max_prefix=None, max_group=None, stream=None) -> None:
+    """hps_seq_attention over packed pages uint8 [blocks, kv heads, hps_seq_packed_bytes(block size, dim)]; the other arguments are as there."""
+    T, H, D = shape = q.shape
+    dtype = q.dtype
+    packed = _packed_pages(pages, D)
+    block = packed[4]
+    n, = lens.shape
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("block_table: expected a tensor [requests, width]")
+    width, groups, prefix_width = block_table.shape[1], 0, 0
+    if prefix_lens is not None:
+        groups, = prefix_lens.shape
+        if prefix_table is None or group_offsets is None or prefix_table.dim() != 2 or prefix_table.shape[0] != groups:
+            raise ValueError("prefix_table: expected a tensor [groups, width], and group_offsets with it")
+        prefix_width = prefix_table.shape[1]
+    if lse is not None and lse.shape != (T, H):
+        raise ValueError(f"lse: expected shape {(T, H)}, got {tuple(lse.shape)}")
+    args = _SEQ_ATTENTION_PACKED.pack(
+        *_heads(q, "q", dtype, shape), *_heads(out, "out", dtype, shape), *packed, _ints(prefix_table, "prefix_table") if groups else 0,
+        _ints(prefix_lens, "prefix_lens") if groups else 0, _ints(group_offsets, "group_offsets", groups + 1) if groups else 0,
+        _ints(block_table, "block_table"), _ints(lens, "lens"), _ints(token_offsets, "token_offsets", n + 1), _ptr(lse, _float32) or 0,
+        T, n, groups, width, prefix_width, T if max_new is None else max_new, T if max_group is None else max_group,
+        width * block if max_len is None else max_len, prefix_width * block if max_prefix is None else max_prefix, H, pages.shape[1], D,
+        _dtype_of(q), D ** -0.5 if scale is None else scale)
+    _here(q, pages, block_table, lens, token_offsets, out, prefix_table, prefix_lens, group_offsets, lse)
+    status = (_lib or load_library()).hps_seq_attention_packed(session, args, _stream(stream))
     if status:
         _check_seq(status)

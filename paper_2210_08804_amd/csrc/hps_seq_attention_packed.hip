@@ -1,0 +1,698 @@
+// Attention over pages that hold keys and values in 4 bits (hps_seq.h), for gfx950.
+//
+// What it computes, and how the work is cut and joined, is as in attention over 16-bit pages.  Here a key and its value are 17/32
+// of a byte a number, so that the conversion to 16 bits, not memory, is what few rows have to be fast at:
+//
+//   few rows (Few)    Every wave reads codes straight into the registers that the matrix instructions read, converted there; nothing
+//                     goes through LDS.  Scores are S^T = K Q^T with 16x16x32 instructions: lane (m = l % 16, g = l / 16) of the first
+//                     operand holds 8 * G neighbours of one key (G = head_dim / 32), which is one load; which key a row m stands for is
+//                     free, and chosen so that a lane ends with the scores of keys 8 g .. 8 g + 7 of its row, which are
+//                     its share of the second operand of O^T = V^T W^T as they are.  The pages' values lie so that a lane's
+//                     2 G numbers of 8 tokens are 8 * G adjacent bytes; two conversions (of a pair of numbers of two tokens) and two
+//                     byte permutations give a register of either number of both.
+//   many rows (Wide)  Keys and values are converted once for 128 rows on their way to LDS, where they lie as rows of 16-bit
+//                     pages do, and the loop is theirs.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "hps_seq_attend.h"
+#include "hps_seq_packed.h"
+
+namespace {
+
+template <typename T> struct Type16;
+template <> struct Type16<__bf16> {
+    static __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Type16<_Float16> {
+    static __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+// Over the four lanes that share a row.
+__device__ __forceinline__ float row_max(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return both_max(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return both_sum(__uint_as_float(r.x) + __uint_as_float(r.y));
+}
+
+// Two codes, byte `at` of x (known when compiled), as numbers of 16 bits each.
+template <typename T> __device__ __forceinline__ uint32_t two(uint32_t x, float s, int at) {
+    typedef Packed<T> P;
+    return __builtin_bit_cast(uint32_t, at == 0 ? P::template values<0>(x, s) : at == 1 ? P::template values<1>(x, s) : at == 2 ? P::template values<2>(x, s) : P::template values<3>(x, s));
+}
+template <typename T, typename F> __device__ __forceinline__ F eight(uint32_t x, float s) {
+    return __builtin_bit_cast(F, u32x4{two<T>(x, s, 0), two<T>(x, s, 1), two<T>(x, s, 2), two<T>(x, s, 3)});
+}
+
+// How many scales a lane's numbers have: of 8 G neighbours of a key, of 2 G of a value.
+template <int G> constexpr int kKeyScales = G == 3 ? 3 : G == 8 ? 2 : 1;
+template <int G> constexpr int kValueScales = G == 3 ? 3 : 1;
+// Which 32 numbers of a head scale x of lane part g of four (c of 16) is of; and which scale dword s (pair p) has.
+template <int G> __device__ __forceinline__ uint32_t key_group(uint32_t g, int x) { return G == 3 ? (3 * g + x) / 4 : G == 8 ? 2 * g + x : G * g / 4; }
+template <int G> __device__ __forceinline__ uint32_t value_group(uint32_t c, int x) { return G == 3 ? (6 * c + 2 * x) / 32 : 2 * G * c / 32; }
+template <int G> constexpr int key_scale(int s) { return G == 3 ? s : G == 8 ? s / 4 : 0; }
+template <int G> constexpr int value_scale(int p) { return G == 3 ? p : 0; }
+
+// kBytes bytes of a tile, in dwords (the last one may be part of one).
+template <int kWords> struct Words { uint32_t w[kWords]; };
+template <int kWords, int kAlign> __device__ __forceinline__ void load_words(const char *from, uint32_t (&to)[kWords]) {
+    constexpr int kEach = kAlign >= 16 && kWords % 4 == 0 ? 4 : kAlign >= 8 && kWords % 2 == 0 ? 2 : 1;
+    typedef uint32_t piece __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+    for (int i = 0; i < kWords; i += kEach) {
+        if constexpr (kEach == 1) to[i] = *(const uint32_t *)(from + 4 * i);
+        else {
+            const piece x = *(const piece *)(from + 4 * i);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) to[i + j] = x[j];
+        }
+    }
+}
+
+// ---- few rows
+
+template <typename T, int G, int NT> struct Few {
+    typedef typename Type<T>::frag frag;
+    static constexpr int KS = kKeyScales<G>, VS = kValueScales<G>;
+    static constexpr uint32_t kLds = 4 * 2 * G * 64 * 16 * NT, kSums = 4 * 16 * NT * sizeof(float2);
+    // The codes and scales of 32 keys and values, as loaded.
+    struct Raw {
+        uint32_t k[2][G], ks[2][KS], v[2 * G];
+        uint32_t vs[VS][2];
+    };
+
+    const Args &a;
+    const Item it;
+    const uint32_t lane, n, g;
+    const char *const tiles;                           // of the head
+    frag q[NT][G];
+    f32x4 o[NT][2 * G];
+    float m[NT], l[NT];
+    int32_t limit[NT];
+    uint32_t k_off, v_off, ks_off[KS], vs_off[VS];
+
+    __device__ __forceinline__ Few(const Args &args, const Item &item)
+        : a(args), it(item), lane(threadIdx.x & 63u), n(lane & 15u), g(lane >> 4), tiles(args.k + (int64_t)item.head * args.page_head) {
+        const uint32_t place = 8 * (n >> 2 & 1u) + (n & 3u);               // of the lane's first key, in its 16
+        k_off = place * (16 * G) + g * (4 * G);
+        v_off = (g & 1u) * (128 * G) + n * (8 * G);
+#pragma unroll
+        for (int x = 0; x < KS; ++x) ks_off[x] = place * G + key_group<G>(g, x);
+#pragma unroll
+        for (int x = 0; x < VS; ++x) vs_off[x] = (g & 1u) * (8 * G) + value_group<G>(n, x) * 8;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t row = it.row0 + 16 * t + n, i = row / a.ratio;
+            const bool there = row < it.rows;
+            limit[t] = !there ? kAll : it.causal_from == kAll ? (int32_t)it.end : min((int32_t)it.end, it.causal_from + (int32_t)i);
+            const char *src = a.q + (int64_t)(it.token0 + i) * a.q_token + (int64_t)(it.head * a.ratio + (row - i * a.ratio)) * a.q_head + g * (16 * G);
+#pragma unroll
+            for (int s = 0; s < G; ++s) {
+                u32x4 x = {0, 0, 0, 0};
+                if (there) x = *(const u32x4 *)(src + 16 * s);
+                q[t][s] = __builtin_bit_cast(frag, x);
+            }
+#pragma unroll
+            for (int i2 = 0; i2 < 2 * G; ++i2) o[t][i2] = f32x4{0, 0, 0, 0};
+            m[t] = -kInf;
+            l[t] = 0.f;
+        }
+    }
+
+    __device__ __forceinline__ int32_t block_of(uint32_t at) const { return at < it.end ? scalar(it.table, at >> a.sh) : -1; }
+
+    // Requests 32 keys and values from `at` on (a multiple of 16; at < it.end), in blocks id0 and id1.  Behind the end of the keys, and in the place of a
+    // block that is none, something else of the pages comes: hidden later, or made zeros here.
+    __device__ __forceinline__ void load(Raw &r, uint32_t at, int32_t id0, int32_t id1) const {
+        const bool bad0 = (uint32_t)id0 >= a.n_blocks, more = at + 16 < it.end, bad1 = more && (uint32_t)id1 >= a.n_blocks;
+        const uint32_t block = 1u << a.sh, p0 = at & (block - 1u), p1 = more ? (at + 16) & (block - 1u) : p0;
+        const char *t0 = tiles + (int64_t)(bad0 ? 0 : id0) * a.packed_block, *t1 = more ? tiles + (int64_t)(bad1 ? 0 : id1) * a.packed_block : t0;
+        const char *c0 = t0 + p0 * (16 * G), *c1 = t1 + p1 * (16 * G), *s0 = t0 + block * (32 * G) + p0 * G, *s1 = t1 + block * (32 * G) + p1 * G;
+        const char *kc = (n & 8u ? c1 : c0) + k_off, *vc = (g & 2u ? c1 : c0) + block * (16 * G) + v_off;
+        const char *ks = n & 8u ? s1 : s0, *vs = (g & 2u ? s1 : s0) + block * G;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            load_words<G, (G % 4 == 0 ? 16 : 4 * (G & 3))>(kc + j * (64 * G), r.k[j]);
+#pragma unroll
+            for (int x = 0; x < KS; ++x) r.ks[j][x] = *(const uint8_t *)(ks + ks_off[x] + j * (4 * G));
+        }
+        load_words<2 * G, (G % 2 == 0 ? 16 : 8)>(vc, r.v);
+#pragma unroll
+        for (int x = 0; x < VS; ++x) load_words<2, 8>(vs + vs_off[x], r.vs[x]);
+        if (__builtin_expect(bad0 || bad1, 0)) {
+            if (lane == 0) atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
+            const bool no_key = n & 8u ? bad1 : bad0, no_value = g & 2u ? (more ? bad1 : bad0) : bad0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int x = 0; x < G; ++x) r.k[j][x] = no_key ? 0u : r.k[j][x];
+#pragma unroll
+                for (int x = 0; x < KS; ++x) r.ks[j][x] = no_key ? 0u : r.ks[j][x];
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * G; ++x) r.v[x] = no_value ? 0u : r.v[x];
+#pragma unroll
+            for (int x = 0; x < VS; ++x) {
+                r.vs[x][0] = no_value ? 0u : r.vs[x][0];
+                r.vs[x][1] = no_value ? 0u : r.vs[x][1];
+            }
+        }
+    }
+
+    __device__ __forceinline__ void move(int t, float top) {
+        const float next = fmaxf(m[t], top - Type<T>::kBelow), ref = next == -kInf ? 0.f : next, f = exp2_(m[t] - ref);
+        l[t] *= f;
+#pragma unroll
+        for (int i = 0; i < 2 * G; ++i) o[t][i] *= f;
+        m[t] = next;
+    }
+
+    // 32 keys and values from `at` on, of which some rows may not see some where `edge`.
+    __device__ __forceinline__ void step(Raw &r, uint32_t at, uint32_t least) {
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float f[KS];
+#pragma unroll
+            for (int x = 0; x < KS; ++x) f[x] = packed_scale<T>(r.ks[j][x]);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const frag k = eight<T, frag>(r.k[j][i], f[key_scale<G>(i)]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) s[t][j] = Type16<T>::mfma(k, q[t][i], s[t][j]);
+            }
+        }
+        const bool edge = at + 32 > least;             // uniform
+        if (edge) hide_all(s, r, at);
+        frag w[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float top = s[t][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[t][i / 4][i % 4]);
+            top = row_max(top) * a.c;
+            if (__ballot(top > m[t] + Type<T>::kSlack)) move(t, top);      // also the first time: m is -inf
+            const float ref = m[t] == -kInf ? 0.f : m[t];
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = exp2_(__builtin_fmaf(s[t][i / 4][i % 4], a.c, -ref));
+                sum += x;
+                w[t][i] = (T)x;
+            }
+            l[t] += sum;
+        }
+        float f[VS][8];
+        uint32_t largest = 0;
+#pragma unroll
+        for (int x = 0; x < VS; ++x)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t b = r.vs[x][i / 4] >> 8 * (i % 4) & 255u;
+                largest = max(largest, b);
+                f[x][i] = __uint_as_float(b << 23);
+            }
+        if (__builtin_expect(__ballot(largest > kPackedMost<T>) != 0, 0)) {
+#pragma unroll
+            for (int x = 0; x < VS; ++x)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[x][i] = packed_scale<T>(__float_as_uint(f[x][i]) >> 23);
+        }
+#pragma unroll
+        for (int p = 0; p < G; ++p) {                  // the lane's numbers 2 p and 2 p + 1 of its eight tokens
+            u32x4 even, odd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b0 = 2 * i * G + p, b1 = b0 + G;
+                const uint32_t x = two<T>(r.v[b0 / 4], f[value_scale<G>(p)][2 * i], b0 % 4), y = two<T>(r.v[b1 / 4], f[value_scale<G>(p)][2 * i + 1], b1 % 4);
+                even[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                odd[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                o[t][2 * p] = Type16<T>::mfma(__builtin_bit_cast(frag, even), w[t], o[t][2 * p]);
+                o[t][2 * p + 1] = Type16<T>::mfma(__builtin_bit_cast(frag, odd), w[t], o[t][2 * p + 1]);
+            }
+        }
+    }
+
+    // Hides the scores that a row does not see.  A hidden value must not meet the weight 0 if it is no number: values behind the end get
+    // the scale 0, and where a value that some rows see is no number, those rows' results become NaN here and the product takes a 0.
+    __device__ __forceinline__ void hide_all(f32x4 (&s)[NT][2], Raw &r, uint32_t at) {
+        const uint32_t first = at + 8 * g;
+        uint32_t seen[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            seen[t] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool see = (int32_t)(first + i) < limit[t];
+                seen[t] |= see ? 1u << i : 0u;
+                s[t][i / 4][i % 4] = see ? s[t][i / 4][i % 4] : -kInf;
+            }
+        }
+        uint32_t bad = 0;
+#pragma unroll
+        for (int x = 0; x < VS; ++x)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t shift = 8 * (i % 4), b = r.vs[x][i / 4] >> shift & 255u;
+                if (first + i >= it.end) r.vs[x][i / 4] &= ~(255u << shift);
+                else if (b > kPackedMost<T>) {
+                    bad |= 1u << (8 * x + i);
+                    r.vs[x][i / 4] &= ~(255u << shift);
+                }
+            }
+        if (__builtin_expect(__ballot(bad != 0) == 0, 1)) return;
+#pragma unroll 1
+        for (int e = 0; e < 8 * VS; ++e) {             // token e % 8 of each eight, scale e / 8 of the lanes that hold values
+            const uint64_t who = __ballot(bad >> e & 1u);
+            if (!who) continue;
+#pragma unroll
+            for (int oct = 0; oct < 4; ++oct)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const bool see = __shfl(seen[t], 16 * oct + (int)n) >> (e & 7) & 1u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const bool poisoned = see && (who >> (16 * oct + 4 * g + j) & 1u);
+#pragma unroll
+                        for (int i = 0; i < 2 * G; ++i)
+                            if (VS == 1 || i / 2 == (e >> 3)) o[t][i][j] = poisoned ? __builtin_nanf("") : o[t][i][j];
+                    }
+                }
+        }
+    }
+
+    __device__ __forceinline__ uint32_t least_limit() const {               // over the wave's rows
+        int32_t x = max(limit[0], 0);
+#pragma unroll
+        for (int t = 1; t < NT; ++t) x = min(x, max(limit[t], 0));
+        for (int d = 1; d < 16; d <<= 1) x = min(x, __shfl_xor(x, d));
+        return uniform((uint32_t)x);
+    }
+
+    // Every `stride`-th 32 keys from `from` on, the next ones' codes under way.
+    __device__ __forceinline__ void run(uint32_t from, uint32_t stride) {
+        if (from >= it.end) return;
+        const uint32_t least = least_limit();
+        Raw here, there;
+        load(here, from, block_of(from), block_of(from + 16));
+        int32_t id0 = block_of(from + stride), id1 = block_of(from + stride + 16);
+        for (uint32_t at = from;;) {
+            uint32_t next = at + stride;
+            if (next < it.end) load(there, next, id0, id1);
+            id0 = block_of(next + stride);
+            id1 = block_of(next + stride + 16);
+            step(here, at, least);
+            if (next >= it.end) return;
+            at = next + stride;
+            if (at < it.end) load(here, at, id0, id1);
+            id0 = block_of(at + stride);
+            id1 = block_of(at + stride + 16);
+            step(there, next, least);
+            if (at >= it.end) return;
+        }
+    }
+
+    // The lane's 8 G neighbours of a row, from number 8 G g on.
+    template <typename F> static __device__ __forceinline__ f32x4 quad(int y, F of) { return f32x4{of(4 * y), of(4 * y + 1), of(4 * y + 2), of(4 * y + 3)}; }
+    __device__ __forceinline__ f32x4 quad(int t, int y) const {
+        return quad(y, [&](int x) { return o[t][x % (2 * G)][x / (2 * G)]; });
+    }
+
+    struct Place {
+        char *to;
+        bool direct;
+        float f;
+        __device__ __forceinline__ void put4(uint32_t dim, f32x4 x) const {
+            if (direct) {
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                t4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = f == 0.f ? (T)0.f : (T)(x[j] * f);
+                *(t4 *)(to + dim * 2) = y;
+            } else {
+                *(f32x4 *)(to + dim * 4) = x;
+            }
+        }
+    };
+    __device__ __forceinline__ Place place(uint32_t row, float ref, float sum, bool first) const {
+        const uint32_t i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
+        const size_t at = (size_t)t * a.q_heads + h, part = (size_t)it.part * a.n_tokens * a.q_heads + at;
+        if (first) {
+            if (!a.direct) a.part_ml[part] = make_float2(ref, sum);
+            else if (a.lse) a.lse[at] = sum == 0.f ? -kInf : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+        }
+        return {a.direct ? a.out + (int64_t)t * a.out_token + (int64_t)h * a.out_head : (char *)(a.part_o + part * (32 * G)), a.direct != 0, sum == 0.f ? 0.f : 1.f / sum};
+    }
+    // The wave's own rows, as they are.
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t row = it.row0 + 16 * t + n;
+            const float sum = row_sum(l[t]);
+            if (row >= it.rows) continue;
+            const Place p = place(row, m[t], sum, g == 0);
+#pragma unroll
+            for (int y = 0; y < 2 * G; ++y) p.put4(8 * G * g + 4 * y, quad(t, y));
+        }
+    }
+    // The four waves have the same rows and different keys: joined through LDS, each wave a quarter of the values.
+    __device__ __forceinline__ void finish_split(char *shared) {
+        const uint32_t wave = uniform(threadIdx.x >> 6);
+        f32x4 *l_o = (f32x4 *)shared;                  // [wave][NT * 2 G][64]
+        float2 *l_ml = (float2 *)(shared + kLds);      // [wave][NT * 16]
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float sum = row_sum(l[t]);
+#pragma unroll
+            for (int y = 0; y < 2 * G; ++y) l_o[(wave * (NT * 2 * G) + t * 2 * G + y) * 64 + lane] = quad(t, y);
+            if (g == 0) l_ml[(wave * NT + t) * 16 + n] = make_float2(m[t], sum);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t row = it.row0 + 16 * t + n;
+            float ref = -kInf, total = 0.f, f[kWaves];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) ref = fmaxf(ref, l_ml[(w * NT + t) * 16 + n].x);
+            const float at = ref == -kInf ? 0.f : ref;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float2 x = l_ml[(w * NT + t) * 16 + n];
+                f[w] = exp2_(x.x - at);
+                total += f[w] * x.y;
+            }
+            if (row >= it.rows) continue;
+            const Place p = place(row, ref, total, wave == 0 && g == 0);
+            for (uint32_t y = wave; y < 2 * G; y += kWaves) {
+                f32x4 x{};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) x += f[w] * l_o[(w * (NT * 2 * G) + t * 2 * G + y) * 64 + lane];
+                p.put4(8 * G * g + 4 * y, x);
+            }
+        }
+    }
+};
+
+// ---- many rows
+
+template <typename T, int G> struct Wide : Engine<T, G, true> {
+    typedef Engine<T, G, true> E;
+    typedef typename E::frag frag;
+    static constexpr int KS = kKeyScales<G>, VS = kValueScales<G>;
+    // The codes and scales of a lane's share of 16 keys (8 G neighbours of one) and of 16 values (2 G numbers of four).
+    struct Raw {
+        uint32_t k[G], ks[KS], v[G], vs[VS];
+        bool has_key, has_value;
+    };
+    const char *const tiles;
+    uint32_t k_off, v_off, key_row, value_row;
+
+    __device__ __forceinline__ Wide(const Args &args, const Item &item, uint32_t lds_base, uint32_t first_row)
+        : E(args, item, lds_base, first_row), tiles(args.k + (int64_t)item.head * args.page_head) {
+        key_row = this->lane >> 2;
+        value_row = 8 * (this->lane >> 5) + 4 * (this->lane & 1u);
+        k_off = key_row * (16 * G) + (this->lane & 3u) * (4 * G);
+        v_off = (this->lane >> 5) * (128 * G) + (this->lane >> 1 & 15u) * (8 * G) + (this->lane & 1u) * (4 * G);
+    }
+
+    // Block of the 16 tokens from `at` on: true if it is one, false (and a flag, within the length) if not.
+    __device__ __forceinline__ bool valid(uint32_t at, int32_t id) const {
+        if (__builtin_expect((uint32_t)id < this->a.n_blocks, 1)) return true;
+        if (at < this->it.end && this->lane == 0) atomicOr(this->a.flags, HPS_SEQ_FLAG_BLOCK);
+        return false;
+    }
+    __device__ __forceinline__ void fetch_keys(Raw &r, uint32_t at, int32_t id) const {
+        r.has_key = valid(at, id);
+        if (!r.has_key) return;
+        const uint32_t block = 1u << this->a.sh, p = at & (block - 1u);
+        const char *t = tiles + (int64_t)id * this->a.packed_block;
+        load_words<G, (G % 4 == 0 ? 16 : 4 * (G & 3))>(t + p * (16 * G) + k_off, r.k);
+#pragma unroll
+        for (int x = 0; x < KS; ++x) r.ks[x] = *(const uint8_t *)(t + block * (32 * G) + (p + key_row) * G + key_group<G>(this->lane & 3u, x));
+    }
+    __device__ __forceinline__ void fetch_values(Raw &r, uint32_t at, int32_t id) const {
+        r.has_value = valid(at, id);
+        if (!r.has_value) return;
+        const uint32_t block = 1u << this->a.sh, p = at & (block - 1u);
+        const char *t = tiles + (int64_t)id * this->a.packed_block;
+        load_words<G, (G % 4 == 0 ? 16 : 4 * (G & 3))>(t + block * (16 * G) + p * (16 * G) + v_off, r.v);
+#pragma unroll
+        for (int x = 0; x < VS; ++x)
+            r.vs[x] = *(const uint32_t *)(t + block * (33 * G) + p * G + (this->lane >> 5) * (8 * G) + value_group<G>(this->lane >> 1 & 15u, x) * 8 + 4 * (this->lane & 1u));
+    }
+    // To rows of 16 bits in LDS, as Engine::load16 leaves them; zeros for a block that is none, and for values behind the end.
+    __device__ __forceinline__ void put_keys(const Raw &r, uint32_t to) const {
+        typedef __attribute__((address_space(3))) u32x4 lds4;
+        const uint32_t row = to + key_row * E::kRow, sw = E::sw_k(key_row);
+#pragma unroll
+        for (int s = 0; s < G; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (r.has_key) x = __builtin_bit_cast(u32x4, eight<T, frag>(r.k[s], packed_scale<T>(r.ks[key_scale<G>(s)])));
+            *(lds4 *)(lds_char *)(uintptr_t)(row + ((G * (this->lane & 3u) + s) ^ sw) * 16) = x;
+        }
+    }
+    __device__ __forceinline__ void put_values(const Raw &r, uint32_t at, uint32_t to) const {
+        const uint32_t c = this->lane >> 1 & 15u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                  // tokens
+            const uint32_t t = value_row + i, row = to + t * E::kRow, sw = E::sw_v(t);
+            const bool there = r.has_value && at + t < this->it.end;
+            uint32_t x[G];
+#pragma unroll
+            for (int p = 0; p < G; ++p) {
+                const int b = i * G + p;
+                x[p] = there ? two<T>(r.v[b / 4], packed_scale<T>(r.vs[value_scale<G>(p)] >> 8 * i & 255u), b % 4) : 0u;
+            }
+            // 4 G bytes from byte 4 G c of the row on; chunks of 16 bytes change places
+            if constexpr (G % 4 == 0) {
+                typedef __attribute__((address_space(3))) u32x4 lds4;
+#pragma unroll
+                for (int p = 0; p < G; p += 4) *(lds4 *)(lds_char *)(uintptr_t)(row + ((G / 4 * c + p / 4) ^ sw) * 16) = u32x4{x[p], x[p + 1], x[p + 2], x[p + 3]};
+            } else if constexpr (G == 2) {
+                typedef __attribute__((address_space(3))) u32x2 lds2;
+                *(lds2 *)(lds_char *)(uintptr_t)(row + ((c >> 1) ^ sw) * 16 + (c & 1u) * 8) = u32x2{x[0], x[1]};
+            } else {
+                typedef __attribute__((address_space(3))) uint32_t lds1;
+#pragma unroll
+                for (int p = 0; p < G; ++p) {
+                    const uint32_t at4 = G * c + p;
+                    *(lds1 *)(lds_char *)(uintptr_t)(row + ((at4 >> 2) ^ sw) * 16 + (at4 & 3u) * 4) = x[p];
+                }
+            }
+        }
+    }
+
+    // Engine::wide, with a step's keys and values requested one step earlier, into registers, and converted to LDS while the step in front
+    // is computed.
+    __device__ __forceinline__ void run() {
+        const uint32_t wave = uniform(threadIdx.x >> 6), least = this->least_limit(), mine = 16 * wave;
+        const Item &it = this->it;
+        if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
+        uint32_t at = it.first;                        // the step's first value; its first key is 32 further on
+        uint32_t keys_to = this->lds + mine * E::kRow, values_to = keys_to + E::kWideValues, flip = E::kStage;
+        Raw r;
+        // keys `first` .. + 32 go to the second half of the other place, as if they were the end of a step in front
+        if (wave >= 2) {
+            fetch_keys(r, at + mine - 32, block_at(at + mine - 32));
+            put_keys(r, keys_to + E::kStage);
+        }
+        fetch_keys(r, at + 32 + mine, block_at(at + 32 + mine));
+        fetch_values(r, at + mine, block_at(at + mine));
+        put_keys(r, keys_to);
+        put_values(r, at + mine, values_to);
+        fetch_keys(r, at + 96 + mine, block_at(at + 96 + mine));
+        fetch_values(r, at + 64 + mine, block_at(at + 64 + mine));
+        int32_t key_id = block_at(at + 160 + mine), value_id = block_at(at + 128 + mine);
+        meet();
+        this->k_row += E::kStage;
+        f32x16 s = this->template scores<32 * E::kRow>(), t;
+        this->k_row -= E::kStage;
+        auto start = [&] {                             // everybody is done with the last step's keys and values
+            meet();
+            if (at + 96 < it.end) put_keys(r, keys_to + flip);
+            if (at + 64 < it.end) put_values(r, at + 64 + mine, values_to + flip);
+            if (at + 160 < it.end) fetch_keys(r, at + 160 + mine, key_id);
+            if (at + 128 < it.end) fetch_values(r, at + 128 + mine, value_id);
+            key_id = block_at(at + 224 + mine);
+            value_id = block_at(at + 192 + mine);
+            this->fresh();
+        };
+        auto end = [&] {                               // the places change
+            keys_to += flip;
+            values_to += flip;
+            this->k_row += flip;
+            this->v_row += flip;
+            this->here += flip;
+            flip = 0u - flip;
+            at += 64;
+        };
+        frag w[2];
+        for (;;) {
+            uint32_t left = 2;                         // stretches of 32 keys that the step has left
+            bool ahead = false;                        // t has the next stretch's scores
+            for (;;) {
+                start();
+                if (at + 64 > least) break;
+                t = this->template scores<0>();
+                float sum = this->weights(s, w, this->m);   // infinite, or NaN, the first time: m is -inf
+                if (__ballot(!(sum < Type<T>::kMost))) {
+                    ahead = true;
+                    break;
+                }
+                this->l += sum;
+                this->template add_values<E::kWideValues>(w);
+                s = this->template scores<32 * E::kRow>();
+                sum = this->weights(t, w, this->m);
+                if (__ballot(!(sum < Type<T>::kMost))) {
+                    ahead = true;
+                    left = 1;
+                    const f32x16 x = s;
+                    s = t;
+                    t = x;
+                    break;
+                }
+                this->l += sum;
+                this->template add_values<E::kWideValues + 32 * E::kRow>(w);
+                end();
+                if (at >= it.end) return;
+            }
+            if (left == 2) {
+                this->template rest<E::kWideValues>(s, w, at, least);
+                s = ahead ? t : this->template scores<0>();
+                t = this->template scores<32 * E::kRow>();
+            }
+            this->template rest<E::kWideValues + 32 * E::kRow>(s, w, at + 32, least);
+            s = t;
+            end();
+            if (at >= it.end) return;
+        }
+    }
+    __device__ __forceinline__ int32_t block_at(uint32_t at) const { return at < this->it.end ? scalar(this->it.table, at >> this->a.sh) : -1; }
+};
+
+// Work-groups of few rows alone: 16 * NT of an item.
+template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads, 2) packed_few_kernel(const Args a) {
+    typedef Few<T, G, NT> F;
+    extern __shared__ __align__(16) char shared[];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    Item it;
+    bool is_wide, solo;
+    if (!item_of<kWideRows, 16 * NT>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    F e(a, it);
+    e.run(solo ? it.first : it.first + 32 * wave, solo ? 32 : 32 * kWaves);
+    if (solo) e.finish();
+    else e.finish_split(shared);
+}
+
+// Either kind, where a history or the own tokens have many rows.
+template <typename T, int G> __global__ void __launch_bounds__(kThreads, G <= 4 ? 2 : 1) packed_kernel(const Args a) {
+    typedef Wide<T, G> W;
+    typedef Few<T, G, 1> F;
+    extern __shared__ __align__(16) char shared[];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    Item it;
+    bool is_wide, solo;
+    if (!item_of<kWideRows, 16>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (is_wide) {
+        W e(a, it, (uint32_t)(uintptr_t)(lds_char *)shared, 32 * wave);
+        e.run();
+        e.finish(32 * wave);
+    } else {
+        F e(a, it);
+        e.run(solo ? it.first : it.first + 32 * wave, solo ? 32 : 32 * kWaves);
+        if (solo) e.finish();
+        else e.finish_split(shared);
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------
+
+template <typename T, int G, int NT> constexpr uint32_t kFewLds = Few<T, G, NT>::kLds + Few<T, G, NT>::kSums;
+template <typename T, int G> constexpr uint32_t kMixedLds = Wide<T, G>::kLds > kFewLds<T, G, 1> ? Wide<T, G>::kLds : kFewLds<T, G, 1>;
+
+template <typename T, int G> hipError_t allow_lds() {
+    static_assert(kMixedLds<T, G> <= 160 * 1024 && kFewLds<T, G, 2> <= 160 * 1024, "LDS of a CU");
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_kernel<T, G>), hipFuncAttributeMaxDynamicSharedMemorySize, kMixedLds<T, G>)) return e;
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_few_kernel<T, G, 1>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds<T, G, 1>)) return e;
+    if constexpr (G <= 4) return hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_few_kernel<T, G, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds<T, G, 2>);
+    return hipSuccess;
+}
+template <typename T> hipError_t allow_lds() {
+    if (hipError_t e = allow_lds<T, 3>()) return e;
+    if (hipError_t e = allow_lds<T, 4>()) return e;
+    return allow_lds<T, 8>();
+}
+
+template <typename T, int G> hipError_t launch(Args &a, int kind, uint32_t groups, hipStream_t st) {
+    return seq_launches(groups, [&](uint32_t first, uint32_t n) {
+        a.first_group = first;
+        if (kind == 0) hipLaunchKernelGGL((packed_kernel<T, G>), dim3(n), dim3(kThreads), (kMixedLds<T, G>), st, a);
+        else if (kind == 1) hipLaunchKernelGGL((packed_few_kernel<T, G, 1>), dim3(n), dim3(kThreads), (kFewLds<T, G, 1>), st, a);
+        else if constexpr (G <= 4) hipLaunchKernelGGL((packed_few_kernel<T, G, 2>), dim3(n), dim3(kThreads), (kFewLds<T, G, 2>), st, a);
+    });
+}
+
+template <typename T> hipError_t launch(Args &a, int kind, uint32_t groups, hipStream_t st) {
+    switch (a.head_dim) {
+    case 32: return launch<T, 1>(a, kind, groups, st);
+    case 64: return launch<T, 2>(a, kind, groups, st);
+    case 96: return launch<T, 3>(a, kind, groups, st);
+    case 128: return launch<T, 4>(a, kind, groups, st);
+    default: return launch<T, 8>(a, kind, groups, st);
+    }
+}
+
+bool wide_rows(uint64_t rows, uint32_t) { return rows > 32; }
+uint32_t beside(bool, uint32_t head_dim) { return head_dim <= 128 ? 2u : 1u; }
+double step_time(bool wide, double n, double beside, uint32_t cus, double size) {
+    return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(1.5, beside * 0.0034 * size);
+}
+
+}  // namespace
+
+hipError_t seq_packed_allow_lds() {
+    if (hipError_t e = allow_lds<_Float16>()) return e;
+    return allow_lds<__bf16>();
+}
+
+extern "C" {
+
+hps_status_t hps_seq_attention_packed(hps_seq_attention_t *s, const hps_seq_attention_packed_args_t *args, void *stream) {
+    Args a{};
+    bool work = false;
+    if (hps_status_t st = seq_attend_args(s, args, a, work)) return st;
+    const hps_seq_attention_packed_args_t &r = *args;
+    if (hps_status_t st = seq_check_packed(r.pages, r.head_dim)) return st;
+    if (!work) return HPS_OK;
+    a.k = reinterpret_cast<const char *>(r.pages.data);
+    a.packed_block = r.pages.block_stride;
+    a.page_head = r.pages.head_stride;
+    if (r.pages.n_blocks == 0) {                       // no block number is one; what is read in their place is thrown away, and has to be somewhere
+        static_assert(65536u * 32 * 4 >= HPS_SEQ_MAX_BLOCK * 256 / 16 * 17, "a tile lies within any session's memory");
+        a.k = reinterpret_cast<const char *>(s->part_o);
+        a.packed_block = a.page_head = 0;
+    }
+    // rows of a tile: 16 where all fit one, else 32, of which the mixed kernel makes tiles of 16
+    const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, group_rows = r.n_groups && r.max_prefix ? (uint64_t)a.max_group * a.ratio : 0;
+    const bool mixed = own_rows > 32 || (group_rows && wide_rows(group_rows, r.max_prefix));
+    const int kind = mixed ? 0 : (own_rows <= 16 && group_rows <= 16) || r.head_dim > 128 ? 1 : 2;
+    const SeqAttendShape shape = {kWideRows, kind == 2 ? 32u : 16u, 32, kWideKeys, 32, 512, wide_rows, beside, step_time};
+    uint32_t groups, parts;
+    if (hps_status_t st = seq_attend_cut(a, shape, *s, groups, parts)) return st;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    SEQ_TRY(seq_attend_check(a, st));
+    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, kind, groups, st) : launch<__bf16>(a, kind, groups, st));
+    SEQ_TRY(seq_attend_join(a, r.dtype, parts, st));
+    return HPS_OK;
+}
+
+}  // extern "C"

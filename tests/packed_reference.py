@@ -127,3 +127,16 @@ def store(tiles, block, D, slot, head, which, code, scale):
         tile[at] = ((tile[at].long() & (0xF0 if half == 0 else 0x0F)) | (c << (4 * half))).to(torch.uint8)
     tile[s] = scale.to(torch.uint8)
     return b[code < 0]
+
+
+def packed(k, v, dtype):
+    """Tiles uint8 [blocks, heads, bytes] of pages k, v [blocks, block, heads, D]; the codes of groups that are no numbers are 0."""
+    n, block, K, D = k.shape
+    (kb, kh), (vb, vh), ks, vs = places(block, D)
+    tiles = torch.zeros(n, K, block * D * 17 // 16, dtype=torch.int64)
+    for x, b, h, s in ((k, kb, kh, ks), (v, vb, vh, vs)):
+        code, scale = quantised(x.transpose(1, 2), dtype)                   # [n, K, block, D]
+        code = code.clamp(min=0) << (4 * h)
+        tiles.scatter_add_(2, b.expand(n, K, block, D).flatten(2), code.flatten(2))
+        tiles.scatter_(2, s.expand(n, K, *s.shape).flatten(2), scale.flatten(2))
+    return tiles.to(torch.uint8)
