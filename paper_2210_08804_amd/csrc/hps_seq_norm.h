@@ -27,7 +27,15 @@ struct NormArgs {
 
 constexpr uint32_t kNormThreads = 256;
 
-template <typename T, int E> struct alignas(E * sizeof(T) > 16 ? 16 : E * sizeof(T)) NormVec { T v[E]; };
+// E values as they are loaded and stored: 16 bytes, or one value.
+template <typename T, int E> struct NormVec {
+    typedef uint32_t raw __attribute__((ext_vector_type(4)));
+    struct V { T v[E]; };
+};
+template <typename T> struct NormVec<T, 1> {
+    typedef T raw;
+    struct V { T v[1]; };
+};
 
 // Sum over the 1 << bits lanes that hold a head; every lane gets it, the same bits.
 template <int kCtrl> __device__ __forceinline__ float norm_dpp(float x) {
@@ -50,16 +58,40 @@ __device__ __forceinline__ float norm_sum(float x, uint32_t bits) {
     return x;
 }
 
-// The values that lane `l` of a head has: kPer spans of two vectors of E, for halves the two that hold E pairs.
-template <typename T, int E> struct NormSpan {
-    typedef NormVec<T, E> V;
+// 1 / sqrt(mean + eps), to the last bit but one.
+__device__ __forceinline__ float norm_inverse(const NormArgs &a, float squares) { return __builtin_amdgcn_rsqf(__builtin_fmaf(squares, a.per_value, a.eps)); }
+
+// E floats from an address of 4 bytes.
+template <int E> struct NormFloats { float v[E]; };
+template <int E> __device__ __forceinline__ NormFloats<E> norm_floats(const float *from) {
+    NormFloats<E> x;
+    if constexpr (E % 4 == 0) {
+        typedef float quad __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+            const quad y = *(const quad *)(from + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.v[i + j] = y[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) x.v[i] = from[i];
+    }
+    return x;
+}
+
+// The values that a lane has of a head, two vectors of E: for halves the two that hold E pairs, for neighbours (kWithin) two that
+// lie side by side.
+template <typename T, int E, bool kWithin> struct NormSpan {
+    typedef typename NormVec<T, E>::V V;
+    typedef typename NormVec<T, E>::raw raw;
     uint32_t o0, o1;                                   // the two vectors, in values
     bool has0, has1, turn0, turn1;
     float cs[E], sn[E];                                // of the pairs: across the two vectors E, within them E / 2 each
     float w[2 * E];
 
     __device__ __forceinline__ void place(const NormArgs &a, uint32_t s) {
-        if (a.interleaved) {
+        if (kWithin || a.interleaved) {
             o0 = 2 * s * E;
             o1 = o0 + E;
         } else {
@@ -72,41 +104,62 @@ template <typename T, int E> struct NormSpan {
         turn0 = a.table && o0 < 2 * a.half;
         turn1 = a.table && o1 < 2 * a.half;
     }
-    __device__ __forceinline__ bool within(const NormArgs &a) const { return a.interleaved && E > 1; }
     __device__ __forceinline__ void weights(const float *weight) {
 #pragma unroll
         for (int j = 0; j < 2 * E; ++j) w[j] = 1.f;
         if (!weight) return;
+        if (has0) {
+            const NormFloats<E> x = norm_floats<E>(weight + o0);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if (has0) w[j] = weight[o0 + j];
-            if (has1) w[E + j] = weight[o1 + j];
+            for (int j = 0; j < E; ++j) w[j] = x.v[j];
+        }
+        if (has1) {
+            const NormFloats<E> x = norm_floats<E>(weight + o1);
+#pragma unroll
+            for (int j = 0; j < E; ++j) w[E + j] = x.v[j];
         }
     }
+    // Cosines and sines (those times `sign`) of a position; NaN behind the table's last one.
     __device__ __forceinline__ void angles(const NormArgs &a, uint32_t s, int32_t pos, float sign) {
-#pragma unroll
-        for (int j = 0; j < E; ++j) cs[j] = sn[j] = 0.f;
-        if (!turn0) return;
-        if ((uint32_t)pos >= a.max_pos) {
-#pragma unroll
-            for (int j = 0; j < E; ++j) cs[j] = sn[j] = __builtin_nanf("");
-            return;
-        }
-        const float2 *row = (const float2 *)a.table + (size_t)pos * a.half;
-        const uint32_t pair = within(a) ? s * E : a.interleaved ? s : o0, n = within(a) && !turn1 ? E / 2 : E;
+        const bool known = (uint32_t)pos < a.max_pos;
+        const float *row = a.table + (size_t)(known ? pos : 0) * (2 * a.half);
+        constexpr int kFirst = kWithin ? E / 2 : E;    // pairs of the first vector, or of both
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            if ((uint32_t)j < n) {
-                const float2 f = row[pair + j];
-                cs[j] = f.x;
-                sn[j] = f.y * sign;
+            cs[j] = 1.f;
+            sn[j] = 0.f;
+        }
+        if (turn0) {
+            const NormFloats<2 * kFirst> x = norm_floats<2 * kFirst>(row + 2 * (kWithin || a.interleaved ? s * E : o0));
+#pragma unroll
+            for (int j = 0; j < kFirst; ++j) {
+                cs[j] = x.v[2 * j];
+                sn[j] = x.v[2 * j + 1];
             }
         }
+        if (kWithin && turn1) {
+            const NormFloats<E> x = norm_floats<E>(row + 2 * s * E + E);
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) {
+                cs[E / 2 + j] = x.v[2 * j];
+                sn[E / 2 + j] = x.v[2 * j + 1];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            cs[j] = known ? cs[j] : __builtin_nanf("");
+            sn[j] = known ? sn[j] * sign : __builtin_nanf("");
+        }
     }
-    __device__ __forceinline__ void load(const char *from, float (&x)[2 * E]) const {
-        V u{}, v{};
-        if (has0) u = *(const V *)(from + o0 * sizeof(T));
-        if (has1) v = *(const V *)(from + o1 * sizeof(T));
+    struct Raw { raw u, v; };
+    __device__ __forceinline__ Raw request(const char *from) const {
+        Raw r{};
+        if (has0) r.u = *(const raw *)(from + o0 * sizeof(T));
+        if (has1) r.v = *(const raw *)(from + o1 * sizeof(T));
+        return r;
+    }
+    static __device__ __forceinline__ void take(const Raw &r, float (&x)[2 * E]) {
+        const V u = __builtin_bit_cast(V, r.u), v = __builtin_bit_cast(V, r.v);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             x[j] = (float)u.v[j];
@@ -120,70 +173,82 @@ template <typename T, int E> struct NormSpan {
             u.v[j] = (T)x[j];
             v.v[j] = (T)x[E + j];
         }
-        if (has0) *(V *)(to + o0 * sizeof(T)) = u;
-        if (has1) *(V *)(to + o1 * sizeof(T)) = v;
+        if (has0) *(raw *)(to + o0 * sizeof(T)) = __builtin_bit_cast(raw, u);
+        if (has1) *(raw *)(to + o1 * sizeof(T)) = __builtin_bit_cast(raw, v);
     }
     static __device__ __forceinline__ void pair(float &p, float &q, float c, float s) {
         const float qs = q * s, qc = q * c, u = __builtin_fmaf(p, c, -qs), v = __builtin_fmaf(p, s, qc);
         p = u;
         q = v;
     }
-    __device__ __forceinline__ void turn(const NormArgs &a, float (&x)[2 * E]) const {
-        if (!turn0) return;
-        if (within(a)) {
-            if constexpr (E > 1) {
+    __device__ __forceinline__ void turn(float (&x)[2 * E]) const {
+        if constexpr (kWithin) {
+            if (turn0)
 #pragma unroll
-                for (int j = 0; j < E / 2; ++j) {
-                    pair(x[2 * j], x[2 * j + 1], cs[j], sn[j]);
-                    if (turn1) pair(x[E + 2 * j], x[E + 2 * j + 1], cs[E / 2 + j], sn[E / 2 + j]);
-                }
-            }
+                for (int j = 0; j < E / 2; ++j) pair(x[2 * j], x[2 * j + 1], cs[j], sn[j]);
+            if (turn1)
+#pragma unroll
+                for (int j = 0; j < E / 2; ++j) pair(x[E + 2 * j], x[E + 2 * j + 1], cs[E / 2 + j], sn[E / 2 + j]);
         } else {
+            if (turn0)
 #pragma unroll
-            for (int j = 0; j < E; ++j) pair(x[j], x[E + j], cs[j], sn[j]);
+                for (int j = 0; j < E; ++j) pair(x[j], x[E + j], cs[j], sn[j]);
         }
     }
 };
 
 // A work-group's heads of one tensor: y = turn(w x / sqrt(mean(x^2) + eps)).  A lane's place in its head stays the same from head to
-// head, so weights, cosines and sines are read once.  E = 1 is for rows that are not in whole 16-byte vectors.
-template <typename T, int E> __device__ __forceinline__ void norm_forward(const NormArgs &a, const NormTensor &g, uint32_t group) {
+// head, so weights, cosines and sines are read once for all of its heads; the next head is under way while one is computed.  E = 1 is
+// for rows that are not in whole 16-byte vectors.
+template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_forward(const NormArgs &a, const NormTensor &g, uint32_t group) {
     constexpr int kPer = E == 1 ? 4 : 1;
+    typedef NormSpan<T, E, kWithin> Span;
     const uint32_t l = threadIdx.x & ((1u << a.lane_bits) - 1u), row = threadIdx.x >> a.lane_bits;
     const uint32_t beside = row / g.heads_beside, t = group * g.tokens_beside + beside;
     if (beside >= g.tokens_beside || t >= a.n_tokens) return;               // all lanes of a head, or none
+    uint32_t h = row - beside * g.heads_beside;
+    if (h >= g.heads) return;
     const int32_t pos = a.table ? a.positions[t] : 0;
-    if (pos < 0) return;
-    NormSpan<T, E> sp[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const uint32_t s = l + ((uint32_t)i << a.lane_bits);
-        sp[i].place(a, s);
-        sp[i].weights(a.norm ? g.weight : nullptr);
-        sp[i].angles(a, s, pos, 1.f);
-    }
+    Span sp[kPer];
+    typename Span::Raw next[kPer];
     const char *from = g.in + (int64_t)t * g.in_token;
     char *to = g.out + (int64_t)t * g.out_token;
-    for (uint32_t h = row % g.heads_beside; h < g.heads; h += g.heads_beside) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        sp[i].place(a, l + ((uint32_t)i << a.lane_bits));
+        next[i] = sp[i].request(from + (int64_t)h * g.in_head);
+        sp[i].weights(a.norm ? g.weight : nullptr);
+    }
+    if (pos < 0) return;
+    if (a.table)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sp[i].angles(a, l + ((uint32_t)i << a.lane_bits), pos, 1.f);
+    for (;;) {
         float x[kPer][2 * E], r = 1.f;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sp[i].load(from + (int64_t)h * g.in_head, x[i]);
+        for (int i = 0; i < kPer; ++i) Span::take(next[i], x[i]);
+        const uint32_t after = h + g.heads_beside;
+        if (after < g.heads)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) next[i] = sp[i].request(from + (int64_t)after * g.in_head);
         if (a.norm) {
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
                 for (int j = 0; j < 2 * E; ++j) sum = __builtin_fmaf(x[i][j], x[i][j], sum);
-            r = 1.f / __builtin_sqrtf(__builtin_fmaf(norm_sum(sum, a.lane_bits), a.per_value, a.eps));
+            r = norm_inverse(a, norm_sum(sum, a.lane_bits));
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (a.norm)
 #pragma unroll
                 for (int j = 0; j < 2 * E; ++j) x[i][j] = x[i][j] * r * sp[i].w[j];
-            sp[i].turn(a, x[i]);
+            sp[i].turn(x[i]);
             sp[i].store(to + (int64_t)h * g.out_head, x[i]);
         }
+        h = after;
+        if (h >= g.heads) return;
     }
 }
 
@@ -191,7 +256,7 @@ template <typename T, int E> __device__ __forceinline__ void norm_forward(const 
 SEQ_HIDDEN bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, const hps_seq_heads_t *back, int size);
 // Whether every row starts on 16 bytes and no vector holds pairs of two kinds; sets the lanes of a head for either.
 SEQ_HIDDEN bool norm_whole(NormArgs &a, uint32_t rot_dim, int size);
-// Shares a tensor's rows between work-groups, which take several tokens where there are enough of them.
+// Shares a tensor's rows between work-groups: with enough of them a lane gets several heads of a token, and a work-group several tokens.
 SEQ_HIDDEN void norm_share(NormArgs &a, int i, uint32_t most_groups);
 SEQ_HIDDEN hps_status_t norm_check(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens, double eps,
                         const float *q_weight, const float *k_weight);

@@ -7,21 +7,21 @@
 
 namespace {
 
-template <typename T, int E> __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
+template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
     const uint32_t group = a.first_group + blockIdx.x;
-    if (group < a.x[0].groups) norm_forward<T, E>(a, a.x[0], group);
-    else norm_forward<T, E>(a, a.x[1], group - a.x[0].groups);
+    if (group < a.x[0].groups) norm_forward<T, E, kWithin>(a, a.x[0], group);
+    else norm_forward<T, E, kWithin>(a, a.x[1], group - a.x[0].groups);
 }
 
 // With n = r x, r = 1 / sqrt(mean(x^2) + eps), and y = turn(w n): dz = turn back(dy); dw = sum dz n; with g = w dz
 //   dx = r (g - n mean(g n)),
 // so a head takes one pass with two sums.  A work-group goes through tokens with its weights' sums in registers, joins its lanes' in
 // LDS at the end, and a second kernel adds up the work-groups'.
-template <typename T, int E> __device__ __forceinline__ void norm_backward(const NormArgs &a, const NormTensor &g, uint32_t which, uint32_t group) {
+template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_backward(const NormArgs &a, const NormTensor &g, uint32_t which, uint32_t group) {
     constexpr int kPer = E == 1 ? 4 : 1;
     __shared__ float l_sum[kNormThreads][kPer * 2 * E + 1];
     const uint32_t l = threadIdx.x & ((1u << a.lane_bits) - 1u), row = threadIdx.x >> a.lane_bits, beside = row / g.heads_beside;
-    NormSpan<T, E> sp[kPer];
+    NormSpan<T, E, kWithin> sp[kPer];
     float sum[kPer][2 * E];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -35,27 +35,28 @@ template <typename T, int E> __device__ __forceinline__ void norm_backward(const
         if (beside >= g.tokens_beside || t >= a.n_tokens) break;
         const int32_t pos = a.table ? a.positions[t] : 0;
         if (pos < 0) continue;
+        if (a.table)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sp[i].angles(a, l + ((uint32_t)i << a.lane_bits), pos, -1.f);
+            for (int i = 0; i < kPer; ++i) sp[i].angles(a, l + ((uint32_t)i << a.lane_bits), pos, -1.f);
         const char *from = g.in + (int64_t)t * g.in_token, *back = g.back + (int64_t)t * g.back_token;
         char *to = g.out + (int64_t)t * g.out_token;
         for (uint32_t h = row % g.heads_beside; h < g.heads; h += g.heads_beside) {
             float x[kPer][2 * E], z[kPer][2 * E], squares = 0.f, products = 0.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                sp[i].load(from + (int64_t)h * g.in_head, x[i]);
-                sp[i].load(back + (int64_t)h * g.back_head, z[i]);
+                NormSpan<T, E, kWithin>::take(sp[i].request(from + (int64_t)h * g.in_head), x[i]);
+                NormSpan<T, E, kWithin>::take(sp[i].request(back + (int64_t)h * g.back_head), z[i]);
             }
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                sp[i].turn(a, z[i]);
+                sp[i].turn(z[i]);
 #pragma unroll
                 for (int j = 0; j < 2 * E; ++j) {
                     squares = __builtin_fmaf(x[i][j], x[i][j], squares);
                     products = __builtin_fmaf(z[i][j] * sp[i].w[j], x[i][j], products);
                 }
             }
-            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(norm_sum(squares, a.lane_bits), a.per_value, a.eps));
+            const float r = norm_inverse(a, norm_sum(squares, a.lane_bits));
             const float c = norm_sum(products, a.lane_bits) * r * a.per_value;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -79,7 +80,7 @@ template <typename T, int E> __device__ __forceinline__ void norm_backward(const
     float *to = a.parts + ((size_t)which * HPS_SEQ_NORM_PARTS + group) * a.head_dim;
     for (uint32_t x = threadIdx.x; x < (uint32_t)(kPer * 2 * E) << a.lane_bits; x += kNormThreads) {
         const uint32_t lane = x & ((1u << a.lane_bits) - 1u), at = x >> a.lane_bits, j = at % (2 * E);
-        NormSpan<T, E> of;
+        NormSpan<T, E, kWithin> of;
         of.place(a, lane + (at / (2 * E) << a.lane_bits));
         if (!(j < E ? of.has0 : of.has1)) continue;
         float y = 0.f;
@@ -88,28 +89,36 @@ template <typename T, int E> __device__ __forceinline__ void norm_backward(const
     }
 }
 
-template <typename T, int E> __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(const NormArgs a) {
+template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(const NormArgs a) {
     const uint32_t group = blockIdx.x;
-    if (group < a.x[0].groups) norm_backward<T, E>(a, a.x[0], 0, group);
-    else norm_backward<T, E>(a, a.x[1], 1, group - a.x[0].groups);
+    if (group < a.x[0].groups) norm_backward<T, E, kWithin>(a, a.x[0], 0, group);
+    else norm_backward<T, E, kWithin>(a, a.x[1], 1, group - a.x[0].groups);
 }
 
-// Sums of the work-groups' parts, 16 values of a weight to a work-group, 16 threads to a value.
-__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
-    __shared__ float l_sum[16][17];
-    const uint32_t which = blockIdx.y, d = blockIdx.x * 16 + (threadIdx.x & 15u), way = threadIdx.x >> 4;
+// Sums of the work-groups' parts, 16 values of a weight to a work-group, 64 threads to a value.
+constexpr uint32_t kJoinWays = 64;
+__global__ void __launch_bounds__(16 * kJoinWays) norm_join_kernel(const NormArgs a) {
+    __shared__ float l_sum[kJoinWays][17];
+    const uint32_t which = blockIdx.y, d = blockIdx.x * 16 + (threadIdx.x & 15u), way = threadIdx.x >> 4, n = a.x[which].groups;
     float *to = a.weight_grad[which];
     if (!to) return;
     const float *from = a.parts + (size_t)which * HPS_SEQ_NORM_PARTS * a.head_dim + d;
     float sum = 0.f;
-    if (d < a.head_dim)
-        for (uint32_t p = way; p < a.x[which].groups; p += 16) sum += from[(size_t)p * a.head_dim];
+    if (d < a.head_dim) {
+        constexpr uint32_t kEach = HPS_SEQ_NORM_PARTS / kJoinWays;
+        float x[kEach];
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) x[i] = way + i * kJoinWays < n ? from[(size_t)(way + i * kJoinWays) * a.head_dim] : 0.f;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) sum += x[i];
+    }
     l_sum[way][threadIdx.x & 15u] = sum;
     __syncthreads();
-    if (way || d >= a.head_dim) return;
-    sum = 0.f;
-    for (int i = 0; i < 16; ++i) sum += l_sum[i][threadIdx.x];
-    to[d] = sum;
+    for (uint32_t w = kJoinWays / 2; w; w >>= 1) {
+        if (way < w) l_sum[way][threadIdx.x & 15u] += l_sum[way + w][threadIdx.x & 15u];
+        __syncthreads();
+    }
+    if (way == 0 && d < a.head_dim) to[d] = l_sum[0][threadIdx.x];
 }
 
 int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
@@ -117,22 +126,27 @@ int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
 template <typename T> hipError_t launch_norm(NormArgs &a, bool whole, hipStream_t st) {
     return seq_launches((uint64_t)a.x[0].groups + a.x[1].groups, [&](uint32_t first, uint32_t n) {
         a.first_group = first;
-        if (whole) hipLaunchKernelGGL((norm_kernel<T, 16 / sizeof(T)>), dim3(n), dim3(kNormThreads), 0, st, a);
-        else hipLaunchKernelGGL((norm_kernel<T, 1>), dim3(n), dim3(kNormThreads), 0, st, a);
+        if (whole && a.interleaved) hipLaunchKernelGGL((norm_kernel<T, 16 / sizeof(T), true>), dim3(n), dim3(kNormThreads), 0, st, a);
+        else if (whole) hipLaunchKernelGGL((norm_kernel<T, 16 / sizeof(T), false>), dim3(n), dim3(kNormThreads), 0, st, a);
+        else hipLaunchKernelGGL((norm_kernel<T, 1, false>), dim3(n), dim3(kNormThreads), 0, st, a);
     });
 }
 
 template <typename T> hipError_t launch_grad(const NormArgs &a, bool whole, hipStream_t st) {
     const uint32_t n = a.x[0].groups + a.x[1].groups;
     if (n) {
-        if (whole) hipLaunchKernelGGL((norm_grad_kernel<T, 16 / sizeof(T)>), dim3(n), dim3(kNormThreads), 0, st, a);
-        else hipLaunchKernelGGL((norm_grad_kernel<T, 1>), dim3(n), dim3(kNormThreads), 0, st, a);
+        if (whole && a.interleaved) hipLaunchKernelGGL((norm_grad_kernel<T, 16 / sizeof(T), true>), dim3(n), dim3(kNormThreads), 0, st, a);
+        else if (whole) hipLaunchKernelGGL((norm_grad_kernel<T, 16 / sizeof(T), false>), dim3(n), dim3(kNormThreads), 0, st, a);
+        else hipLaunchKernelGGL((norm_grad_kernel<T, 1, false>), dim3(n), dim3(kNormThreads), 0, st, a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (!a.weight_grad[0] && !a.weight_grad[1]) return hipSuccess;
-    hipLaunchKernelGGL(norm_join_kernel, dim3((a.head_dim + 15) / 16, 2), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((a.head_dim + 15) / 16, 2), dim3(16 * kJoinWays), 0, st, a);
     return hipGetLastError();
 }
+
+constexpr uint32_t kGradGroups = 512;                  // of a tensor's gradients
+static_assert(kGradGroups <= HPS_SEQ_NORM_PARTS, "a part each");
 
 NormArgs args_of(const hps_seq_norm_args_t &r) {
     NormArgs a{};
@@ -183,15 +197,21 @@ bool norm_whole(NormArgs &a, uint32_t rot_dim, int size) {
     return whole;
 }
 
+constexpr uint32_t kFill = 2048;                       // work-groups that keep the device busy, eight to a CU
+
 void norm_share(NormArgs &a, int i, uint32_t most_groups) {
     NormTensor &x = a.x[i];
     x.heads_beside = x.tokens_beside = 1;
     x.groups = 0;
     if (x.heads == 0 || a.n_tokens == 0) return;
-    const uint32_t rows = kNormThreads >> a.lane_bits, passes = (x.heads + rows - 1) / rows, spare = a.n_tokens / 1024 + 1;
-    x.heads_beside = (x.heads + passes - 1) / passes;
+    const uint32_t rows = kNormThreads >> a.lane_bits;
+    const uint64_t full = ((uint64_t)a.n_tokens * x.heads + rows - 1) / rows;                  // work-groups with a head to a lane
+    uint32_t each = full >= 4 * kFill ? 4 : full >= 2 * kFill ? 2 : 1;
+    if (x.heads > each * rows) each = (x.heads + rows - 1) / rows;
+    x.heads_beside = (x.heads + each - 1) / each;
+    const uint32_t spare = (uint32_t)(full / kFill) + 1;                    // few rows: a token each
     x.tokens_beside = rows / x.heads_beside;
-    if (x.tokens_beside > spare) x.tokens_beside = spare;                   // few tokens: a work-group each
+    if (x.tokens_beside > spare) x.tokens_beside = spare;
     x.groups = (a.n_tokens + x.tokens_beside - 1) / x.tokens_beside;
     if (x.groups > most_groups) x.groups = most_groups;
 }
@@ -242,8 +262,8 @@ hps_status_t hps_seq_norm_rope_grad(const hps_seq_norm_args_t *args, const hps_s
     a.weight_grad[0] = q_weight_grad;
     a.weight_grad[1] = k_weight_grad;
     const bool whole = norm_whole(a, 2 * a.half, size_of(r.dtype));
-    norm_share(a, 0, HPS_SEQ_NORM_PARTS);
-    norm_share(a, 1, HPS_SEQ_NORM_PARTS);
+    norm_share(a, 0, kGradGroups);
+    norm_share(a, 1, kGradGroups);
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(r.dtype == HPS_SEQ_F32 ? launch_grad<float>(a, whole, st) : r.dtype == HPS_SEQ_F16 ? launch_grad<_Float16>(a, whole, st) : launch_grad<__bf16>(a, whole, st));
     return HPS_OK;

@@ -35,6 +35,7 @@ struct PackedArgs {
 };
 
 constexpr uint32_t kThreads = 256;
+constexpr uint32_t kFill = 2048;                       // work-groups that keep the device busy, eight to a CU
 
 template <int kCtrl> __device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false); }
 template <int kCtrl> __device__ __forceinline__ double moved(double x) {
@@ -56,13 +57,13 @@ __device__ __forceinline__ double head_sum(double x, uint32_t bits) {
     return x;
 }
 
-template <typename T> struct alignas(16) Eight { T v[8]; };
+template <typename T> struct Eight { T v[8]; };
 template <typename T> __device__ __forceinline__ Eight<T> load8(const char *from, bool whole) {
+    typedef uint32_t raw __attribute__((ext_vector_type(2 * sizeof(T)), aligned(16)));
+    if (whole) return __builtin_bit_cast(Eight<T>, *(const raw *)from);
     Eight<T> x;
-    if (whole) x = *(const Eight<T> *)from;
-    else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = ((const T *)from)[j];
+    for (int j = 0; j < 8; ++j) x.v[j] = ((const T *)from)[j];
     return x;
 }
 
@@ -123,77 +124,69 @@ struct Place {
 // sum can change a key by as much: in 64 bits that does not happen, and it costs nothing here (its operations run at the rate of
 // 32 bits on this device).
 template <typename T> struct Keys {
-    float cs[8], sn[8], w[8], wp[8];                   // of the lane's values and of their partners in the turning
+    double own[8], other[8];                           // factors of the lane's values, and of their partners in the turning
     uint32_t d;
     bool in, turns;
+    struct Raw { Eight<T> x, p; };
     __device__ __forceinline__ uint32_t partner(const NormArgs &n, uint32_t x) const { return n.interleaved ? x ^ 1u : x < n.half ? x + n.half : x - n.half; }
-    __device__ __forceinline__ Keys(const PackedArgs &a, uint32_t first, int32_t pos) : d(first) {
+    __device__ __forceinline__ Keys(const PackedArgs &a, uint32_t first) : d(first) {
+        in = d < a.norm.head_dim;
+        turns = a.norm.table && in && d < 2 * a.norm.half;
+    }
+    __device__ __forceinline__ void factors(const PackedArgs &a, int32_t pos) {
         const NormArgs &n = a.norm;
-        in = d < n.head_dim;
-        turns = n.table && in && d < 2 * n.half;
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j) {
-            cs[j] = 1.f;
-            sn[j] = 0.f;
-            w[j] = wp[j] = 1.f;
+            own[j] = 1.0;
+            other[j] = 0.0;
             if (!in) continue;
-            if (n.norm && a.k_weight) w[j] = wp[j] = a.k_weight[d + j];
+            const bool weighted = n.norm && a.k_weight;
+            const double w = weighted ? (double)a.k_weight[d + j] : 1.0;
+            own[j] = w;
             if (!turns || d + j >= 2 * n.half) continue;
-            if (n.norm && a.k_weight) wp[j] = a.k_weight[partner(n, d + j)];
             float2 f = make_float2(__builtin_nanf(""), __builtin_nanf(""));
-            if ((uint32_t)pos < n.max_pos) f = ((const float2 *)n.table)[(size_t)pos * n.half + (n.interleaved ? (d + j) / 2 : (d + j) % n.half)];
-            cs[j] = f.x;
-            sn[j] = (n.interleaved ? ((d + j) & 1u) == 0 : d + j < n.half) ? -f.y : f.y;          // a cos - b sin, b cos + a sin
+            if ((uint32_t)pos < n.max_pos) f = ((const float2 *)n.table)[(size_t)pos * n.half + (n.interleaved ? (d + j) / 2 : d + j < n.half ? d + j : d + j - n.half)];
+            const bool leads = n.interleaved ? ((d + j) & 1u) == 0 : d + j < n.half;          // a cos - b sin; b cos + a sin
+            own[j] = w * (double)f.x;
+            other[j] = (weighted ? (double)a.k_weight[partner(n, d + j)] : 1.0) * (double)(leads ? -f.y : f.y);
         }
     }
-    __device__ __forceinline__ void values(const PackedArgs &a, const char *from, double (&y)[8]) const {
+    __device__ __forceinline__ Raw request(const PackedArgs &a, const char *from) const {
         const NormArgs &n = a.norm;
-        T x[8], p[8];
+        Raw r{};
+        if (!in) return r;
+        r.x = load8<T>(from + d * sizeof(T), a.whole);
+        if (!turns || n.interleaved) return r;
+        if (a.whole) r.p = load8<T>(from + partner(n, d) * sizeof(T), true);
+        else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = p[j] = (T)0.f;
-        if (in) {
-            const Eight<T> u = load8<T>(from + d * sizeof(T), a.whole);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = p[j] = u.v[j];
-            if (turns) {
-                if (n.interleaved) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[j] = x[j ^ 1];
-                } else if (a.whole) {
-                    const Eight<T> v = load8<T>(from + partner(n, d) * sizeof(T), true);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[j] = v.v[j];
-                } else {
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j)
-                        if (d + j < 2 * n.half) p[j] = ((const T *)from)[partner(n, d + j)];
-                }
-            }
-        }
-        double r = 1.0;
+            for (uint32_t j = 0; j < 8; ++j)
+                if (d + j < 2 * n.half) r.p.v[j] = ((const T *)from)[partner(n, d + j)];
+        return r;
+    }
+    __device__ __forceinline__ void values(const PackedArgs &a, const Raw &r, double (&y)[8]) const {
+        const NormArgs &n = a.norm;
+        double scale = 1.0;
         if (n.norm) {
             double sum = 0.0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)(float)x[j], (double)(float)x[j], sum);
-            r = 1.0 / __builtin_sqrt(head_sum(sum, a.lane_bits) / (double)n.head_dim + a.eps);
+            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)(float)r.x.v[j], (double)(float)r.x.v[j], sum);
+            scale = 1.0 / __builtin_sqrt(head_sum(sum, a.lane_bits) / (double)n.head_dim + a.eps);
         }
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            double z = (double)(float)x[j], zp = (double)(float)p[j];
-            if (n.norm) {
-                z = z * r * (double)w[j];
-                zp = zp * r * (double)wp[j];
-            }
-            y[j] = turns && d + j < 2 * n.half ? __builtin_fma(z, (double)cs[j], zp * (double)sn[j]) : z;
+        for (int j = 0; j < 8; ++j) {
+            const double x = (double)(float)r.x.v[j] * own[j];
+            y[j] = turns ? __builtin_fma((double)(float)(n.interleaved ? r.x.v[j ^ 1] : r.p.v[j]), other[j], x) : x;
+            if (n.norm) y[j] *= scale;
         }
     }
 };
 
 // Work-groups of the launch: the queries' first (as in the norm kernels), then those of keys and values.  Bound by HBM where there are many
 // tokens, else by the chain slot, position, row, largest value, store.
-template <typename T, int E> __global__ void __launch_bounds__(kThreads) append_kernel(const PackedArgs a) {
+template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kThreads) append_kernel(const PackedArgs a) {
     uint32_t group = a.first_group + blockIdx.x;
-    if (group < a.norm.x[0].groups) return norm_forward<T, E>(a.norm, a.norm.x[0], group);
+    if (group < a.norm.x[0].groups) return norm_forward<T, E, kWithin>(a.norm, a.norm.x[0], group);
     const Place at(a, group - a.norm.x[0].groups);
     if (!at.live) return;
     const int32_t pos = a.norm.table ? a.norm.positions[at.token] : 0;
@@ -202,18 +195,19 @@ template <typename T, int E> __global__ void __launch_bounds__(kThreads) append_
     const uint32_t place = slot & (a.tile.block - 1u);
     uint8_t *const block = a.pages + (int64_t)(slot >> a.sh) * a.page_block;
     if (at.values) {
+        const char *from = a.v + (int64_t)at.token * a.v_token + at.d * sizeof(T);
+        Eight<T> next{};
+        if (at.d < a.tile.dim) next = load8<T>(from + (int64_t)at.head0 * a.v_head, a.whole);
         for (uint32_t h = at.head0; h < at.heads; ++h) {
-            const char *from = a.v + (int64_t)at.token * a.v_token + (int64_t)h * a.v_head;
             uint8_t *to = block + (int64_t)h * a.page_head;
             float x[8];
             uint32_t top = 0;
-            if (at.d < a.tile.dim) {
-                const Eight<T> u = load8<T>(from + at.d * sizeof(T), a.whole);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = (float)u.v[j];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+            for (int j = 0; j < 8; ++j) {
+                x[j] = (float)next.v[j];
+                top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
             }
+            if (h + 1 < at.heads && at.d < a.tile.dim) next = load8<T>(from + (int64_t)(h + 1) * a.v_head, a.whole);
             top = group_max(top);
             if (at.d >= a.tile.dim) continue;
             // the same number's leading word in 64 bits; numbers below 2^-126 get the least scale either way
@@ -223,11 +217,16 @@ template <typename T, int E> __global__ void __launch_bounds__(kThreads) append_
         }
         return;
     }
-    const Keys<T> keys(a, at.d, pos);
+    Keys<T> keys(a, at.d);
+    const char *from = a.k + (int64_t)at.token * a.k_token;
+    typename Keys<T>::Raw next = keys.request(a, from + (int64_t)at.head0 * a.k_head);
+    keys.factors(a, pos);
     for (uint32_t h = at.head0; h < at.heads; ++h) {
         uint8_t *to = block + (int64_t)h * a.page_head;
         double y[8];
-        keys.values(a, a.k + (int64_t)at.token * a.k_token + (int64_t)h * a.k_head, y);
+        const typename Keys<T>::Raw raw = next;
+        if (h + 1 < at.heads) next = keys.request(a, from + (int64_t)(h + 1) * a.k_head);
+        keys.values(a, raw, y);
         uint32_t top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -269,7 +268,8 @@ template <typename T> __global__ void __launch_bounds__(kThreads) read_kernel(co
 #pragma unroll
         for (int j = 0; j < 8; ++j) x.v[j] = p[j / 2][j % 2];
         char *to = out + (int64_t)h * (at.values ? a.v_head : a.k_head);
-        if (a.whole) *(Eight<T> *)to = x;
+        typedef uint32_t raw __attribute__((ext_vector_type(2 * sizeof(T)), aligned(16)));
+        if (a.whole) *(raw *)to = __builtin_bit_cast(raw, x);
         else
 #pragma unroll
             for (int j = 0; j < 8; ++j) ((T *)to)[j] = x.v[j];
@@ -278,12 +278,14 @@ template <typename T> __global__ void __launch_bounds__(kThreads) read_kernel(co
 
 int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
 
-// Lanes, and the heads that a work-group goes through: all where there are tokens enough to fill the device, else one.
+// Lanes, and the heads that a work-group goes through: several where there are tokens enough to fill the device, else one.
 void share(PackedArgs &a, uint32_t n_tokens) {
     a.lane_bits = 2;
     while ((8u << a.lane_bits) < a.tile.dim) ++a.lane_bits;
     const uint32_t tokens = (kThreads >> a.lane_bits) / 2, chunks = (n_tokens + tokens - 1) / tokens;
-    a.heads_each = chunks >= 1024 ? a.kv_heads : 1;
+    const uint64_t full = (uint64_t)chunks * a.kv_heads;
+    a.heads_each = full >= 4 * kFill ? 4 : full >= 2 * kFill ? 2 : 1;
+    if (a.heads_each > a.kv_heads) a.heads_each = a.kv_heads;
     a.head_groups = (a.kv_heads + a.heads_each - 1) / a.heads_each;
 }
 
@@ -299,8 +301,9 @@ void put_pages(PackedArgs &a, const hps_seq_packed_t &p, uint32_t head_dim) {
 template <typename T> hipError_t launch_append(PackedArgs &a, bool whole, hipStream_t st) {
     return seq_launches((uint64_t)a.norm.x[0].groups + a.kv_groups, [&](uint32_t first, uint32_t n) {
         a.first_group = first;
-        if (whole) hipLaunchKernelGGL((append_kernel<T, 16 / sizeof(T)>), dim3(n), dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL((append_kernel<T, 1>), dim3(n), dim3(kThreads), 0, st, a);
+        if (whole && a.norm.interleaved) hipLaunchKernelGGL((append_kernel<T, 16 / sizeof(T), true>), dim3(n), dim3(kThreads), 0, st, a);
+        else if (whole) hipLaunchKernelGGL((append_kernel<T, 16 / sizeof(T), false>), dim3(n), dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((append_kernel<T, 1, false>), dim3(n), dim3(kThreads), 0, st, a);
     });
 }
 
