@@ -254,8 +254,8 @@ template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_
 
 // Puts a tensor's heads into place i.  false if it is not there or not aligned to its values.
 SEQ_HIDDEN bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, const hps_seq_heads_t *back, int size);
-// Whether every row starts on 16 bytes and no vector holds pairs of two kinds; sets the lanes of a head for either.
-SEQ_HIDDEN bool norm_whole(NormArgs &a, uint32_t rot_dim, int size);
+// Whether every row starts on 16 bytes, no vector holds pairs of two kinds, and `more`; sets the lanes of a head for either.
+SEQ_HIDDEN bool norm_whole(NormArgs &a, uint32_t rot_dim, int size, bool more = true);
 // Shares a tensor's rows between work-groups: with enough of them a lane gets several heads of a token, and a work-group several tokens.
 SEQ_HIDDEN void norm_share(NormArgs &a, int i, uint32_t most_groups);
 SEQ_HIDDEN hps_status_t norm_check(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens, double eps,

@@ -184,9 +184,9 @@ bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, con
     return heads == 0 || (in.data && out.data && seq_aligned(in.data, size) && seq_aligned(out.data, size) && (!back || (back->data && seq_aligned(back->data, size))));
 }
 
-bool norm_whole(NormArgs &a, uint32_t rot_dim, int size) {
+bool norm_whole(NormArgs &a, uint32_t rot_dim, int size, bool more) {
     const uint32_t most = 16 / size;
-    bool whole = a.head_dim % most == 0 && (a.interleaved ? rot_dim % most : a.half % most) == 0;
+    bool whole = more && a.head_dim % most == 0 && (a.interleaved ? rot_dim % most : a.half % most) == 0;
     for (const NormTensor &x : a.x)
         if (x.heads)
             whole = whole && seq_aligned(x.in, 16) && seq_aligned(x.out, 16) && seq_aligned(x.back, 16) &&
@@ -211,7 +211,7 @@ void norm_share(NormArgs &a, int i, uint32_t most_groups) {
     x.heads_beside = (x.heads + each - 1) / each;
     const uint32_t spare = (uint32_t)(full / kFill) + 1;                    // few rows: a token each
     x.tokens_beside = rows / x.heads_beside;
-    if (x.tokens_beside > spare) x.tokens_beside = spare;
+    if (most_groups > HPS_SEQ_NORM_PARTS && x.tokens_beside > spare) x.tokens_beside = spare;
     x.groups = (a.n_tokens + x.tokens_beside - 1) / x.tokens_beside;
     if (x.groups > most_groups) x.groups = most_groups;
 }

@@ -27,11 +27,10 @@ struct PackedArgs {
     int64_t page_block, page_head;
     const int32_t *slots;
     const float *k_weight;
-    double eps;
+    double eps, per_value;                             // 1 / head_dim
     uint32_t kv_heads, n_slots, sh, lane_bits, heads_each, head_groups;     // lanes of a head: 1 << lane_bits, 8 values each; heads of a work-group
     uint32_t first_group, kv_groups;
     Tile tile;
-    int32_t whole;                                     // rows of 16-byte vectors, and a vector's partners in one
 };
 
 constexpr uint32_t kThreads = 256;
@@ -58,21 +57,39 @@ __device__ __forceinline__ double head_sum(double x, uint32_t bits) {
 }
 
 template <typename T> struct Eight { T v[8]; };
-template <typename T> __device__ __forceinline__ Eight<T> load8(const char *from, bool whole) {
+template <bool kWhole, typename T> __device__ __forceinline__ Eight<T> load8(const char *from) {
     typedef uint32_t raw __attribute__((ext_vector_type(2 * sizeof(T)), aligned(16)));
-    if (whole) return __builtin_bit_cast(Eight<T>, *(const raw *)from);
+    if constexpr (kWhole) return __builtin_bit_cast(Eight<T>, *(const raw *)from);
     Eight<T> x;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x.v[j] = ((const T *)from)[j];
     return x;
 }
 
-// The scale byte of 32 values, of which the largest in size has the leading word `top` in 64 bits (its last bit set where the rest of
-// the number is not 0): the least power of two s with a <= 7 s, 7 being 1.75 * 2^2.
+// The scale byte of 32 values, of which the largest in size is `top` (as bits of 32): the least power of two s with a <= 7 s, 7 being 1.75 * 2^2.
 template <typename T> __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
-    if (top >= 0x7FF00000u) return 255u;               // infinite or NaN
-    const int b = (int)(top >> 20) - 1023 - 2 + ((top & 0xFFFFFu) > 0xC0000u) + 127;
+    if (top >= 0x7F800000u) return 255u;               // infinite or NaN
+    const int b = (int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x600000u);  // numbers below 2^-126 get the least scale either way
     return (uint32_t)min(max(b, kPackedLeast<T>), (int)kPackedMost<T>);
+}
+
+// Numbers in 32 bits that are cut off, the last bit set where anything was: what is rounded to few bits afterwards is rounded as if from 64
+// bits, and compared with a number of few bits as if it had them all.  (Conversions in the mode that cuts off, which is left again at once.)
+__device__ __forceinline__ void odd_floats(const double (&y)[8], float (&x)[8]) {
+    asm("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 4), 15\n\t"
+        "v_cvt_f32_f64 %0, %8\n\tv_cvt_f32_f64 %1, %9\n\tv_cvt_f32_f64 %2, %10\n\tv_cvt_f32_f64 %3, %11\n\t"
+        "v_cvt_f32_f64 %4, %12\n\tv_cvt_f32_f64 %5, %13\n\tv_cvt_f32_f64 %6, %14\n\tv_cvt_f32_f64 %7, %15\n\t"
+        "s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 4), 0"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(y[0]), "v"(y[1]), "v"(y[2]), "v"(y[3]), "v"(y[4]), "v"(y[5]), "v"(y[6]), "v"(y[7]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(__float_as_uint(x[j]) | min((uint32_t)__builtin_bit_cast(uint64_t, y[j]) & 0x1FFFFFFFu, 1u));
+}
+
+// 1 / sqrt(x): the instruction's 2^-26 or so, and a step that leaves the third power of it.
+__device__ __forceinline__ double inverse_root(double x) {
+    const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0);
+    return __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
 }
 
 // Eight values' codes.  The conversion takes 32 bits, rounds to the nearest, of two to the even code, and ends at 6.
@@ -123,134 +140,141 @@ struct Place {
 // A lane's eight keys in 64 bits, normed and turned.  Codes are steps of up to half a value's size, so a difference in the last bit of a
 // sum can change a key by as much: in 64 bits that does not happen, and it costs nothing here (its operations run at the rate of
 // 32 bits on this device).
-template <typename T> struct Keys {
+template <typename T, bool kWhole, bool kWithin> struct Keys {
     double own[8], other[8];                           // factors of the lane's values, and of their partners in the turning
     uint32_t d;
     bool in, turns;
     struct Raw { Eight<T> x, p; };
-    __device__ __forceinline__ uint32_t partner(const NormArgs &n, uint32_t x) const { return n.interleaved ? x ^ 1u : x < n.half ? x + n.half : x - n.half; }
-    __device__ __forceinline__ Keys(const PackedArgs &a, uint32_t first) : d(first) {
+    static __device__ __forceinline__ bool neighbours(const NormArgs &n) { return kWhole ? kWithin : n.interleaved != 0; }
+    __device__ __forceinline__ uint32_t partner(const NormArgs &n, uint32_t x) const { return neighbours(n) ? x ^ 1u : x < n.half ? x + n.half : x - n.half; }
+    __device__ __forceinline__ Keys(const PackedArgs &a, uint32_t first, bool plain) : d(first) {
         in = d < a.norm.head_dim;
-        turns = a.norm.table && in && d < 2 * a.norm.half;
+        turns = !plain && a.norm.table && in && d < 2 * a.norm.half;
     }
     __device__ __forceinline__ void factors(const PackedArgs &a, int32_t pos) {
         const NormArgs &n = a.norm;
+        const float *weight = n.norm ? a.k_weight : nullptr;
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
+        for (int j = 0; j < 8; ++j) {
             own[j] = 1.0;
             other[j] = 0.0;
-            if (!in) continue;
-            const bool weighted = n.norm && a.k_weight;
-            const double w = weighted ? (double)a.k_weight[d + j] : 1.0;
-            own[j] = w;
-            if (!turns || d + j >= 2 * n.half) continue;
-            float2 f = make_float2(__builtin_nanf(""), __builtin_nanf(""));
-            if ((uint32_t)pos < n.max_pos) f = ((const float2 *)n.table)[(size_t)pos * n.half + (n.interleaved ? (d + j) / 2 : d + j < n.half ? d + j : d + j - n.half)];
-            const bool leads = n.interleaved ? ((d + j) & 1u) == 0 : d + j < n.half;          // a cos - b sin; b cos + a sin
-            own[j] = w * (double)f.x;
-            other[j] = (weighted ? (double)a.k_weight[partner(n, d + j)] : 1.0) * (double)(leads ? -f.y : f.y);
         }
+        if (!in) return;
+        NormFloats<8> w{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}}, wp = w;
+        if (weight) w = norm_floats<8>(weight + d);
+        const bool known = (uint32_t)pos < n.max_pos, leads = d < n.half;
+        const float *row = n.table + (size_t)(known ? pos : 0) * (2 * n.half);
+        if (!turns) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) own[j] = (double)w.v[j];
+        } else if (kWhole && !kWithin) {               // eight of one half
+            if (weight) wp = norm_floats<8>(weight + partner(n, d));
+            const NormFloats<16> f = norm_floats<16>(row + 2 * (leads ? d : d - n.half));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                own[j] = (double)w.v[j] * (double)f.v[2 * j];
+                other[j] = (double)wp.v[j] * (double)(leads ? -f.v[2 * j + 1] : f.v[2 * j + 1]);      // a cos - b sin; b cos + a sin
+            }
+        } else if (kWhole) {                           // four pairs of neighbours
+            const NormFloats<8> f = norm_floats<8>(row + d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                own[j] = (double)w.v[j] * (double)f.v[j & ~1];
+                other[j] = (double)w.v[j ^ 1] * (double)(j & 1 ? f.v[j] : -f.v[j + 1]);
+            }
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                own[j] = (double)w.v[j];
+                if (d + j >= 2 * n.half) continue;
+                const uint32_t at = d + j, pair = n.interleaved ? at / 2 : at < n.half ? at : at - n.half;
+                const bool first = n.interleaved ? (at & 1u) == 0 : at < n.half;
+                own[j] *= (double)row[2 * pair];
+                other[j] = (weight ? (double)weight[partner(n, at)] : 1.0) * (double)(first ? -row[2 * pair + 1] : row[2 * pair + 1]);
+            }
+        }
+        if (turns && !known)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j)
+                if (d + j < 2 * n.half) own[j] = __builtin_nan("");
     }
     __device__ __forceinline__ Raw request(const PackedArgs &a, const char *from) const {
         const NormArgs &n = a.norm;
         Raw r{};
         if (!in) return r;
-        r.x = load8<T>(from + d * sizeof(T), a.whole);
-        if (!turns || n.interleaved) return r;
-        if (a.whole) r.p = load8<T>(from + partner(n, d) * sizeof(T), true);
+        r.x = load8<kWhole, T>(from + d * sizeof(T));
+        if (!turns || neighbours(n)) return r;
+        if constexpr (kWhole) r.p = load8<true, T>(from + partner(n, d) * sizeof(T));
         else
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j)
                 if (d + j < 2 * n.half) r.p.v[j] = ((const T *)from)[partner(n, d + j)];
         return r;
     }
-    __device__ __forceinline__ void values(const PackedArgs &a, const Raw &r, double (&y)[8]) const {
+    __device__ __forceinline__ void values(const PackedArgs &a, const Raw &r, float (&out)[8]) const {
         const NormArgs &n = a.norm;
         double scale = 1.0;
         if (n.norm) {
             double sum = 0.0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)(float)r.x.v[j], (double)(float)r.x.v[j], sum);
-            scale = 1.0 / __builtin_sqrt(head_sum(sum, a.lane_bits) / (double)n.head_dim + a.eps);
+            scale = inverse_root(__builtin_fma(head_sum(sum, a.lane_bits), a.per_value, a.eps));
         }
+        double y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const double x = (double)(float)r.x.v[j] * own[j];
-            y[j] = turns ? __builtin_fma((double)(float)(n.interleaved ? r.x.v[j ^ 1] : r.p.v[j]), other[j], x) : x;
+            y[j] = turns ? __builtin_fma((double)(float)(neighbours(n) ? r.x.v[j ^ 1] : r.p.v[j]), other[j], x) : x;
             if (n.norm) y[j] *= scale;
         }
+        odd_floats(y, out);
     }
 };
 
 // Work-groups of the launch: the queries' first (as in the norm kernels), then those of keys and values.  Bound by HBM where there are many
 // tokens, else by the chain slot, position, row, largest value, store.
 template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kThreads) append_kernel(const PackedArgs a) {
-    uint32_t group = a.first_group + blockIdx.x;
-    if (group < a.norm.x[0].groups) return norm_forward<T, E, kWithin>(a.norm, a.norm.x[0], group);
-    const Place at(a, group - a.norm.x[0].groups);
+    // the two kinds in turn, so that one's arithmetic runs beside the other's loads
+    const uint32_t group = a.first_group + blockIdx.x, pairs = 2 * min(a.norm.x[0].groups, a.kv_groups);
+    const bool queries = group < pairs ? (group & 1u) == 0 : a.norm.x[0].groups > a.kv_groups;
+    const uint32_t mine = group < pairs ? group / 2 : group - pairs / 2;
+    if (queries) return norm_forward<T, E, kWithin>(a.norm, a.norm.x[0], mine);
+    const Place at(a, mine);
     if (!at.live) return;
     const int32_t pos = a.norm.table ? a.norm.positions[at.token] : 0;
     const uint32_t slot = (uint32_t)a.slots[at.token];
     if (pos < 0 || slot >= a.n_slots) return;          // all lanes of a row
     const uint32_t place = slot & (a.tile.block - 1u);
     uint8_t *const block = a.pages + (int64_t)(slot >> a.sh) * a.page_block;
-    if (at.values) {
-        const char *from = a.v + (int64_t)at.token * a.v_token + at.d * sizeof(T);
-        Eight<T> next{};
-        if (at.d < a.tile.dim) next = load8<T>(from + (int64_t)at.head0 * a.v_head, a.whole);
-        for (uint32_t h = at.head0; h < at.heads; ++h) {
-            uint8_t *to = block + (int64_t)h * a.page_head;
-            float x[8];
-            uint32_t top = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = (float)next.v[j];
-                top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-            }
-            if (h + 1 < at.heads && at.d < a.tile.dim) next = load8<T>(from + (int64_t)(h + 1) * a.v_head, a.whole);
-            top = group_max(top);
-            if (at.d >= a.tile.dim) continue;
-            // the same number's leading word in 64 bits; numbers below 2^-126 get the least scale either way
-            const uint32_t b = top >= 0x7F800000u ? 255u : scale_of<T>((top >> 3) + ((1023u - 127u) << 20) | ((top & 7u) != 0));
-            put_values(to, a.tile, place, at.d, codes_of(x, __uint_as_float(b << 23)));
-            if ((at.d & 31u) == 0) to[a.tile.value_scale(place, at.d)] = (uint8_t)b;
-        }
-        return;
-    }
-    Keys<T> keys(a, at.d);
-    const char *from = a.k + (int64_t)at.token * a.k_token;
-    typename Keys<T>::Raw next = keys.request(a, from + (int64_t)at.head0 * a.k_head);
-    keys.factors(a, pos);
+    const bool in = at.d < a.tile.dim;
+    const char *from = at.values ? a.v + (int64_t)at.token * a.v_token : a.k + (int64_t)at.token * a.k_token;
+    const int64_t step = at.values ? a.v_head : a.k_head;
+    typedef Keys<T, (E > 1), kWithin> K;
+    K keys(a, at.d, at.values);
+    typename K::Raw next = keys.request(a, from + (int64_t)at.head0 * step);
+    if (!at.values) keys.factors(a, pos);
     for (uint32_t h = at.head0; h < at.heads; ++h) {
-        uint8_t *to = block + (int64_t)h * a.page_head;
-        double y[8];
-        const typename Keys<T>::Raw raw = next;
-        if (h + 1 < at.heads) next = keys.request(a, from + (int64_t)(h + 1) * a.k_head);
-        keys.values(a, raw, y);
+        float x[8];
+        const typename K::Raw raw = next;
+        if (h + 1 < at.heads) next = keys.request(a, from + (int64_t)(h + 1) * step);
+        if (at.values)                                 // uniform in a wave, of heads up to 128
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = (float)raw.x.v[j];
+        else keys.values(a, raw, x);
         uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint64_t u = __builtin_bit_cast(uint64_t, y[j]);
-            top = max(top, ((uint32_t)(u >> 32) & 0x7FFFFFFFu) | ((uint32_t)u != 0));
-        }
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
         top = group_max(top);
-        if (at.d >= a.tile.dim) continue;
-        const uint32_t b = scale_of<T>(top);
-        // rounded here, in 64 bits, to what the conversion then takes as it is
-        const double inverse = __builtin_bit_cast(double, (uint64_t)(1023u + 127u - b) << 52);
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double v = __builtin_fabs(y[j]) * inverse;
-            const double step = v < 2.0 ? 0.5 : v < 4.0 ? 1.0 : 2.0, back = v < 2.0 ? 2.0 : v < 4.0 ? 1.0 : 0.5;
-            x[j] = (float)__builtin_copysign(__builtin_rint(v * back) * step, y[j]);
-        }
-        *(uint32_t *)(to + a.tile.key(place, at.d)) = codes_of(x, 1.f);
-        if ((at.d & 31u) == 0) to[a.tile.key_scale(place, at.d)] = (uint8_t)b;
+        if (!in) continue;
+        const uint32_t b = scale_of<T>(top), codes = codes_of(x, __uint_as_float(b << 23));
+        uint8_t *to = block + (int64_t)h * a.page_head;
+        if (at.values) put_values(to, a.tile, place, at.d, codes);
+        else *(uint32_t *)(to + a.tile.key(place, at.d)) = codes;
+        if ((at.d & 31u) == 0) to[at.values ? a.tile.value_scale(place, at.d) : a.tile.key_scale(place, at.d)] = (uint8_t)b;
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) read_kernel(const PackedArgs a) {
+template <typename T, bool kWhole> __global__ void __launch_bounds__(kThreads) read_kernel(const PackedArgs a) {
     const Place at(a, a.first_group + blockIdx.x);
     if (!at.live || at.d >= a.tile.dim) return;
     const uint32_t slot = (uint32_t)a.slots[at.token], place = slot & (a.tile.block - 1u);
@@ -269,7 +293,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) read_kernel(co
         for (int j = 0; j < 8; ++j) x.v[j] = p[j / 2][j % 2];
         char *to = out + (int64_t)h * (at.values ? a.v_head : a.k_head);
         typedef uint32_t raw __attribute__((ext_vector_type(2 * sizeof(T)), aligned(16)));
-        if (a.whole) *(raw *)to = __builtin_bit_cast(raw, x);
+        if constexpr (kWhole) *(raw *)to = __builtin_bit_cast(raw, x);
         else
 #pragma unroll
             for (int j = 0; j < 8; ++j) ((T *)to)[j] = x.v[j];
@@ -307,10 +331,11 @@ template <typename T> hipError_t launch_append(PackedArgs &a, bool whole, hipStr
     });
 }
 
-template <typename T> hipError_t launch_read(PackedArgs &a, hipStream_t st) {
+template <typename T> hipError_t launch_read(PackedArgs &a, bool whole, hipStream_t st) {
     return seq_launches(a.kv_groups, [&](uint32_t first, uint32_t n) {
         a.first_group = first;
-        hipLaunchKernelGGL((read_kernel<T>), dim3(n), dim3(kThreads), 0, st, a);
+        if (whole) hipLaunchKernelGGL((read_kernel<T, true>), dim3(n), dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((read_kernel<T, false>), dim3(n), dim3(kThreads), 0, st, a);
     });
 }
 
@@ -357,8 +382,6 @@ hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, voi
     n.norm = r.norm != 0;
     SEQ_REQUIRE(norm_put(n, 0, r.q_heads, r.q, r.q_out, nullptr, size) && r.k.data && r.v.data && seq_aligned(r.k.data, size) && seq_aligned(r.v.data, size),
                 "q, q_out, k and v must be device pointers aligned to their type");
-    const bool whole = norm_whole(n, 2 * n.half, size);
-    norm_share(n, 0, 0xFFFFFFFFu);
     a.k = static_cast<const char *>(r.k.data);
     a.v = static_cast<const char *>(r.v.data);
     a.k_token = r.k.token_stride * size;
@@ -368,9 +391,12 @@ hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, voi
     a.slots = r.slots;
     a.k_weight = r.k_weight;
     a.eps = r.eps;
+    a.per_value = 1.0 / r.head_dim;
     a.kv_heads = r.kv_heads;
     put_pages(a, r.pages, r.head_dim);
-    a.whole = heads16(a.k, a.k_token, a.k_head) && heads16(a.v, a.v_token, a.v_head) && (n.interleaved || n.half % 8 == 0);
+    // vectors of eight keys, none of which holds pairs of two kinds
+    const bool whole = norm_whole(n, 2 * n.half, size, heads16(a.k, a.k_token, a.k_head) && heads16(a.v, a.v_token, a.v_head) && (n.interleaved ? 2 * n.half : n.half) % 8 == 0);
+    norm_share(n, 0, 0xFFFFFFFFu);
     share(a, r.n_tokens);
     const uint32_t tokens = (kThreads >> a.lane_bits) / 2;
     const uint64_t kv_groups = a.n_slots ? (uint64_t)((r.n_tokens + tokens - 1) / tokens) * a.head_groups : 0;
@@ -403,14 +429,14 @@ hps_status_t hps_seq_read_packed(const hps_seq_packed_t *pages, const int32_t *s
     a.slots = slots;
     a.kv_heads = kv_heads;
     put_pages(a, *pages, head_dim);
-    a.whole = heads16(a.k_out, a.k_token, a.k_head) && heads16(a.v_out, a.v_token, a.v_head);
+    const bool whole = heads16(a.k_out, a.k_token, a.k_head) && heads16(a.v_out, a.v_token, a.v_head);
     share(a, n_tokens);
     const uint32_t tokens = (kThreads >> a.lane_bits) / 2;
     const uint64_t groups = (uint64_t)((n_tokens + tokens - 1) / tokens) * a.head_groups;
     SEQ_REQUIRE(groups < (1ull << 32), "too many tokens and heads for one call");
     a.kv_groups = (uint32_t)groups;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    SEQ_TRY(dtype == HPS_SEQ_F32 ? launch_read<float>(a, st) : dtype == HPS_SEQ_F16 ? launch_read<_Float16>(a, st) : launch_read<__bf16>(a, st));
+    SEQ_TRY(dtype == HPS_SEQ_F32 ? launch_read<float>(a, whole, st) : dtype == HPS_SEQ_F16 ? launch_read<_Float16>(a, whole, st) : launch_read<__bf16>(a, whole, st));
     return HPS_OK;
 }
 

@@ -152,6 +152,20 @@ def test_roundings():
                 c.check()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_keys_next_to_a_border(interleaved):
+    """Keys that lie 2^-28 and less beside the middle of two codes, or of two scales, further than 32 bits tell: rounded as in 64."""
+    D, middles = 64, torch.tensor([.25, .75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0])
+    for largest in (6.0, 7.0):                         # 7 with something more has the next scale
+        for off in (2.0 ** -28, -2.0 ** -28, 2.0 ** -40, -2.0 ** -40, 2.0 ** -52, 0.0):
+            c = Case(BF, 1, 0, 1, D, 16, D, norm=False, seed=11)
+            c.row[:] = 1
+            cos = middles.repeat(4).clamp(max=largest)
+            c.table = torch.stack((cos, torch.full_like(cos, off)), -1)[None]           # values middle - off, and middle + off of the partners
+            c.positions[:] = 0
+            c.check(interleaved)
+
+
 @pytest.mark.parametrize("dtype", [F32, HF, BF])
 def test_sizes_of_values(dtype):
     """Groups at the ends of what a type holds; one that is not finite leaves its neighbours alone."""
