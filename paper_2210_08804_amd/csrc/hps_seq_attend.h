@@ -7,6 +7,18 @@
 
 #include "hps_seq_common.h"
 
+// Division of a number below 2^31 by one that the host knows: one of the device's own takes some 40 instructions, and a work-group has five
+// in front of its first load.
+struct SeqDivisor {
+    uint32_t d, m, s;
+    static SeqDivisor of(uint32_t d) {
+        uint32_t s = 0;
+        while (s < 31 && (1u << s) < d) ++s;
+        return {d, (uint32_t)((((1ull << s) - d) << 32) / d + 1), s};
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return (__umulhi(m, x) + x) >> s; }
+};
+
 struct SeqAttendArgs {
     const char *q, *k, *v;
     char *out;
@@ -23,6 +35,7 @@ struct SeqAttendArgs {
     uint32_t first_group;                              // of this launch
     int32_t history_wide, own_mode, direct;            // direct: one part only, results go straight out
     float c;                                           // scale * log2(e)
+    SeqDivisor by_kv_heads, by_ratio, by_history_tiles, by_history_combos, by_history_chunks, by_own_chunks, by_own_tiles;
     int64_t packed_block;                              // packed pages: block stride in bytes; page_head is the heads', k the tiles
 };
 
@@ -137,6 +150,7 @@ struct Item {
     uint32_t token0, row0, rows;                       // the tile's rows are row0 .. of `rows` (token, head) pairs from token0 on
     uint32_t head, part;                               // key/value head; part that the result is
     int32_t causal_from;                               // row's query i sees keys below causal_from + i; or kAll
+    int32_t id0, id1;                                  // blocks of the first 32 keys of the wave, read ahead of the lengths (a place that the table holds)
 };
 constexpr int32_t kAll = 0x7FFFFFFF;
 
@@ -610,28 +624,43 @@ __device__ __forceinline__ uint32_t length(const Args &a, int32_t x, uint32_t wi
     return min(n, fits);
 }
 
+// Reads the blocks of the first 32 keys that a wave of few rows has.
+__device__ __forceinline__ void first_blocks(const Args &a, Item &it, uint32_t width, uint32_t wave) {
+    if (width == 0) {
+        it.id0 = it.id1 = -1;
+        return;
+    }
+    const uint32_t at = it.first + 32 * wave, last = width - 1;
+    it.id0 = scalar(it.table, min(at >> a.sh, last));
+    it.id1 = scalar(it.table, min((at + 16) >> a.sh, last));
+}
+
 // The work of one work-group, or of one of its waves where each has its own (solo).  false: none, and what it would leave is marked.
-template <uint32_t kWide, uint32_t kNarrow>
+template <uint32_t kWide, uint32_t kNarrow, bool kAhead>                  // kAhead: the first blocks are read too
 __device__ __forceinline__ bool item_of(const Args &a, uint32_t group, uint32_t wave, uint32_t lane, Item &it, bool &is_wide, bool &solo) {
     solo = false;
     if (group < a.history_groups) {
         // Work-groups of one (group, chunk, head) read the same keys: they go to one XCD (workgroups are dealt to the eight in turn).
         uint32_t combo, tile;
         if (a.history_combos >= 8) {
-            const uint32_t y = group >> 3;
-            combo = (group & 7u) + 8 * (y / a.history_tiles);
-            tile = y % a.history_tiles;
+            const uint32_t y = group >> 3, q = a.by_history_tiles.quotient(y);
+            combo = (group & 7u) + 8 * q;
+            tile = y - q * a.history_tiles;
             if (combo >= a.history_combos) return false;
         } else {
-            combo = group % a.history_combos;
-            tile = group / a.history_combos;
+            tile = a.by_history_combos.quotient(group);
+            combo = group - tile * a.history_combos;
         }
         // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
         // side by side, one head's rows are in few of the L2's channels.
         // From group to group the chunks do: where histories end at different lengths, the last chunks have little to do, and must not
         // all be one XCD's (26 groups of 187 to 3,000 keys, two heads of 64, 4 chunks 50.6 -> 42.8 us, 8 chunks 51.7 -> 48.6).
-        const uint32_t rest = combo / a.kv_heads, g = rest / a.history_chunks, chunk = (rest + g) % a.history_chunks;
-        it.head = (combo + rest) % a.kv_heads;
+        const uint32_t rest = a.by_kv_heads.quotient(combo), g = a.by_history_chunks.quotient(rest), turned = rest + g, chunk = turned - a.by_history_chunks.quotient(turned) * a.history_chunks;
+        it.head = combo + rest - a.by_kv_heads.quotient(combo + rest) * a.kv_heads;
+        it.table = a.prefix_table + (size_t)g * a.prefix_width;
+        it.first = chunk * a.history_chunk;
+        if (kAhead) first_blocks(a, it, a.prefix_width, a.history_wide ? 0 : wave);
+        const int32_t prefix = scalar(a.prefix_lens, g);
         const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
         const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
         const uint32_t n = t1 > t0 ? t1 - t0 : 0;
@@ -641,9 +670,7 @@ __device__ __forceinline__ bool item_of(const Args &a, uint32_t group, uint32_t 
         it.rows = min(n, a.max_group) * a.ratio;
         it.row0 = tile * (is_wide ? kWide : kNarrow);
         if (it.row0 >= it.rows) return false;
-        it.table = a.prefix_table + (size_t)g * a.prefix_width;
-        it.first = chunk * a.history_chunk;
-        it.end = min(length(a, scalar(a.prefix_lens, g), a.prefix_width, a.max_prefix), it.first + a.history_chunk);
+        it.end = min(length(a, prefix, a.prefix_width, a.max_prefix), it.first + a.history_chunk);
         it.causal_from = kAll;
         it.part = chunk;
     } else {
@@ -654,11 +681,15 @@ __device__ __forceinline__ bool item_of(const Args &a, uint32_t group, uint32_t 
             x = x * kWaves + wave;
             if (x >= a.own_items) return false;              // no wave of a solo work-group waits for another
         }
-        it.head = x % a.kv_heads;
-        uint32_t rest = x / a.kv_heads;
-        const uint32_t chunk = rest % a.own_chunks;
-        rest /= a.own_chunks;
-        const uint32_t tile = rest % a.own_tiles, r = rest / a.own_tiles;
+        const uint32_t rest = a.by_kv_heads.quotient(x), tiles = a.by_own_chunks.quotient(rest), r = a.by_own_tiles.quotient(tiles), turn = rest - tiles * a.own_chunks, tile = tiles - r * a.own_tiles;
+        it.head = x - rest * a.kv_heads;
+        // The chunks are dealt anew to each request: where lengths differ, the last ones have little to do, and work-groups a fixed number
+        // apart share a CU.
+        const uint32_t dealt = turn + (r * 0x9E3779B9u >> 24), chunk = dealt - a.by_own_chunks.quotient(dealt) * a.own_chunks;
+        it.table = a.block_table + (size_t)r * a.table_width;
+        it.first = chunk * a.own_chunk;
+        if (kAhead) first_blocks(a, it, a.table_width, solo || is_wide ? 0 : wave);
+        const int32_t own = scalar(a.lens, r);
         const uint32_t t0 = clamp_to(scalar(a.token_offsets, r), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r + 1), a.n_tokens);
         const uint32_t n = t1 > t0 ? t1 - t0 : 0, tile_rows = is_wide ? kWide : kNarrow;
         if (n > a.max_new) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
@@ -666,11 +697,9 @@ __device__ __forceinline__ bool item_of(const Args &a, uint32_t group, uint32_t 
         it.rows = min(n, a.max_new) * a.ratio;
         it.row0 = tile * tile_rows;
         if (it.row0 >= it.rows) return false;
-        const uint32_t len = length(a, scalar(a.lens, r), a.table_width, a.max_len);
-        it.table = a.block_table + (size_t)r * a.table_width;
-        it.first = chunk * a.own_chunk;
+        const uint32_t len = length(a, own, a.table_width, a.max_len);
         // places by all of the request's new tokens: queries may end inside it
-        const int32_t from = (int32_t)len - (scalar(a.token_offsets, r + 1) - (int32_t)t0) + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
+        const int32_t from = (int32_t)len - (scalar(a.token_offsets, r + 1) - (int32_t)t0) + 1, last = from + (int32_t)(a.by_ratio.quotient(min(it.rows, it.row0 + tile_rows) - 1));        // keys that the tile's last row sees
         it.causal_from = n > 1 ? from : kAll;
         it.end = min((uint32_t)max(last, 0), it.first + a.own_chunk);
         it.part = a.history_chunks + chunk;

@@ -35,7 +35,7 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
     const uint32_t group = a.first_group + blockIdx.x;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, kNarrowRows>(a, group, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<kWideRows, kNarrowRows, false>(a, group, wave, lane, it, is_wide, solo)) return;
     if (is_wide) {
         E e(a, it, lds_base, 32 * wave);
         e.wide();
@@ -285,6 +285,14 @@ hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const
     SEQ_REQUIRE(history_groups + own_groups < (1ull << 31) && own_items < (1ull << 31), "too many requests, heads and chunks for one launch");
     a.history_groups = (uint32_t)history_groups;
     a.own_items = (uint32_t)own_items;
+    const auto divisor = [](uint32_t d) { return SeqDivisor::of(d ? d : 1); };
+    a.by_kv_heads = divisor(a.kv_heads);
+    a.by_ratio = divisor(a.ratio);
+    a.by_history_tiles = divisor(a.history_tiles);
+    a.by_history_combos = divisor(a.history_combos);
+    a.by_history_chunks = divisor(a.history_chunks);
+    a.by_own_chunks = divisor(a.own_chunks);
+    a.by_own_tiles = divisor(a.own_tiles);
     parts = a.history_chunks + a.own_chunks;
     a.direct = parts == 1;
     groups = (uint32_t)(history_groups + own_groups);

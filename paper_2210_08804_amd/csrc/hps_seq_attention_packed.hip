@@ -48,6 +48,12 @@ template <typename T, typename F> __device__ __forceinline__ F eight(uint32_t x,
     return __builtin_bit_cast(F, u32x4{two<T>(x, s, 0), two<T>(x, s, 1), two<T>(x, s, 2), two<T>(x, s, 3)});
 }
 
+// The highest bit of each byte of x that is the scale of no number.
+template <typename T> __device__ __forceinline__ uint32_t odd_bytes(uint32_t x) {
+    constexpr uint32_t k = (0x7Fu - (kPackedMost<T> & 0x7Fu)) * 0x01010101u;
+    return ((x & 0x7F7F7F7Fu) + k) & x & 0x80808080u;
+}
+
 // How many scales a lane's numbers have: of 8 G neighbours of a key, of 2 G of a value.
 template <int G> constexpr int kKeyScales = G == 3 ? 3 : G == 8 ? 2 : 1;
 template <int G> constexpr int kValueScales = G == 3 ? 3 : 1;
@@ -83,7 +89,10 @@ template <typename T, int G, int NT> struct Few {
     struct Raw {
         uint32_t k[2][G], ks[2][KS], v[2 * G];
         uint32_t vs[VS][2];
+        bool bad0, bad1;                               // of the first and of the second 16: their block is none
     };
+    // Where 32 keys begin, and their blocks.  Beyond the end: the first ones again, so that there always are loads under way to count.
+    struct Where { uint32_t at; int32_t id0, id1; };
 
     const Args &a;
     const Item it;
@@ -93,6 +102,7 @@ template <typename T, int G, int NT> struct Few {
     f32x4 o[NT][2 * G];
     float m[NT], l[NT];
     int32_t limit[NT];
+    uint32_t poison[NT];                               // bit 4 x + j: the row saw a value that is no number in the lane's scale x, numbers j
     uint32_t k_off, v_off, ks_off[KS], vs_off[VS];
 
     __device__ __forceinline__ Few(const Args &args, const Item &item)
@@ -106,7 +116,7 @@ template <typename T, int G, int NT> struct Few {
         for (int x = 0; x < VS; ++x) vs_off[x] = (g & 1u) * (8 * G) + value_group<G>(n, x) * 8;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const uint32_t row = it.row0 + 16 * t + n, i = row / a.ratio;
+            const uint32_t row = it.row0 + 16 * t + n, i = a.by_ratio.quotient(row);
             const bool there = row < it.rows;
             limit[t] = !there ? kAll : it.causal_from == kAll ? (int32_t)it.end : min((int32_t)it.end, it.causal_from + (int32_t)i);
             const char *src = a.q + (int64_t)(it.token0 + i) * a.q_token + (int64_t)(it.head * a.ratio + (row - i * a.ratio)) * a.q_head + g * (16 * G);
@@ -120,17 +130,23 @@ template <typename T, int G, int NT> struct Few {
             for (int i2 = 0; i2 < 2 * G; ++i2) o[t][i2] = f32x4{0, 0, 0, 0};
             m[t] = -kInf;
             l[t] = 0.f;
+            poison[t] = 0;
         }
     }
 
-    __device__ __forceinline__ int32_t block_of(uint32_t at) const { return at < it.end ? scalar(it.table, at >> a.sh) : -1; }
+    __device__ __forceinline__ Where where(uint32_t x, uint32_t from) const {
+        const uint32_t at = x < it.end ? x : from, second = at + 16 < it.end ? at + 16 : at;
+        return {at, scalar(it.table, at >> a.sh), scalar(it.table, second >> a.sh)};
+    }
 
-    // Requests 32 keys and values from `at` on (a multiple of 16; at < it.end), in blocks id0 and id1.  Behind the end of the keys, and in the place of a
-    // block that is none, something else of the pages comes: hidden later, or made zeros here.
-    __device__ __forceinline__ void load(Raw &r, uint32_t at, int32_t id0, int32_t id1) const {
-        const bool bad0 = (uint32_t)id0 >= a.n_blocks, more = at + 16 < it.end, bad1 = more && (uint32_t)id1 >= a.n_blocks;
-        const uint32_t block = 1u << a.sh, p0 = at & (block - 1u), p1 = more ? (at + 16) & (block - 1u) : p0;
-        const char *t0 = tiles + (int64_t)(bad0 ? 0 : id0) * a.packed_block, *t1 = more ? tiles + (int64_t)(bad1 ? 0 : id1) * a.packed_block : t0;
+    // Requests 32 keys and values (from a multiple of 16 below the end).  Behind the end of the keys, and in the place of a block that is
+    // none, something else of the pages comes: hidden, or made zeros, in front of its use.
+    __device__ __forceinline__ void load(Raw &r, const Where &w) const {
+        const bool more = w.at + 16 < it.end;
+        r.bad0 = (uint32_t)w.id0 >= a.n_blocks;
+        r.bad1 = (uint32_t)w.id1 >= a.n_blocks;        // without a second 16: the first one's
+        const uint32_t block = 1u << a.sh, p0 = w.at & (block - 1u), p1 = more ? (w.at + 16) & (block - 1u) : p0;
+        const char *t0 = tiles + (uint64_t)(uint32_t)(r.bad0 ? 0 : w.id0) * (uint64_t)a.packed_block, *t1 = tiles + (uint64_t)(uint32_t)(r.bad1 ? 0 : w.id1) * (uint64_t)a.packed_block;
         const char *c0 = t0 + p0 * (16 * G), *c1 = t1 + p1 * (16 * G), *s0 = t0 + block * (32 * G) + p0 * G, *s1 = t1 + block * (32 * G) + p1 * G;
         const char *kc = (n & 8u ? c1 : c0) + k_off, *vc = (g & 2u ? c1 : c0) + block * (16 * G) + v_off;
         const char *ks = n & 8u ? s1 : s0, *vs = (g & 2u ? s1 : s0) + block * G;
@@ -143,23 +159,25 @@ template <typename T, int G, int NT> struct Few {
         load_words<2 * G, (G % 2 == 0 ? 16 : 8)>(vc, r.v);
 #pragma unroll
         for (int x = 0; x < VS; ++x) load_words<2, 8>(vs + vs_off[x], r.vs[x]);
-        if (__builtin_expect(bad0 || bad1, 0)) {
-            if (lane == 0) atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
-            const bool no_key = n & 8u ? bad1 : bad0, no_value = g & 2u ? (more ? bad1 : bad0) : bad0;
+    }
+
+    // A block that is none stands for zeros.
+    __device__ __forceinline__ void zeros(Raw &r) const {
+        if (lane == 0) atomicOr(a.flags, HPS_SEQ_FLAG_BLOCK);
+        const bool no_key = n & 8u ? r.bad1 : r.bad0, no_value = g & 2u ? r.bad1 : r.bad0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int x = 0; x < G; ++x) r.k[j][x] = no_key ? 0u : r.k[j][x];
+            for (int x = 0; x < G; ++x) r.k[j][x] = no_key ? 0u : r.k[j][x];
 #pragma unroll
-                for (int x = 0; x < KS; ++x) r.ks[j][x] = no_key ? 0u : r.ks[j][x];
-            }
+            for (int x = 0; x < KS; ++x) r.ks[j][x] = no_key ? 0u : r.ks[j][x];
+        }
 #pragma unroll
-            for (int x = 0; x < 2 * G; ++x) r.v[x] = no_value ? 0u : r.v[x];
+        for (int x = 0; x < 2 * G; ++x) r.v[x] = no_value ? 0u : r.v[x];
 #pragma unroll
-            for (int x = 0; x < VS; ++x) {
-                r.vs[x][0] = no_value ? 0u : r.vs[x][0];
-                r.vs[x][1] = no_value ? 0u : r.vs[x][1];
-            }
+        for (int x = 0; x < VS; ++x) {
+            r.vs[x][0] = no_value ? 0u : r.vs[x][0];
+            r.vs[x][1] = no_value ? 0u : r.vs[x][1];
         }
     }
 
@@ -171,8 +189,9 @@ template <typename T, int G, int NT> struct Few {
         m[t] = next;
     }
 
-    // 32 keys and values from `at` on, of which some rows may not see some where `edge`.
+    // 32 keys and values from `at` on.
     __device__ __forceinline__ void step(Raw &r, uint32_t at, uint32_t least) {
+        if (__builtin_expect(r.bad0 || r.bad1, 0)) zeros(r);
         f32x4 s[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f32x4{0, 0, 0, 0};
@@ -188,8 +207,17 @@ template <typename T, int G, int NT> struct Few {
                 for (int t = 0; t < NT; ++t) s[t][j] = Type16<T>::mfma(k, q[t][i], s[t][j]);
             }
         }
-        const bool edge = at + 32 > least;             // uniform
-        if (edge) hide_all(s, r, at);
+        const bool edge = at + 32 > least;             // uniform: some rows do not see some keys
+        uint32_t seen[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) seen[t] = 255u;
+        if (edge) hide(s, r, at, seen);
+        uint32_t odd[VS][2], any = 0;
+#pragma unroll
+        for (int x = 0; x < VS; ++x)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) any |= odd[x][i] = odd_bytes<T>(r.vs[x][i]);
+        if (__builtin_expect(__ballot(any != 0) != 0, 0)) spoil(r, odd, edge, seen);
         frag w[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -209,21 +237,10 @@ template <typename T, int G, int NT> struct Few {
             l[t] += sum;
         }
         float f[VS][8];
-        uint32_t largest = 0;
 #pragma unroll
         for (int x = 0; x < VS; ++x)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t b = r.vs[x][i / 4] >> 8 * (i % 4) & 255u;
-                largest = max(largest, b);
-                f[x][i] = __uint_as_float(b << 23);
-            }
-        if (__builtin_expect(__ballot(largest > kPackedMost<T>) != 0, 0)) {
-#pragma unroll
-            for (int x = 0; x < VS; ++x)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[x][i] = packed_scale<T>(__float_as_uint(f[x][i]) >> 23);
-        }
+            for (int i = 0; i < 8; ++i) f[x][i] = __uint_as_float((r.vs[x][i / 4] >> 8 * (i % 4) & 255u) << 23);
 #pragma unroll
         for (int p = 0; p < G; ++p) {                  // the lane's numbers 2 p and 2 p + 1 of its eight tokens
             u32x4 even, odd;
@@ -242,52 +259,64 @@ template <typename T, int G, int NT> struct Few {
         }
     }
 
-    // Hides the scores that a row does not see.  A hidden value must not meet the weight 0 if it is no number: values behind the end get
-    // the scale 0, and where a value that some rows see is no number, those rows' results become NaN here and the product takes a 0.
-    __device__ __forceinline__ void hide_all(f32x4 (&s)[NT][2], Raw &r, uint32_t at) {
-        const uint32_t first = at + 8 * g;
-        uint32_t seen[NT];
+    // Hides the scores that a row does not see, and values behind the end: their scales become 0, as the weights that they meet are.
+    __device__ __forceinline__ void hide(f32x4 (&s)[NT][2], Raw &r, uint32_t at, uint32_t (&seen)[NT]) const {
+        const int32_t first = (int32_t)(at + 8 * g);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            seen[t] = 0;
+            const int32_t many = min(max(limit[t] - first, 0), 8);
+            seen[t] = (1u << many) - 1u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool see = (int32_t)(first + i) < limit[t];
-                seen[t] |= see ? 1u << i : 0u;
-                s[t][i / 4][i % 4] = see ? s[t][i / 4][i % 4] : -kInf;
-            }
+            for (int i = 0; i < 8; ++i) s[t][i / 4][i % 4] = i < many ? s[t][i / 4][i % 4] : -kInf;
         }
-        uint32_t bad = 0;
+        const int32_t there = min(max((int32_t)it.end - first, 0), 8);
+        const uint32_t low = there >= 4 ? ~0u : (1u << 8 * there) - 1u, high = there >= 8 ? ~0u : there <= 4 ? 0u : (1u << 8 * (there - 4)) - 1u;
+#pragma unroll
+        for (int x = 0; x < VS; ++x) {
+            r.vs[x][0] &= low;
+            r.vs[x][1] &= high;
+        }
+    }
+
+    // Some values are no numbers.  Where all rows see all keys the product shows it, from a scale that is NaN.  A hidden value must not meet
+    // its weight 0 like that: there the product takes a 0, and the rows that see the value are told by `poison`.
+    __device__ __forceinline__ void spoil(Raw &r, const uint32_t (&odd)[VS][2], bool edge, const uint32_t (&seen)[NT]) {
 #pragma unroll
         for (int x = 0; x < VS; ++x)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t shift = 8 * (i % 4), b = r.vs[x][i / 4] >> shift & 255u;
-                if (first + i >= it.end) r.vs[x][i / 4] &= ~(255u << shift);
-                else if (b > kPackedMost<T>) {
-                    bad |= 1u << (8 * x + i);
-                    r.vs[x][i / 4] &= ~(255u << shift);
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t bytes = (odd[x][i] >> 7) * 255u;
+                r.vs[x][i] = edge ? r.vs[x][i] & ~bytes : r.vs[x][i] | bytes;
+            }
+        if (!edge) return;
+#pragma unroll
+        for (int x = 0; x < VS; ++x)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t left = odd[x][i] >> 7;
+#pragma unroll 1
+                for (int e = 4 * i; e < 4 * i + 4; ++e, left >>= 8) {       // token e of each eight
+                    const uint64_t who = __ballot(left & 1u);               // lanes that hold values: number c of 16, eight tokens g
+                    if (!who) continue;
+#pragma unroll
+                    for (int oct = 0; oct < 4; ++oct)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const bool see = __shfl(seen[t], 16 * oct + (int)n) >> e & 1u;
+                            poison[t] |= see ? ((uint32_t)(who >> (16 * oct + 4 * g)) & 15u) << 4 * x : 0u;
+                        }
                 }
             }
-        if (__builtin_expect(__ballot(bad != 0) == 0, 1)) return;
-#pragma unroll 1
-        for (int e = 0; e < 8 * VS; ++e) {             // token e % 8 of each eight, scale e / 8 of the lanes that hold values
-            const uint64_t who = __ballot(bad >> e & 1u);
-            if (!who) continue;
+    }
+    __device__ __forceinline__ void poisoned() {
 #pragma unroll
-            for (int oct = 0; oct < 4; ++oct)
+        for (int t = 0; t < NT; ++t)
+            if (__builtin_expect(__ballot(poison[t] != 0) != 0, 0))
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const bool see = __shfl(seen[t], 16 * oct + (int)n) >> (e & 7) & 1u;
+                for (int i = 0; i < 2 * G; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const bool poisoned = see && (who >> (16 * oct + 4 * g + j) & 1u);
-#pragma unroll
-                        for (int i = 0; i < 2 * G; ++i)
-                            if (VS == 1 || i / 2 == (e >> 3)) o[t][i][j] = poisoned ? __builtin_nanf("") : o[t][i][j];
-                    }
-                }
-        }
+                    for (int j = 0; j < 4; ++j)
+                        if (poison[t] >> (4 * value_scale<G>(i / 2) + j) & 1u) o[t][i][j] = __builtin_nanf("");
     }
 
     __device__ __forceinline__ uint32_t least_limit() const {               // over the wave's rows
@@ -298,27 +327,28 @@ template <typename T, int G, int NT> struct Few {
         return uniform((uint32_t)x);
     }
 
-    // Every `stride`-th 32 keys from `from` on, the next ones' codes under way.
+    // Every `stride`-th 32 keys from `from` on, the next ones' codes under way, the blocks of those behind them too.
     __device__ __forceinline__ void run(uint32_t from, uint32_t stride) {
         if (from >= it.end) return;
         const uint32_t least = least_limit();
         Raw here, there;
-        load(here, from, block_of(from), block_of(from + 16));
-        int32_t id0 = block_of(from + stride), id1 = block_of(from + stride + 16);
-        for (uint32_t at = from;;) {
-            uint32_t next = at + stride;
-            if (next < it.end) load(there, next, id0, id1);
-            id0 = block_of(next + stride);
-            id1 = block_of(next + stride + 16);
+        load(here, Where{from, it.id0, from + 16 < it.end ? it.id1 : it.id0});
+        Where next = where(from + stride, from);
+        uint32_t at = from, left = (it.end - from + stride - 1) / stride;
+        // Two steps a turn, with one way out: a second one in the middle has the compiler wait there for loads that are to stay under way.
+#pragma unroll 1
+        for (; left >= 2; left -= 2) {
+            load(there, next);
+            next = where(at + 2 * stride, from);
             step(here, at, least);
-            if (next >= it.end) return;
-            at = next + stride;
-            if (at < it.end) load(here, at, id0, id1);
-            id0 = block_of(at + stride);
-            id1 = block_of(at + stride + 16);
-            step(there, next, least);
-            if (at >= it.end) return;
+            at += stride;
+            load(here, next);
+            next = where(at + 2 * stride, from);
+            step(there, at, least);
+            at += stride;
         }
+        if (left) step(here, at, least);
+        poisoned();
     }
 
     // The lane's 8 G neighbours of a row, from number 8 G g on.
@@ -344,7 +374,7 @@ template <typename T, int G, int NT> struct Few {
         }
     };
     __device__ __forceinline__ Place place(uint32_t row, float ref, float sum, bool first) const {
-        const uint32_t i = row / a.ratio, h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
+        const uint32_t i = a.by_ratio.quotient(row), h = it.head * a.ratio + (row - i * a.ratio), t = it.token0 + i;
         const size_t at = (size_t)t * a.q_heads + h, part = (size_t)it.part * a.n_tokens * a.q_heads + at;
         if (first) {
             if (!a.direct) a.part_ml[part] = make_float2(ref, sum);
@@ -407,22 +437,20 @@ template <typename T, int G, int NT> struct Few {
 template <typename T, int G> struct Wide : Engine<T, G, true> {
     typedef Engine<T, G, true> E;
     typedef typename E::frag frag;
+    typedef __attribute__((address_space(3))) uint32_t lds1;
+    typedef __attribute__((address_space(3))) u32x2 lds2;
+    typedef __attribute__((address_space(3))) u32x4 lds4;
     static constexpr int KS = kKeyScales<G>, VS = kValueScales<G>;
-    // The codes and scales of a lane's share of 16 keys (8 G neighbours of one) and of 16 values (2 G numbers of four).
-    struct Raw {
-        uint32_t k[G], ks[KS], v[G], vs[VS];
-        bool has_key, has_value;
-    };
-    const char *const tiles;
-    uint32_t k_off, v_off, key_row, value_row;
+    // A wave's share of a step as the pages hold it, 16 keys and 16 values: codes of keys, of values, scales of keys, of values.
+    static constexpr uint32_t kCodes = 256 * G, kKeyScalesAt = 2 * kCodes, kValueScalesAt = kKeyScalesAt + 16 * G, kRaw = kValueScalesAt + 16 * G;
+    static constexpr uint32_t kLds = E::kLds + 4 * kRaw;
 
-    __device__ __forceinline__ Wide(const Args &args, const Item &item, uint32_t lds_base, uint32_t first_row)
-        : E(args, item, lds_base, first_row), tiles(args.k + (int64_t)item.head * args.page_head) {
-        key_row = this->lane >> 2;
-        value_row = 8 * (this->lane >> 5) + 4 * (this->lane & 1u);
-        k_off = key_row * (16 * G) + (this->lane & 3u) * (4 * G);
-        v_off = (this->lane >> 5) * (128 * G) + (this->lane >> 1 & 15u) * (8 * G) + (this->lane & 1u) * (4 * G);
-    }
+    const char *const tiles;
+    const uint32_t raw;
+    bool has_key, has_value;                           // whether what is under way is there: its block is one
+
+    __device__ __forceinline__ Wide(const Args &args, const Item &item, uint32_t lds_base, uint32_t wave)
+        : E(args, item, lds_base, 32 * wave), tiles(args.k + (int64_t)item.head * args.page_head), raw(lds_base + E::kLds + wave * kRaw), has_key(false), has_value(false) {}
 
     // Block of the 16 tokens from `at` on: true if it is one, false (and a flag, within the length) if not.
     __device__ __forceinline__ bool valid(uint32_t at, int32_t id) const {
@@ -430,58 +458,96 @@ template <typename T, int G> struct Wide : Engine<T, G, true> {
         if (at < this->it.end && this->lane == 0) atomicOr(this->a.flags, HPS_SEQ_FLAG_BLOCK);
         return false;
     }
-    __device__ __forceinline__ void fetch_keys(Raw &r, uint32_t at, int32_t id) const {
-        r.has_key = valid(at, id);
-        if (!r.has_key) return;
-        const uint32_t block = 1u << this->a.sh, p = at & (block - 1u);
-        const char *t = tiles + (int64_t)id * this->a.packed_block;
-        load_words<G, (G % 4 == 0 ? 16 : 4 * (G & 3))>(t + p * (16 * G) + k_off, r.k);
+    // kBytes, a multiple of 16, from an address that all lanes share to LDS.
+    template <uint32_t kBytes> __device__ __forceinline__ void fetch(const char *from, uint32_t to) const {
 #pragma unroll
-        for (int x = 0; x < KS; ++x) r.ks[x] = *(const uint8_t *)(t + block * (32 * G) + (p + key_row) * G + key_group<G>(this->lane & 3u, x));
+        for (uint32_t i = 0; i < kBytes; i += 1024)
+            if (kBytes - i >= 1024 || this->lane * 16 < kBytes - i) load_to_lds(from + i, this->lane * 16, to + i);
     }
-    __device__ __forceinline__ void fetch_values(Raw &r, uint32_t at, int32_t id) const {
-        r.has_value = valid(at, id);
-        if (!r.has_value) return;
+    __device__ __forceinline__ void fetch_keys(uint32_t at, int32_t id) {
+        has_key = valid(at, id);
+        if (!has_key) return;
         const uint32_t block = 1u << this->a.sh, p = at & (block - 1u);
-        const char *t = tiles + (int64_t)id * this->a.packed_block;
-        load_words<G, (G % 4 == 0 ? 16 : 4 * (G & 3))>(t + block * (16 * G) + p * (16 * G) + v_off, r.v);
-#pragma unroll
-        for (int x = 0; x < VS; ++x)
-            r.vs[x] = *(const uint32_t *)(t + block * (33 * G) + p * G + (this->lane >> 5) * (8 * G) + value_group<G>(this->lane >> 1 & 15u, x) * 8 + 4 * (this->lane & 1u));
+        const char *t = tiles + (uint64_t)(uint32_t)id * (uint64_t)this->a.packed_block;
+        fetch<kCodes>(t + p * (16 * G), raw);
+        fetch<16 * G>(t + block * (32 * G) + p * G, raw + kKeyScalesAt);
     }
-    // To rows of 16 bits in LDS, as Engine::load16 leaves them; zeros for a block that is none, and for values behind the end.
-    __device__ __forceinline__ void put_keys(const Raw &r, uint32_t to) const {
-        typedef __attribute__((address_space(3))) u32x4 lds4;
-        const uint32_t row = to + key_row * E::kRow, sw = E::sw_k(key_row);
+    __device__ __forceinline__ void fetch_values(uint32_t at, int32_t id) {
+        has_value = valid(at, id);
+        if (!has_value) return;
+        const uint32_t block = 1u << this->a.sh, p = at & (block - 1u);
+        const char *t = tiles + (uint64_t)(uint32_t)id * (uint64_t)this->a.packed_block;
+        fetch<kCodes>(t + block * (16 * G) + p * (16 * G), raw + kCodes);
+        fetch<16 * G>(t + block * (33 * G) + p * G, raw + kValueScalesAt);
+    }
+    template <int kWords> static __device__ __forceinline__ void read_words(uint32_t from, uint32_t (&to)[kWords]) {
+        if constexpr (kWords % 4 == 0) {
 #pragma unroll
-        for (int s = 0; s < G; ++s) {
-            u32x4 x = {0, 0, 0, 0};
-            if (r.has_key) x = __builtin_bit_cast(u32x4, eight<T, frag>(r.k[s], packed_scale<T>(r.ks[key_scale<G>(s)])));
-            *(lds4 *)(lds_char *)(uintptr_t)(row + ((G * (this->lane & 3u) + s) ^ sw) * 16) = x;
+            for (int i = 0; i < kWords; i += 4) {
+                const u32x4 x = *(const lds4 *)(lds_char *)(uintptr_t)(from + 4 * i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to[i + j] = x[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) to[i] = *(const lds1 *)(lds_char *)(uintptr_t)(from + 4 * i);
         }
     }
-    __device__ __forceinline__ void put_values(const Raw &r, uint32_t at, uint32_t to) const {
-        const uint32_t c = this->lane >> 1 & 15u;
+    // To rows of 16 bits, as Engine::load16 leaves them: a lane has 8 G neighbours of a key.  Zeros for a block that is none.
+    __device__ __forceinline__ void put_keys(uint32_t to) const {
+        const uint32_t key = this->lane >> 2, part = this->lane & 3u, row = to + key * E::kRow, sw = E::sw_k(key);
+        uint32_t k[G];
+        float f[KS];
+        read_words(raw + key * (16 * G) + part * (4 * G), k);
+#pragma unroll
+        for (int x = 0; x < KS; ++x)
+            f[x] = packed_scale<T>(*(const __attribute__((address_space(3))) uint8_t *)(lds_char *)(uintptr_t)(raw + kKeyScalesAt + key * G + key_group<G>(part, x)));
+        if (!has_key)
+#pragma unroll
+            for (int s = 0; s < G; ++s) k[s] = 0, f[key_scale<G>(s)] = 1.f;
+#pragma unroll
+        for (int s = 0; s < G; ++s) *(lds4 *)(lds_char *)(uintptr_t)(row + ((G * part + s) ^ sw) * 16) = __builtin_bit_cast(u32x4, eight<T, frag>(k[s], f[key_scale<G>(s)]));
+    }
+    // And 2 G numbers of four values.  Zeros behind the end too.
+    __device__ __forceinline__ void put_values(uint32_t at, uint32_t to) const {
+        const uint32_t c = this->lane >> 1 & 15u, first = 8 * (this->lane >> 5) + 4 * (this->lane & 1u);
+        uint32_t v[G], vs[VS], odd = 0;
+        read_words(raw + kCodes + (this->lane >> 5) * (128 * G) + c * (8 * G) + (this->lane & 1u) * (4 * G), v);
+#pragma unroll
+        for (int x = 0; x < VS; ++x) {
+            vs[x] = *(const lds1 *)(lds_char *)(uintptr_t)(raw + kValueScalesAt + (this->lane >> 5) * (8 * G) + value_group<G>(c, x) * 8 + 4 * (this->lane & 1u));
+            odd |= odd_bytes<T>(vs[x]);
+        }
+        const bool careful = !has_value || at + 16 > this->it.end;          // uniform
+        if (__builtin_expect(careful || __ballot(odd != 0) != 0, 0)) {
+            const int32_t there = has_value ? min(max((int32_t)this->it.end - (int32_t)(at + first), 0), 4) : 0;
+#pragma unroll
+            for (int x = 0; x < VS; ++x) vs[x] |= (odd_bytes<T>(vs[x]) >> 7) * 255u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i < there) continue;
+#pragma unroll
+                for (int x = 0; x < VS; ++x) vs[x] &= ~(255u << 8 * i);
+#pragma unroll
+                for (int p = 0; p < G; ++p) v[(i * G + p) / 4] &= ~(255u << 8 * ((i * G + p) % 4));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                  // tokens
-            const uint32_t t = value_row + i, row = to + t * E::kRow, sw = E::sw_v(t);
-            const bool there = r.has_value && at + t < this->it.end;
+            const uint32_t t = first + i, row = to + t * E::kRow, sw = E::sw_v(t);
             uint32_t x[G];
 #pragma unroll
             for (int p = 0; p < G; ++p) {
                 const int b = i * G + p;
-                x[p] = there ? two<T>(r.v[b / 4], packed_scale<T>(r.vs[value_scale<G>(p)] >> 8 * i & 255u), b % 4) : 0u;
+                x[p] = two<T>(v[b / 4], __uint_as_float((vs[value_scale<G>(p)] >> 8 * i & 255u) << 23), b % 4);
             }
             // 4 G bytes from byte 4 G c of the row on; chunks of 16 bytes change places
             if constexpr (G % 4 == 0) {
-                typedef __attribute__((address_space(3))) u32x4 lds4;
 #pragma unroll
                 for (int p = 0; p < G; p += 4) *(lds4 *)(lds_char *)(uintptr_t)(row + ((G / 4 * c + p / 4) ^ sw) * 16) = u32x4{x[p], x[p + 1], x[p + 2], x[p + 3]};
             } else if constexpr (G == 2) {
-                typedef __attribute__((address_space(3))) u32x2 lds2;
                 *(lds2 *)(lds_char *)(uintptr_t)(row + ((c >> 1) ^ sw) * 16 + (c & 1u) * 8) = u32x2{x[0], x[1]};
             } else {
-                typedef __attribute__((address_space(3))) uint32_t lds1;
 #pragma unroll
                 for (int p = 0; p < G; ++p) {
                     const uint32_t at4 = G * c + p;
@@ -491,37 +557,42 @@ template <typename T, int G> struct Wide : Engine<T, G, true> {
         }
     }
 
-    // Engine::wide, with a step's keys and values requested one step earlier, into registers, and converted to LDS while the step in front
-    // is computed.
+    // Engine::wide, with a step's keys and values brought to LDS one step earlier, as they are, and converted there at the start of the step in
+    // front of theirs.
     __device__ __forceinline__ void run() {
         const uint32_t wave = uniform(threadIdx.x >> 6), least = this->least_limit(), mine = 16 * wave;
         const Item &it = this->it;
         if (it.first >= it.end) return;                // uniform in the work-group, as are all meetings
         uint32_t at = it.first;                        // the step's first value; its first key is 32 further on
         uint32_t keys_to = this->lds + mine * E::kRow, values_to = keys_to + E::kWideValues, flip = E::kStage;
-        Raw r;
         // keys `first` .. + 32 go to the second half of the other place, as if they were the end of a step in front
         if (wave >= 2) {
-            fetch_keys(r, at + mine - 32, block_at(at + mine - 32));
-            put_keys(r, keys_to + E::kStage);
+            fetch_keys(at + mine - 32, block_at(at + mine - 32));
+            wait_loads<0>();
+            put_keys(keys_to + E::kStage);
+            wait_lds();
         }
-        fetch_keys(r, at + 32 + mine, block_at(at + 32 + mine));
-        fetch_values(r, at + mine, block_at(at + mine));
-        put_keys(r, keys_to);
-        put_values(r, at + mine, values_to);
-        fetch_keys(r, at + 96 + mine, block_at(at + 96 + mine));
-        fetch_values(r, at + 64 + mine, block_at(at + 64 + mine));
+        fetch_keys(at + 32 + mine, block_at(at + 32 + mine));
+        fetch_values(at + mine, block_at(at + mine));
+        wait_loads<0>();
+        put_keys(keys_to);
+        put_values(at + mine, values_to);
+        wait_lds();
+        fetch_keys(at + 96 + mine, block_at(at + 96 + mine));
+        fetch_values(at + 64 + mine, block_at(at + 64 + mine));
         int32_t key_id = block_at(at + 160 + mine), value_id = block_at(at + 128 + mine);
         meet();
         this->k_row += E::kStage;
         f32x16 s = this->template scores<32 * E::kRow>(), t;
         this->k_row -= E::kStage;
         auto start = [&] {                             // everybody is done with the last step's keys and values
+            wait_loads<0>();
             meet();
-            if (at + 96 < it.end) put_keys(r, keys_to + flip);
-            if (at + 64 < it.end) put_values(r, at + 64 + mine, values_to + flip);
-            if (at + 160 < it.end) fetch_keys(r, at + 160 + mine, key_id);
-            if (at + 128 < it.end) fetch_values(r, at + 128 + mine, value_id);
+            if (at + 96 < it.end) put_keys(keys_to + flip);
+            if (at + 64 < it.end) put_values(at + 64 + mine, values_to + flip);
+            wait_lds();                                // the wave has read its share: the next one may come
+            if (at + 160 < it.end) fetch_keys(at + 160 + mine, key_id);
+            if (at + 128 < it.end) fetch_values(at + 128 + mine, value_id);
             key_id = block_at(at + 224 + mine);
             value_id = block_at(at + 192 + mine);
             this->fresh();
@@ -579,14 +650,17 @@ template <typename T, int G> struct Wide : Engine<T, G, true> {
     __device__ __forceinline__ int32_t block_at(uint32_t at) const { return at < this->it.end ? scalar(this->it.table, at >> this->a.sh) : -1; }
 };
 
+// Waves of a SIMD that the registers of few rows leave room for: work-groups of a CU.
+template <int G, int NT> constexpr int kFewBeside = NT == 1 ? (G == 8 ? 2 : G >= 3 ? 3 : 4) : G >= 3 ? 2 : G == 2 ? 3 : 4;
+
 // Work-groups of few rows alone: 16 * NT of an item.
-template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads, 2) packed_few_kernel(const Args a) {
+template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads, (kFewBeside<G, NT>)) packed_few_kernel(const Args a) {
     typedef Few<T, G, NT> F;
     extern __shared__ __align__(16) char shared[];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, 16 * NT>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<kWideRows, 16 * NT, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
     F e(a, it);
     e.run(solo ? it.first : it.first + 32 * wave, solo ? 32 : 32 * kWaves);
     if (solo) e.finish();
@@ -601,9 +675,9 @@ template <typename T, int G> __global__ void __launch_bounds__(kThreads, G <= 4 
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, 16>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<kWideRows, 16, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
     if (is_wide) {
-        W e(a, it, (uint32_t)(uintptr_t)(lds_char *)shared, 32 * wave);
+        W e(a, it, (uint32_t)(uintptr_t)(lds_char *)shared, wave);
         e.run();
         e.finish(32 * wave);
     } else {
@@ -652,9 +726,9 @@ template <typename T> hipError_t launch(Args &a, int kind, uint32_t groups, hipS
 }
 
 bool wide_rows(uint64_t rows, uint32_t) { return rows > 32; }
-uint32_t beside(bool, uint32_t head_dim) { return head_dim <= 128 ? 2u : 1u; }
+uint32_t beside(bool wide, uint32_t head_dim) { return head_dim > 128 ? (wide ? 1u : 2u) : wide ? 2u : 3u; }
 double step_time(bool wide, double n, double beside, uint32_t cus, double size) {
-    return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(1.5, beside * 0.0034 * size);
+    return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(0.4 + 0.26 * size, beside * 0.0031 * size);
 }
 
 }  // namespace
