@@ -51,9 +51,9 @@ struct hps_seq_attention_session {
 
 // What the host goes by where it cuts a call into work-groups.
 struct SeqAttendShape {
-    uint32_t wide_rows, narrow_rows, narrow_most, wide_keys, narrow_keys;   // rows of a work-group; own rows that narrow ones serve; keys of a step: of a wide work-group, of a narrow one's wave
+    uint32_t wide_rows, narrow_rows, wide_keys, narrow_keys;                // rows of a work-group; keys of a step: of a wide work-group, of a narrow one's wave
     uint32_t solo_keys;                                // own keys up to which a wave takes a request where there are many
-    bool (*wide)(uint64_t rows, uint32_t prefix);      // whether rows behind a history share keys
+    bool (*wide)(bool own, uint64_t rows, uint32_t keys, uint64_t stretches, uint32_t head_dim);              // whether rows share keys: `rows` behind each of so many stretches of keys
     uint32_t (*beside)(bool wide, uint32_t head_dim);  // work-groups of a CU at a time
     double (*step)(bool wide, double groups, double beside, uint32_t cus, double size);     // us; size: head_dim / 128
 };

@@ -188,8 +188,8 @@ uint32_t choose_chunks(const SeqAttendShape &shape, uint64_t tiles, uint32_t key
 // key heads of 128: 64 requests of 64 / 256 / 512 keys 14.6, 21.9, 32.4 / 13.9, 14.9, 19.9; 512 of 64 / 256 / 512 / 1,024 keys 26.2, 38.0,
 // 63.2, 134.1 / 43.6, 50.6, 69.6, 129.2).
 constexpr SeqAttendShape kShape = {
-    kWideRows, kNarrowRows, kNarrowRows, kWideKeys, kNarrowKeys, 512,
-    [](uint64_t rows, uint32_t prefix) { return rows > (prefix >= 16384 ? 2 : 1) * kNarrowRows; },
+    kWideRows, kNarrowRows, kWideKeys, kNarrowKeys, 512,
+    [](bool own, uint64_t rows, uint32_t keys, uint64_t, uint32_t) { return rows > (!own && keys >= 16384 ? 2 : 1) * kNarrowRows; },
     [](bool, uint32_t head_dim) { return head_dim <= 128 ? 2u : 1u; },
     [](bool wide, double n, double beside, uint32_t cus, double size) { return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(2.2, beside * 0.0121 * size); },
 };
@@ -255,7 +255,7 @@ hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const
     // own tokens: one part at least, so that every row has one
     const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, requests_heads = (uint64_t)a.n_requests * a.kv_heads;
     const uint32_t own_keys = a.max_len ? a.max_len : 1;
-    if (own_rows > shape.narrow_most) {
+    if (shape.wide(true, own_rows, own_keys, requests_heads, a.head_dim)) {
         a.own_mode = kOwnWide;
         a.own_tiles = div_up(own_rows, shape.wide_rows);
         a.own_chunks = choose_chunks(shape, requests_heads * a.own_tiles, own_keys, true, rows, a.head_dim, s.cus, part_limit / 2);
@@ -272,7 +272,7 @@ hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const
     uint64_t history_groups = 0;
     if (a.n_groups && a.max_prefix && a.max_group) {
         const uint64_t group_rows = (uint64_t)a.max_group * a.ratio;
-        a.history_wide = shape.wide(group_rows, a.max_prefix);
+        a.history_wide = shape.wide(false, group_rows, a.max_prefix, (uint64_t)a.n_groups * a.kv_heads, a.head_dim);
         a.history_tiles = div_up(group_rows, a.history_wide ? shape.wide_rows : shape.narrow_rows);
         const uint32_t step = a.history_wide ? shape.wide_keys : shape.narrow_keys * kWaves;
         a.history_chunks = choose_chunks(shape, (uint64_t)a.history_tiles * a.n_groups * a.kv_heads, a.max_prefix, a.history_wide, rows, a.head_dim, s.cus, part_limit - a.own_chunks);

@@ -725,10 +725,21 @@ template <typename T> hipError_t launch(Args &a, int kind, uint32_t groups, hipS
     }
 }
 
-bool wide_rows(uint64_t rows, uint32_t) { return rows > 32; }
+// Many rows pay where what they save is more than their longer start, 7 us: a row of 32 takes 0.76 us for a million keys and heads, one of 128,
+// of which all have to be filled, 0.66 (0.45 and 0.27 at 64 values a head).  (Measured, us a call, few / many, 8 heads of 128: 192 rows, 65,536 keys 89 / 99, 256
+// rows 110 / 106, 512 rows 203 / 187; 512 rows, 8,192 keys 39 / 45, 1,024 rows 64 / 64; heads of 64 34 / 37, 49 / 46.)
+bool wide_rows(bool, uint64_t rows, uint32_t keys, uint64_t stretches, uint32_t head_dim) {
+    const double size = head_dim / 128.0, work = (double)keys * (double)stretches * 1e-6;
+    const double few = head_dim > 128 ? 0.95 * size : 0.14 + 0.62 * size, many = head_dim > 128 ? 0.82 * size : std::fmax(0.12, 0.77 * size - 0.12);      // 16 rows a tile beyond 128 values
+    return work * (few * (double)((rows + 31) / 32 * 32) - many * (double)((rows + 127) / 128 * 128)) > 7.0;
+}
 uint32_t beside(bool wide, uint32_t head_dim) { return head_dim > 128 ? (wide ? 1u : 2u) : wide ? 2u : 3u; }
+// A step of a work-group of few rows (128 keys) takes 1.0 us alone on its CU, which is its chain of loads, conversions and products, and 0.87 for each
+// that shares a CU, which is memory: 5.1 TB/s, at 128 values a head; 0.66 and 0.52 at 64.  (Measured, us a call: 16 rows, 200,003 keys,
+// 8 heads: 32 / 48 / 64 / 80 / 96 / 128 chunks 58.5 / 54.5 / 51.2 / 56.5 / 54.0 / 58.8; with 64 values 39.5 / 40.0 / 33.6 / 37.0 / 33.7 / 34.8; 60,000 keys of
+// 128: 21.5 / 23.2 / 22.4 / 24.9 / 25.0 / 27.8.)
 double step_time(bool wide, double n, double beside, uint32_t cus, double size) {
-    return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(0.4 + 0.26 * size, beside * 0.0031 * size);
+    return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(0.32 + 0.68 * size, std::ceil(beside / cus) * (0.17 + 0.7 * size));
 }
 
 }  // namespace
@@ -755,11 +766,12 @@ hps_status_t hps_seq_attention_packed(hps_seq_attention_t *s, const hps_seq_atte
         a.k = reinterpret_cast<const char *>(s->part_o);
         a.packed_block = a.page_head = 0;
     }
-    // rows of a tile: 16 where all fit one, else 32, of which the mixed kernel makes tiles of 16
+    // rows of a tile of few: 16 where all fit one, and beside work-groups of many, else 32
     const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, group_rows = r.n_groups && r.max_prefix ? (uint64_t)a.max_group * a.ratio : 0;
-    const bool mixed = own_rows > 32 || (group_rows && wide_rows(group_rows, r.max_prefix));
+    const bool mixed = wide_rows(true, own_rows, r.max_len, (uint64_t)r.n_requests * r.kv_heads, r.head_dim) ||
+                       (group_rows && wide_rows(false, group_rows, r.max_prefix, (uint64_t)r.n_groups * r.kv_heads, r.head_dim));
     const int kind = mixed ? 0 : (own_rows <= 16 && group_rows <= 16) || r.head_dim > 128 ? 1 : 2;
-    const SeqAttendShape shape = {kWideRows, kind == 2 ? 32u : 16u, 32, kWideKeys, 32, 512, wide_rows, beside, step_time};
+    const SeqAttendShape shape = {kWideRows, kind == 2 ? 32u : 16u, kWideKeys, 32, 512, wide_rows, beside, step_time};
     uint32_t groups, parts;
     if (hps_status_t st = seq_attend_cut(a, shape, *s, groups, parts)) return st;
     hipStream_t st = static_cast<hipStream_t>(stream);

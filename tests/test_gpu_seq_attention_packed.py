@@ -60,12 +60,27 @@ class Packed(Problem):
 MANY = [(9, 7), (40, 11), (1, 1), (130, 3), (64, 20), (3, 3)]
 
 
+class Shared(Packed):
+    """Bounds that are far beyond the lengths, so that work-groups of many rows, which share keys, are taken for histories and own tokens alike."""
+
+    def run(self, **kw):
+        T, near = self.q.shape[0], dict(self.bounds)
+        if kw.get("bounds", True):
+            self.bounds = dict(max_new=T, max_group=T, max_len=1 << 25, max_prefix=(1 << 25) if len(self.prefix_lens) else 0)
+            self.bounds = {**self.bounds, **{k: v for k, v in near.items() if v == 0}}
+        try:
+            return super().run(**kw)
+        finally:
+            self.bounds = near
+
+
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("D", [32, 64, 96, 128, 256])
 def test_head_dims(D, dtype):
     Packed(dtype, D, 4, 2, 16, [(77, 4), (130, 2)], MIXED, seed=D).check()
     Packed(dtype, D, 8, 2, 32, [(300, 3), (45, 3)], [(9, 4), (40, 1), (1, 1), (130, 3), (64, 4), (3, 3)], seed=D + 2).check()        # 17 to 32 rows
-    Packed(dtype, D, 8, 1, 32, [(200, 6)], MANY, seed=D + 1).check()        # many rows: work-groups share the keys
+    Packed(dtype, D, 8, 1, 32, [(200, 6)], MANY, seed=D + 1).check()
+    Shared(dtype, D, 8, 1, 32, [(200, 6)], MANY, seed=D + 1).check()
 
 
 @pytest.mark.parametrize("H,K", [(1, 1), (5, 5), (8, 2), (12, 3), (16, 1), (32, 8), (40, 1), (33, 11)])
@@ -77,56 +92,69 @@ def test_heads(H, K):
 def test_block_sizes(block):
     for dtype, D in ((BF, 128), (HF, 64), (BF, 96)):
         Packed(dtype, D, 4, 2, block, [(150, 6)], MIXED, seed=block).check()
-        Packed(dtype, D, 16, 2, block, [(300, 6)], [(100, 9), (20, 20), (65, 7), (1, 1), (300, 2), (64, 5)], seed=block).check()
+        for kind in (Packed, Shared):
+            kind(dtype, D, 16, 2, block, [(300, 6)], [(100, 9), (20, 20), (65, 7), (1, 1), (300, 2), (64, 5)], seed=block).check()
 
 
 @pytest.mark.parametrize("n", [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 1000])
 def test_lengths(n):
     """Histories and own tokens that end at, in front of and behind the steps of the kernels."""
-    for new in (1, 9):
+    for new in (1, 8):
         own = max(n, new)
         Packed(BF, 64, 4, 4, 16, [(n, 2)], [(own, new), (new, new)], seed=n).check()
         Packed(BF, 128, 16, 2, 16, [(n, 2)], [(own, new), (new, new)], seed=n + 1).check()
         Packed(HF, 64, 4, 1, 64, [], [(own, new), (new, 1)], seed=n + 2).check()
+    for D in (64, 128):
+        Shared(BF, D, 16, 1, 16, [(n, 2)], [(max(n, 8), 8), (8, 8)], seed=n + 3).check()
 
 
 @pytest.mark.parametrize("rows", [1, 4, 15, 16, 17, 31, 32, 33, 64, 127, 128, 129, 300])
 def test_rows(rows):
     Packed(BF, 64, 2, 2, 16, [(270, rows)], [(3, 1)] * rows, seed=rows).check()
     Packed(BF, 64, 2, 1, 16, [(90, 1)], [(rows + 5, rows)], seed=rows).check()
+    if rows > 100:
+        Shared(BF, 64, 2, 2, 16, [(270, rows)], [(3, 1)] * rows, seed=rows).check()
+        Shared(BF, 64, 2, 1, 16, [(90, 1)], [(rows + 5, rows)], seed=rows).check()
 
 
 @pytest.mark.parametrize("layout", ["heads first", "apart"])
 def test_layouts_and_strides(layout):
     Packed(BF, 96, 6, 3, 16, [(140, 6)], MIXED, layout=layout).check(strided=True)
     Packed(HF, 128, 12, 3, 32, [(140, 6)], [(60, 9)] * 6, layout=layout).check(strided=True)
+    Shared(HF, 128, 12, 3, 32, [(140, 6)], [(60, 9)] * 6, layout=layout).check(strided=True)
 
 
 def test_long_prompts_without_a_history():
-    Packed(BF, 128, 4, 1, 16, [], [(513, 513), (700, 300), (40, 40)]).check()
-    Packed(HF, 64, 2, 2, 64, [], [(1, 1), (1500, 257)]).check()
+    for kind in (Packed, Shared):
+        kind(BF, 128, 4, 1, 16, [], [(513, 513), (700, 300), (40, 40)]).check()
+        kind(HF, 64, 2, 2, 64, [], [(1, 1), (1500, 257)]).check()
 
 
 def test_long_stretches_are_cut_and_joined():
     Packed(BF, 64, 4, 2, 16, [(9001, 2)], [(5, 1), (1, 1)]).check()
     Packed(BF, 64, 4, 2, 16, [], [(9001, 1), (7777, 2)]).check()
     Packed(HF, 128, 8, 1, 64, [(6000, 3)], [(2500, 8), (3000, 2), (64, 1)]).check()
+    Shared(HF, 128, 32, 1, 64, [(6000, 3)], [(2500, 8), (3000, 2), (64, 1)]).check()
+    p = Packed(BF, 32, 128, 1, 16, [(40000, 16)], [(3, 1)] * 16)             # 2,048 rows and near bounds: many rows and several chunks
+    p.check()
 
 
 def test_many_groups_and_requests():
     groups = [(n, 1 + i % 4) for i, n in enumerate((0, 3, 500, 64, 65, 1, 200, 31, 90, 100, 7))]
     n = sum(g[1] for g in groups)
     Packed(BF, 64, 8, 2, 16, groups, [(1 + i * 7 % 50, 1 + i % 2) for i in range(n)]).check()
-    Packed(BF, 64, 8, 2, 16, groups, [(60 + i * 7 % 50, 1 + i * 5 % 40) for i in range(n)]).check()
+    for kind in (Packed, Shared):
+        kind(BF, 64, 8, 2, 16, groups, [(60 + i * 7 % 50, 1 + i * 5 % 40) for i in range(n)]).check()
     Packed(BF, 32, 4, 4, 16, [(70, 300)], [(1 + i % 60, 1) for i in range(300)]).check()      # a wave to a request
 
 
 @pytest.mark.parametrize("new", [1, 30])
 def test_rows_that_attend_to_nothing(new):
     """No history and no own tokens; new tokens that are not all in the length; requests without new tokens; requests of no group; tokens of no request."""
-    p = Packed(BF, 64, 4, 2, 16, [(0, 2), (40, 2)], [(0, 0), (new, new), (50, 0), (new, new), (4 + new, new), (7 + new, new)], tail=3)
+    kind = Shared if new == 30 else Packed
+    p = kind(BF, 64, 4, 2, 16, [(0, 2), (40, 2)], [(0, 0), (new, new), (50, 0), (new, new), (4 + new, new), (7 + new, new)], tail=3)
     p.check()
-    p = Packed(BF, 64, 4, 2, 16, [(0, 1), (40, 1)], [(new, new), (new, new), (new, new)], tail=2)
+    p = kind(BF, 64, 4, 2, 16, [(0, 1), (40, 1)], [(new, new), (new, new), (new, new)], tail=2)
     p.lens = torch.tensor([0, new // 2, 0], dtype=torch.int32)
     p.check()
     p.group_offsets = torch.tensor([1, 1, 2], dtype=torch.int32)
@@ -140,15 +168,15 @@ def test_rows_that_attend_to_nothing(new):
 @pytest.mark.parametrize("D", [64, 96, 128])
 def test_what_is_hidden_has_no_part(D, dtype):
     """Groups of keys and values behind a query's own place that are no numbers (the pool's unused places are in every test)."""
-    for H, K, new in ((4, 4, 13), (4, 2, 13), (16, 2, 20)):                 # up to 16 rows, up to 32, many
-        p = Packed(dtype, D, H, K, 16, [(50, 1)], [(40, new)], seed=5)
+    for kind, H, K, new in ((Packed, 4, 4, 13), (Packed, 4, 2, 13), (Packed, 16, 2, 20), (Shared, 16, 1, 16), (Shared, 32, 2, 24)):      # up to 16 rows, up to 32, more, many
+        p = kind(dtype, D, H, K, 16, [(50, 1)], [(40, new)], seed=5)
         for i, d in ((39, 3), (38, 60), (35, 33), (31, D - 1)):
             b = int(p.block_table[0, i // 16])
             p.v[b, i % 16, 0, d] = math.inf if i == 38 else math.nan
         p.v[int(p.block_table[0, 2]), 4, K - 1, 5] = math.nan                # token 36
         out, lse = p.run()
         want, want_lse, bound, lse_bound = p.want()
-        assert torch.isnan(out[-1]).any() and torch.isfinite(out[-1]).any() and torch.isfinite(lse).all()
+        assert torch.isnan(out[-1]).any() and torch.isfinite(out[0]).all() and torch.isfinite(lse).all()
         R.close(out, want, bound)
         R.close(lse, want_lse, lse_bound)
         p.k[int(p.block_table[0, 2]), 5] = math.nan                          # token 37, whole
@@ -159,14 +187,14 @@ def test_what_is_hidden_has_no_part(D, dtype):
         R.close(lse[:first], want_lse[:first], lse_bound[:first])
         p.v[int(p.prefix_table[0, 0]), 3, :, 1] = math.nan                   # of the history: every row sees it
         out, _ = p.run()
-        assert torch.isnan(out[:, :, :32]).all() and torch.isfinite(out[0, :, 32:]).all()
+        assert torch.isnan(out[:, :, :32]).all() and torch.isfinite(out[0, :, 32:]).all()       # the first query sees none of the others
 
 
-@pytest.mark.parametrize("H,K,new", [(2, 2, 1), (16, 1, 9)])
-def test_scales_beyond_the_type(H, K, new):
+@pytest.mark.parametrize("kind,H,K,new", [(Packed, 2, 2, 1), (Packed, 16, 1, 9), (Shared, 16, 1, 16)])
+def test_scales_beyond_the_type(kind, H, K, new):
     """Scale bytes above the type's last one stand for NaN, as 255 does; 0 stands for 2^-127."""
     for dtype, last in ((BF, 252), (HF, 140)):
-        p = Packed(dtype, 64, H, K, 16, [(40, 1)], [(new, new)], seed=7)
+        p = kind(dtype, 64, H, K, 16, [(40, 1)], [(new, new)], seed=7)
         tiles = p.tiles()
         vs = P.places(16, 64)[3]
         b = int(p.prefix_table[0, 1])
@@ -183,9 +211,9 @@ def test_scales_beyond_the_type(H, K, new):
 
 def test_extreme_scores():
     """Scores that grow along the keys, fall, and are far apart: the running reference and what is joined."""
-    for H, K, new in ((2, 2, 1), (8, 2, 6), (8, 1, 8)):
+    for kind, H, K, new in ((Packed, 2, 2, 1), (Packed, 8, 2, 6), (Packed, 8, 1, 8), (Shared, 32, 1, 8)):
         for sign in (1, -1):
-            p = Packed(BF, 64, H, K, 16, [(700, 1)], [(new + 40, new)], seed=2, scale=1.0)
+            p = kind(BF, 64, H, K, 16, [(700, 1)], [(new + 40, new)], seed=2, scale=1.0)
             p.q[:] = 1
             for t, n in ((p.prefix_table[0], 700), (p.block_table[0], new + 40)):
                 for i in range(n):
@@ -193,10 +221,10 @@ def test_extreme_scores():
             p.check()
 
 
-@pytest.mark.parametrize("H,K,new", [(2, 2, 1), (8, 2, 6), (16, 1, 9)])
-def test_large_values_behind_growing_scores(H, K, new):
+@pytest.mark.parametrize("kind,H,K,new", [(Packed, 2, 2, 1), (Packed, 8, 2, 6), (Packed, 16, 1, 9), (Shared, 16, 1, 16)])
+def test_large_values_behind_growing_scores(kind, H, K, new):
     """The sums are formed against a reference that may lie behind the largest score: they have room for values of 2^80."""
-    p = Packed(BF, 64, H, K, 16, [(3000, 1)], [(new + 40, new)], seed=4, scale=1.0)
+    p = kind(BF, 64, H, K, 16, [(3000, 1)], [(new + 40, new)], seed=4, scale=1.0)
     p.q[:] = 1
     for i in range(3000):
         p.k[int(p.prefix_table[0, i // 16]), i % 16] = i / 1280
@@ -206,10 +234,10 @@ def test_large_values_behind_growing_scores(H, K, new):
     p.check()
 
 
-@pytest.mark.parametrize("H,K,new", [(2, 2, 1), (4, 4, 20), (16, 1, 20)])
-def test_odd_queries_spoil_their_own_rows_only(H, K, new):
+@pytest.mark.parametrize("kind,H,K,new", [(Packed, 2, 2, 1), (Packed, 4, 4, 20), (Shared, 16, 1, 20)])
+def test_odd_queries_spoil_their_own_rows_only(kind, H, K, new):
     for odd in (math.nan, math.inf):
-        p = Packed(BF, 64, H, K, 16, [(700, 2)], [(new + 40, new), (new, new)], seed=6)
+        p = kind(BF, 64, H, K, 16, [(700, 2)], [(new + 40, new), (new, new)], seed=6)
         p.q[0, 1], p.q[new, 0, 7] = odd, odd
         if new > 1:
             p.q[new - 1, H - 1, 63] = odd
@@ -226,26 +254,22 @@ def test_odd_queries_spoil_their_own_rows_only(H, K, new):
             R.close(lse[clean], want_lse[clean], lse_bound[clean])
 
 
-def test_pages_behind_four_gibibytes():
+@pytest.mark.parametrize("kind,H,new", [(Packed, 16, 1), (Shared, 64, 16)])
+def test_pages_behind_four_gibibytes(kind, H, new):
     """Blocks that are more than 2^32 bytes from the first one."""
     K, D, block = 8, 128, 64
-    p = Packed(BF, D, 16, K, block, [(500, 2)], [(5, 1), (70, 2)], spare=0)
+    p = kind(BF, D, H, K, block, [(500, 2)], [(4 + new, new), (70, new)], spare=0)
     tiles = p.tiles()
     n_blocks = (5 << 30) // (K * tiles.shape[2])
     pool = torch.zeros(n_blocks, K, tiles.shape[2], dtype=torch.uint8, device="cuda")
     shift = n_blocks - p.n_blocks
     pool[shift:] = tiles.cuda()
-    up = lambda t: torch.where(t < 0, t, t + shift).cuda()  # noqa: E731
     want, _, bound, _ = p.want()
-    for few in (True, False):
-        out, s = torch.empty(3, 16, D, dtype=BF, device="cuda"), B.hps_seq_attention_create(48, D)
-        bounds = p.bounds if few else dict(p.bounds, max_new=40, max_group=40)           # as if there were many rows
-        B.hps_seq_attention_packed(s, p.q.cuda(), pool, up(p.block_table), p.lens.cuda(), p.offsets.cuda(), out, prefix_table=up(p.prefix_table),
-                                   prefix_lens=p.prefix_lens.cuda(), group_offsets=p.group_offsets.cuda(), **bounds)
-        torch.cuda.synchronize()
-        assert B.hps_seq_attention_flags(s) == 0
-        B.hps_seq_attention_destroy(s)
-        R.close(out.cpu(), want, bound)
+    p.pages = lambda: pool
+    p.prefix_table, p.block_table = (torch.where(t < 0, t, t + shift) for t in (p.prefix_table, p.block_table))
+    out, _ = p.run()
+    assert p.flags == 0
+    R.close(out, want, bound)
 
 
 @pytest.mark.parametrize("H,K", [(4, 2), (64, 2)])
@@ -269,6 +293,14 @@ def test_flags(H, K):
         want, want_lse, bound, lse_bound = p.want()
         R.close(out, want, bound)
         R.close(lse, want_lse, lse_bound)
+    for junk in (-1, 10 ** 6):                         # to work-groups that share keys too
+        p = Shared(BF, 64, 64, 1, 16, [(100, 2)], [(5, 1), (40, 3)])
+        p.prefix_table[0, 3], p.block_table[1, 1] = junk, junk
+        out, lse = p.run()
+        assert p.flags == B.HPS_SEQ_FLAG_BLOCK
+        want, want_lse, bound, lse_bound = p.want()
+        R.close(out, want, bound)
+        R.close(lse, want_lse, lse_bound)
     for bounds in (dict(max_prefix=0), dict(max_group=0)):             # a bound of 0 leaves the histories out, and tells
         p = Packed(BF, 64, H, K, 16, [(100, 2)], [(5, 1), (40, 2)])
         p.bounds.update(bounds)
@@ -276,16 +308,15 @@ def test_flags(H, K):
         assert p.flags == B.HPS_SEQ_FLAG_LENGTH
 
 
-def test_no_blocks_at_all():
+@pytest.mark.parametrize("kind,H", [(Packed, 4), (Shared, 256)])
+def test_no_blocks_at_all(kind, H):
     """Pages without blocks: every token stands for zeros."""
-    p = Packed(BF, 64, 4, 2, 16, [(100, 2)], [(5, 1), (40, 2)])
-    for bounds in (p.bounds, dict(p.bounds, max_new=40, max_group=40)):
-        s, out = B.hps_seq_attention_create(12, 64), torch.full((3, 4, 64), 9.0, dtype=BF, device="cuda")
-        B.hps_seq_attention_packed(s, p.q.cuda(), torch.empty(0, 2, 16 * 68, dtype=torch.uint8, device="cuda"), p.block_table.cuda(), p.lens.cuda(), p.offsets.cuda(), out,
-                                   prefix_table=p.prefix_table.cuda(), prefix_lens=p.prefix_lens.cuda(), group_offsets=p.group_offsets.cuda(), **bounds)
-        torch.cuda.synchronize()
-        assert B.hps_seq_attention_flags(s) == B.HPS_SEQ_FLAG_BLOCK and (out == 0).all()
-        B.hps_seq_attention_destroy(s)
+    p = kind(BF, 64, H, 2, 16, [(100, 2)], [(5, 1), (40, 2)])
+    p.pages = lambda: torch.empty(0, 2, 16 * 68, dtype=torch.uint8, device="cuda")
+    out, lse = p.run()
+    assert p.flags == B.HPS_SEQ_FLAG_BLOCK and (out == 0).all()
+    keys = torch.tensor([105.0, 139, 140], dtype=torch.float64)
+    R.close(lse, keys.log()[:, None].expand(3, H), torch.tensor(1e-5, dtype=torch.float64))
 
 
 def test_refusals():
@@ -362,6 +393,8 @@ def test_two_sessions_side_by_side():
 @pytest.mark.parametrize("H", [8, 64])
 def test_graph_replays_on_new_lengths(H):
     p = Packed(BF, 64, H, 2, 16, [(300, 3), (70, 2)], [(40, 2), (20, 1), (33, 4), (16, 1), (50, 2)])
+    if H == 64:                                        # many rows share keys
+        p.bounds = dict(max_new=10, max_len=1 << 25, max_prefix=1 << 25)
     pages = p.pages()
     T = p.q.shape[0]
     s, out, lse = B.hps_seq_attention_create(T * H, 64), torch.zeros(T, H, 64, dtype=BF, device="cuda"), torch.zeros(T, H, device="cuda")
@@ -392,7 +425,7 @@ def test_graph_replays_on_new_lengths(H):
 @pytest.mark.parametrize("new", [1, 20])
 def test_tokens_behind_the_last_query(new):
     """Offsets may count more tokens than there are queries for: the others' places in their requests stay what they are."""
-    p = Packed(BF, 64, 4, 2, 16, [(40, 2)], [(new, new), (50 + new, 2 * new)], seed=new)
+    p = (Shared if new == 20 else Packed)(BF, 64, 32, 2, 16, [(40, 2)], [(new, new), (50 + new, 2 * new)], seed=new)
     want, want_lse, bound, lse_bound = p.want()
     T = new + max(1, new // 2)
     p.q = p.q[:T]
@@ -405,8 +438,8 @@ def test_tokens_behind_the_last_query(new):
 @pytest.mark.parametrize("H,K,requests", [(4, 2, [(5, 1), (40, 2)]), (16, 1, [(60, 9), (9, 9)]), (2, 2, [(33, 1)] * 300), (2, 2, [(700, 1), (2000, 2)])])
 def test_scores_of_minus_infinity(H, K, requests):
     """Rows whose scores are all minus infinity get 0, whatever the values and however the keys are cut."""
-    for groups in ([], [(100, len(requests))]):
-        p = Packed(BF, 64, H, K, 16, groups, requests)
+    for groups, kind in (([], Packed), ([(100, len(requests))], Packed), ([(100, len(requests))], Shared)):
+        p = kind(BF, 64, H, K, 16, groups, requests)
         p.q[:] = 1
         for t, n in [(p.block_table[r], int(n)) for r, n in enumerate(p.lens)] + [(p.prefix_table[g], int(n)) for g, n in enumerate(p.prefix_lens)]:
             place = torch.arange(n)
