@@ -668,14 +668,14 @@ template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads,
 }
 
 // Either kind, where a history or the own tokens have many rows.
-template <typename T, int G> __global__ void __launch_bounds__(kThreads, G <= 4 ? 2 : 1) packed_kernel(const Args a) {
+template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads, G <= 4 ? 2 : 1) packed_kernel(const Args a) {
     typedef Wide<T, G> W;
-    typedef Few<T, G, 1> F;
+    typedef Few<T, G, NT> F;
     extern __shared__ __align__(16) char shared[];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, 16, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<kWideRows, 16 * NT, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
     if (is_wide) {
         W e(a, it, (uint32_t)(uintptr_t)(lds_char *)shared, wave);
         e.run();
@@ -691,13 +691,26 @@ template <typename T, int G> __global__ void __launch_bounds__(kThreads, G <= 4 
 // ---- host ---------------------------------------------------------------------------------
 
 template <typename T, int G, int NT> constexpr uint32_t kFewLds = Few<T, G, NT>::kLds + Few<T, G, NT>::kSums;
-template <typename T, int G> constexpr uint32_t kMixedLds = Wide<T, G>::kLds > kFewLds<T, G, 1> ? Wide<T, G>::kLds : kFewLds<T, G, 1>;
+template <typename T, int G, int NT> constexpr uint32_t kMixedLds = Wide<T, G>::kLds > kFewLds<T, G, NT> ? Wide<T, G>::kLds : kFewLds<T, G, NT>;
+
+// Kernels of either kind, or of few rows alone, with 16 or 32 rows to a tile of few.
+template <typename T, int G, typename F> hipError_t with_kernel(bool mixed, bool two, F f) {
+    if constexpr (G <= 4) {
+        if (mixed && two) return f(&packed_kernel<T, G, 2>, kMixedLds<T, G, 2>);
+        if (two) return f(&packed_few_kernel<T, G, 2>, kFewLds<T, G, 2>);
+    }
+    if (mixed) return f(&packed_kernel<T, G, 1>, kMixedLds<T, G, 1>);
+    return f(&packed_few_kernel<T, G, 1>, kFewLds<T, G, 1>);
+}
 
 template <typename T, int G> hipError_t allow_lds() {
-    static_assert(kMixedLds<T, G> <= 160 * 1024 && kFewLds<T, G, 2> <= 160 * 1024, "LDS of a CU");
-    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_kernel<T, G>), hipFuncAttributeMaxDynamicSharedMemorySize, kMixedLds<T, G>)) return e;
-    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_few_kernel<T, G, 1>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds<T, G, 1>)) return e;
-    if constexpr (G <= 4) return hipFuncSetAttribute(reinterpret_cast<const void *>(&packed_few_kernel<T, G, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds<T, G, 2>);
+    static_assert(kMixedLds<T, G, 1> <= 160 * 1024 && (G > 4 || (kMixedLds<T, G, 2> <= 80 * 1024 && kFewLds<T, G, 2> <= 80 * 1024)), "LDS of a CU");
+    for (int kind = 0; kind < (G <= 4 ? 4 : 2); ++kind) {
+        const hipError_t e = with_kernel<T, G>((kind & 1) != 0, (kind & 2) != 0, [](auto kernel, uint32_t lds) {
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        });
+        if (e) return e;
+    }
     return hipSuccess;
 }
 template <typename T> hipError_t allow_lds() {
@@ -706,22 +719,22 @@ template <typename T> hipError_t allow_lds() {
     return allow_lds<T, 8>();
 }
 
-template <typename T, int G> hipError_t launch(Args &a, int kind, uint32_t groups, hipStream_t st) {
-    return seq_launches(groups, [&](uint32_t first, uint32_t n) {
-        a.first_group = first;
-        if (kind == 0) hipLaunchKernelGGL((packed_kernel<T, G>), dim3(n), dim3(kThreads), (kMixedLds<T, G>), st, a);
-        else if (kind == 1) hipLaunchKernelGGL((packed_few_kernel<T, G, 1>), dim3(n), dim3(kThreads), (kFewLds<T, G, 1>), st, a);
-        else if constexpr (G <= 4) hipLaunchKernelGGL((packed_few_kernel<T, G, 2>), dim3(n), dim3(kThreads), (kFewLds<T, G, 2>), st, a);
+template <typename T, int G> hipError_t launch(Args &a, bool mixed, bool two, uint32_t groups, hipStream_t st) {
+    return with_kernel<T, G>(mixed, two, [&](auto kernel, uint32_t lds) {
+        return seq_launches(groups, [&](uint32_t first, uint32_t n) {
+            a.first_group = first;
+            hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), lds, st, a);
+        });
     });
 }
 
-template <typename T> hipError_t launch(Args &a, int kind, uint32_t groups, hipStream_t st) {
+template <typename T> hipError_t launch(Args &a, bool mixed, bool two, uint32_t groups, hipStream_t st) {
     switch (a.head_dim) {
-    case 32: return launch<T, 1>(a, kind, groups, st);
-    case 64: return launch<T, 2>(a, kind, groups, st);
-    case 96: return launch<T, 3>(a, kind, groups, st);
-    case 128: return launch<T, 4>(a, kind, groups, st);
-    default: return launch<T, 8>(a, kind, groups, st);
+    case 32: return launch<T, 1>(a, mixed, two, groups, st);
+    case 64: return launch<T, 2>(a, mixed, two, groups, st);
+    case 96: return launch<T, 3>(a, mixed, two, groups, st);
+    case 128: return launch<T, 4>(a, mixed, two, groups, st);
+    default: return launch<T, 8>(a, mixed, two, groups, st);
     }
 }
 
@@ -766,17 +779,17 @@ hps_status_t hps_seq_attention_packed(hps_seq_attention_t *s, const hps_seq_atte
         a.k = reinterpret_cast<const char *>(s->part_o);
         a.packed_block = a.page_head = 0;
     }
-    // rows of a tile of few: 16 where all fit one, and beside work-groups of many, else 32
+    // rows of a tile of few: 16 where all that are served so fit one, else 32 (heads up to 128, whose registers suffice)
     const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, group_rows = r.n_groups && r.max_prefix ? (uint64_t)a.max_group * a.ratio : 0;
-    const bool mixed = wide_rows(true, own_rows, r.max_len, (uint64_t)r.n_requests * r.kv_heads, r.head_dim) ||
-                       (group_rows && wide_rows(false, group_rows, r.max_prefix, (uint64_t)r.n_groups * r.kv_heads, r.head_dim));
-    const int kind = mixed ? 0 : (own_rows <= 16 && group_rows <= 16) || r.head_dim > 128 ? 1 : 2;
-    const SeqAttendShape shape = {kWideRows, kind == 2 ? 32u : 16u, kWideKeys, 32, 512, wide_rows, beside, step_time};
+    const bool own_many = wide_rows(true, own_rows, r.max_len, (uint64_t)r.n_requests * r.kv_heads, r.head_dim);
+    const bool group_many = group_rows && wide_rows(false, group_rows, r.max_prefix, (uint64_t)r.n_groups * r.kv_heads, r.head_dim);
+    const bool two = r.head_dim <= 128 && ((!own_many && own_rows > 16) || (!group_many && group_rows > 16));
+    const SeqAttendShape shape = {kWideRows, two ? 32u : 16u, kWideKeys, 32, 512, wide_rows, beside, step_time};
     uint32_t groups, parts;
     if (hps_status_t st = seq_attend_cut(a, shape, *s, groups, parts)) return st;
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(seq_attend_check(a, st));
-    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, kind, groups, st) : launch<__bf16>(a, kind, groups, st));
+    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, own_many || group_many, two, groups, st) : launch<__bf16>(a, own_many || group_many, two, groups, st));
     SEQ_TRY(seq_attend_join(a, r.dtype, parts, st));
     return HPS_OK;
 }
