@@ -43,7 +43,7 @@ C_DEMO_LIB = os.path.join(ROOT, "tests", "libhps_c_demo.so")
 def build_c_demo():
     """The plain-C caller of the library that one GPU test runs (gcc, C99, no C++ anywhere)."""
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
-    cmd = ["gcc", "-std=c99", "-O1", "-Wall", "-Wextra", "-pedantic", "-fPIC",
+    cmd = ["gcc", "-std=c99", "-O1", "-Wall", "-Wextra", "-pedantic", "-fPIC", "-shared",
            "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(rocm, "include"), C_DEMO_SRC, "-o", C_DEMO_LIB,
            "-L", HERE, "-l:libhps_cache.so", "-Wl,-rpath,$ORIGIN/../paper_2210_08804_amd",
            "-L", os.path.join(rocm, "lib"), "-lamdhip64"]
