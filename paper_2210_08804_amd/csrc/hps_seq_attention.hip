@@ -34,8 +34,74 @@ template <typename T, int DT, bool kExact> __global__ void __launch_bounds__(kTh
     }
     const uint32_t group = a.first_group + blockIdx.x;
     Item it;
-    bool is_wide, solo;
-    if (!item_of<kWideRows, kNarrowRows, false>(a, group, wave, lane, it, is_wide, solo)) return;
+    bool is_wide, solo = false;
+    if (group < a.history_groups) {
+        // Work-groups of one (group, chunk, head) read the same keys: they go to one XCD (workgroups are dealt to the eight in turn).
+        uint32_t combo, tile;
+        if (a.history_combos >= 8) {
+            const uint32_t y = group >> 3;
+            combo = (group & 7u) + 8 * (y / a.history_tiles);
+            tile = y % a.history_tiles;
+            if (combo >= a.history_combos) return;
+        } else {
+            combo = group % a.history_combos;
+            tile = group / a.history_combos;
+        }
+        // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
+        // side by side, one head's rows are in few of the L2's channels.
+        // From group to group the chunks do: where histories end at different lengths, the last chunks have little to do, and must not
+        // all be one XCD's (26 groups of 187 to 3,000 keys, two heads of 64, 4 chunks 50.6 -> 42.8 us, 8 chunks 51.7 -> 48.6).
+        const uint32_t rest = combo / a.kv_heads, g = rest / a.history_chunks, chunk = (rest + g) % a.history_chunks;
+        it.head = (combo + rest) % a.kv_heads;
+        const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0;
+        if (n > a.max_group) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        is_wide = a.history_wide;
+        it.token0 = t0;
+        it.rows = min(n, a.max_group) * a.ratio;
+        it.row0 = tile * (is_wide ? kWideRows : kNarrowRows);
+        if (it.row0 >= it.rows) return;
+        it.table = a.prefix_table + (size_t)g * a.prefix_width;
+        it.first = chunk * a.history_chunk;
+        it.end = min(length(a, scalar(a.prefix_lens, g), a.prefix_width, a.max_prefix), it.first + a.history_chunk);
+        it.causal_from = kAll;
+        it.part = chunk;
+    } else {
+        uint32_t x = group - a.history_groups;
+        is_wide = a.own_mode == kOwnWide;
+        solo = a.own_mode == kOwnSolo;
+        if (solo) {
+            x = x * kWaves + wave;
+            if (x >= a.own_items) return;              // no wave of a solo work-group waits for another
+        }
+        it.head = x % a.kv_heads;
+        uint32_t rest = x / a.kv_heads;
+        const uint32_t chunk = rest % a.own_chunks;
+        rest /= a.own_chunks;
+        const uint32_t tile = rest % a.own_tiles, r = rest / a.own_tiles;
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r + 1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0, tile_rows = is_wide ? kWideRows : kNarrowRows;
+        if (n > a.max_new) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        it.token0 = t0;
+        it.rows = min(n, a.max_new) * a.ratio;
+        it.row0 = tile * tile_rows;
+        if (it.row0 >= it.rows) return;
+        const uint32_t len = length(a, scalar(a.lens, r), a.table_width, a.max_len);
+        it.table = a.block_table + (size_t)r * a.table_width;
+        it.first = chunk * a.own_chunk;
+        // places by all of the request's new tokens: queries may end inside it
+        const int32_t from = (int32_t)len - (scalar(a.token_offsets, r + 1) - (int32_t)t0) + 1, last = from + (int32_t)((min(it.rows, it.row0 + tile_rows) - 1) / a.ratio);        // keys that the tile's last row sees
+        it.causal_from = n > 1 ? from : kAll;
+        it.end = min((uint32_t)max(last, 0), it.first + a.own_chunk);
+        it.part = a.history_chunks + chunk;
+        if (a.history_chunks && chunk == 0 && ((int32_t)r < scalar(a.group_offsets, 0) || (int32_t)r >= scalar(a.group_offsets, a.n_groups)))
+            for (uint32_t p = 0; p < a.history_chunks; ++p) mark_empty(a, it, p, tile_rows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+    }
+    if (it.first >= it.end && !a.direct) {
+        mark_empty(a, it, it.part, is_wide ? kWideRows : kNarrowRows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+        return;
+    }
     if (is_wide) {
         E e(a, it, lds_base, 32 * wave);
         e.wide();

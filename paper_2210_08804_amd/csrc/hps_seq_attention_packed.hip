@@ -650,6 +650,97 @@ template <typename T, int G> struct Wide : Engine<T, G, true> {
     __device__ __forceinline__ int32_t block_at(uint32_t at) const { return at < this->it.end ? scalar(this->it.table, at >> this->a.sh) : -1; }
 };
 
+// Reads the blocks of the first 32 keys that a wave of few rows has.
+__device__ __forceinline__ void first_blocks(const Args &a, Item &it, uint32_t width, uint32_t wave) {
+    if (width == 0) {
+        it.id0 = it.id1 = -1;
+        return;
+    }
+    const uint32_t at = it.first + 32 * wave, last = width - 1;
+    it.id0 = scalar(it.table, min(at >> a.sh, last));
+    it.id1 = scalar(it.table, min((at + 16) >> a.sh, last));
+}
+
+// The work of one work-group, or of one of its waves where each has its own (solo).  false: none, and what it would leave is marked.
+// (The loops over pages of 16 bits have no registers left for what this reads ahead, nor for how the compiler joins its ends: taken as it is it spills 49
+// scalars there and costs 1 % at 512 rows behind 32,768 keys, 4 % at small calls.)
+template <uint32_t kNarrow>                            // rows of a work-group of few
+__device__ __forceinline__ bool item_of(const Args &a, uint32_t group, uint32_t wave, uint32_t lane, Item &it, bool &is_wide, bool &solo) {
+    solo = false;
+    if (group < a.history_groups) {
+        // Work-groups of one (group, chunk, head) read the same keys: they go to one XCD (workgroups are dealt to the eight in turn).
+        uint32_t combo, tile;
+        if (a.history_combos >= 8) {
+            const uint32_t y = group >> 3, q = a.by_history_tiles.quotient(y);
+            combo = (group & 7u) + 8 * q;
+            tile = y - q * a.history_tiles;
+            if (combo >= a.history_combos) return false;
+        } else {
+            tile = a.by_history_combos.quotient(group);
+            combo = group - tile * a.history_combos;
+        }
+        // From chunk to chunk the heads go round, so that an XCD has different ones at a time: where the heads of a token lie
+        // side by side, one head's rows are in few of the L2's channels.
+        // From group to group the chunks do: where histories end at different lengths, the last chunks have little to do, and must not
+        // all be one XCD's (26 groups of 187 to 3,000 keys, two heads of 64, 4 chunks 50.6 -> 42.8 us, 8 chunks 51.7 -> 48.6).
+        const uint32_t rest = a.by_kv_heads.quotient(combo), g = a.by_history_chunks.quotient(rest), turned = rest + g, chunk = turned - a.by_history_chunks.quotient(turned) * a.history_chunks;
+        it.head = combo + rest - a.by_kv_heads.quotient(combo + rest) * a.kv_heads;
+        it.table = a.prefix_table + (size_t)g * a.prefix_width;
+        it.first = chunk * a.history_chunk;
+        first_blocks(a, it, a.prefix_width, a.history_wide ? 0 : wave);
+        const int32_t prefix = scalar(a.prefix_lens, g);
+        const uint32_t r0 = clamp_to(scalar(a.group_offsets, g), a.n_requests), r1 = clamp_to(scalar(a.group_offsets, g + 1), a.n_requests);
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r0), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0;
+        if (n > a.max_group) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        is_wide = a.history_wide;
+        it.token0 = t0;
+        it.rows = min(n, a.max_group) * a.ratio;
+        it.row0 = tile * (is_wide ? kWideRows : kNarrow);
+        if (it.row0 >= it.rows) return false;
+        it.end = min(length(a, prefix, a.prefix_width, a.max_prefix), it.first + a.history_chunk);
+        it.causal_from = kAll;
+        it.part = chunk;
+    } else {
+        uint32_t x = group - a.history_groups;
+        is_wide = a.own_mode == kOwnWide;
+        solo = a.own_mode == kOwnSolo;
+        if (solo) {
+            x = x * kWaves + wave;
+            if (x >= a.own_items) return false;              // no wave of a solo work-group waits for another
+        }
+        const uint32_t rest = a.by_kv_heads.quotient(x), tiles = a.by_own_chunks.quotient(rest), r = a.by_own_tiles.quotient(tiles), turn = rest - tiles * a.own_chunks, tile = tiles - r * a.own_tiles;
+        it.head = x - rest * a.kv_heads;
+        // The chunks are dealt anew to each request: where lengths differ, the last ones have little to do, and work-groups a fixed number
+        // apart share a CU.
+        const uint32_t dealt = turn + (r * 0x9E3779B9u >> 24), chunk = dealt - a.by_own_chunks.quotient(dealt) * a.own_chunks;
+        it.table = a.block_table + (size_t)r * a.table_width;
+        it.first = chunk * a.own_chunk;
+        first_blocks(a, it, a.table_width, solo || is_wide ? 0 : wave);
+        const int32_t own = scalar(a.lens, r);
+        const uint32_t t0 = clamp_to(scalar(a.token_offsets, r), a.n_tokens), t1 = clamp_to(scalar(a.token_offsets, r + 1), a.n_tokens);
+        const uint32_t n = t1 > t0 ? t1 - t0 : 0, tile_rows = is_wide ? kWideRows : kNarrow;
+        if (n > a.max_new) atomicOr(a.flags, HPS_SEQ_FLAG_LENGTH);
+        it.token0 = t0;
+        it.rows = min(n, a.max_new) * a.ratio;
+        it.row0 = tile * tile_rows;
+        if (it.row0 >= it.rows) return false;
+        const uint32_t len = length(a, own, a.table_width, a.max_len);
+        // places by all of the request's new tokens: queries may end inside it
+        const int32_t from = (int32_t)len - (scalar(a.token_offsets, r + 1) - (int32_t)t0) + 1, last = from + (int32_t)(a.by_ratio.quotient(min(it.rows, it.row0 + tile_rows) - 1));        // keys that the tile's last row sees
+        it.causal_from = n > 1 ? from : kAll;
+        it.end = min((uint32_t)max(last, 0), it.first + a.own_chunk);
+        it.part = a.history_chunks + chunk;
+        if (a.history_chunks && chunk == 0 && ((int32_t)r < scalar(a.group_offsets, 0) || (int32_t)r >= scalar(a.group_offsets, a.n_groups)))
+            for (uint32_t p = 0; p < a.history_chunks; ++p) mark_empty(a, it, p, tile_rows, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+    }
+    if (it.first >= it.end && !a.direct) {
+        mark_empty(a, it, it.part, is_wide ? kWideRows : kNarrow, solo ? lane : threadIdx.x, solo ? 64 : kThreads);
+        return false;
+    }
+    return true;
+}
+
 // Waves of a SIMD that the registers of few rows leave room for: work-groups of a CU.
 template <int G, int NT> constexpr int kFewBeside = NT == 1 ? (G == 8 ? 2 : G >= 3 ? 3 : 4) : G >= 3 ? 2 : G == 2 ? 3 : 4;
 
@@ -660,7 +751,7 @@ template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads,
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, 16 * NT, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<16 * NT>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
     F e(a, it);
     e.run(solo ? it.first : it.first + 32 * wave, solo ? 32 : 32 * kWaves);
     if (solo) e.finish();
@@ -675,7 +766,7 @@ template <typename T, int G, int NT> __global__ void __launch_bounds__(kThreads,
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     Item it;
     bool is_wide, solo;
-    if (!item_of<kWideRows, 16 * NT, true>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
+    if (!item_of<16 * NT>(a, a.first_group + blockIdx.x, wave, lane, it, is_wide, solo)) return;
     if (is_wide) {
         W e(a, it, (uint32_t)(uintptr_t)(lds_char *)shared, wave);
         e.run();
