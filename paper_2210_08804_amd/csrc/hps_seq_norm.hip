@@ -16,7 +16,8 @@ template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kNo
 // With n = r x, r = 1 / sqrt(mean(x^2) + eps), and y = turn(w n): dz = turn back(dy); dw = sum dz n; with g = w dz
 //   dx = r (g - n mean(g n)),
 // so a head takes one pass with two sums.  A work-group goes through tokens with its weights' sums in registers, joins its lanes' in
-// LDS at the end, and a second kernel adds up the work-groups'.
+// LDS at the end, and a second kernel adds up the work-groups'.  Bound by HBM where there are many (16,384 tokens of 32 heads of 64 of 32 bits,
+// 403 MB moved: 78 us, 5.2 TB/s, and 4.8 of the sums), else by the chain (2,003 of 24 heads of 96 of 16 bits, 28 MB: 10.6 and 3.9).
 template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_backward(const NormArgs &a, const NormTensor &g, uint32_t which, uint32_t group) {
     constexpr int kPer = E == 1 ? 4 : 1;
     __shared__ float l_sum[kNormThreads][kPer * 2 * E + 1];
@@ -145,7 +146,10 @@ template <typename T> hipError_t launch_grad(const NormArgs &a, bool whole, hipS
     return hipGetLastError();
 }
 
-constexpr uint32_t kGradGroups = 512;                  // of a tensor's gradients
+// Work-groups of a tensor's gradients: fewer leave the device idle, more have more sums to join (us with 256 / 512 / 1,024: 8,192 tokens of 20
+// heads of 128 42.1 / 33.4 / 34.2, of 40 heads 68.0 / 56.4 / 58.1; 16,384 of 32 heads of 64 in 32 bits 85.7 / 87.0 / 89.0; 2,003 of 24 heads of 96
+// 17.4 / 16.4 / 16.9).
+constexpr uint32_t kGradGroups = 512;
 static_assert(kGradGroups <= HPS_SEQ_NORM_PARTS, "a part each");
 
 NormArgs args_of(const hps_seq_norm_args_t &r) {
@@ -197,21 +201,25 @@ bool norm_whole(NormArgs &a, uint32_t rot_dim, int size, bool more) {
     return whole;
 }
 
-constexpr uint32_t kFill = 2048;                       // work-groups that keep the device busy, eight to a CU
+// A lane gets two heads of a token where there still are eight work-groups to a CU, so that weights and angles are read half as often.  (us, one to a lane /
+// two, 8,192 tokens: 20 heads of 128 22.1 / 20.2, 40 heads 38.3 / 36.0, four to a lane 38.7; 24 heads of 96 23.6 / 20.3.  Beside keys and values in one
+// launch four are better, where there are enough: 8,192 tokens of 32 and 8 heads 50.6 -> 44.)  A work-group gets several tokens
+// where there is one for each CU: below that a token each has the shorter chain.  (16 heads of 64, 8,192 tokens: a token at a time 15.1, four 10.5.)
+constexpr uint32_t kFull = 2048, kCus = 256;
 
-void norm_share(NormArgs &a, int i, uint32_t most_groups) {
+void norm_share(NormArgs &a, int i, uint32_t most_groups, uint32_t most_each) {
     NormTensor &x = a.x[i];
     x.heads_beside = x.tokens_beside = 1;
     x.groups = 0;
     if (x.heads == 0 || a.n_tokens == 0) return;
     const uint32_t rows = kNormThreads >> a.lane_bits;
     const uint64_t full = ((uint64_t)a.n_tokens * x.heads + rows - 1) / rows;                  // work-groups with a head to a lane
-    uint32_t each = full >= 4 * kFill ? 4 : full >= 2 * kFill ? 2 : 1;
+    uint32_t each = most_each >= 4 && full >= 4 * kFull ? 4 : full >= kFull ? 2 : 1;
     if (x.heads > each * rows) each = (x.heads + rows - 1) / rows;
     x.heads_beside = (x.heads + each - 1) / each;
-    const uint32_t spare = (uint32_t)(full / kFill) + 1;                    // few rows: a token each
+    const uint64_t spare = full / kCus + 1;
     x.tokens_beside = rows / x.heads_beside;
-    if (most_groups > HPS_SEQ_NORM_PARTS && x.tokens_beside > spare) x.tokens_beside = spare;
+    if (most_groups > HPS_SEQ_NORM_PARTS && x.tokens_beside > spare) x.tokens_beside = (uint32_t)spare;
     x.groups = (a.n_tokens + x.tokens_beside - 1) / x.tokens_beside;
     if (x.groups > most_groups) x.groups = most_groups;
 }
@@ -236,8 +244,8 @@ hps_status_t hps_seq_norm_rope(const hps_seq_norm_args_t *args, void *stream) {
     SEQ_REQUIRE(norm_put(a, 0, r.q_heads, r.q, r.q_out, nullptr, size_of(r.dtype)) && norm_put(a, 1, r.k_heads, r.k, r.k_out, nullptr, size_of(r.dtype)),
                 "q, k, q_out and k_out must be device pointers aligned to their type");
     const bool whole = norm_whole(a, 2 * a.half, size_of(r.dtype));
-    norm_share(a, 0, 0xFFFFFFFFu);
-    norm_share(a, 1, 0xFFFFFFFFu);
+    norm_share(a, 0, 0xFFFFFFFFu, 2);
+    norm_share(a, 1, 0xFFFFFFFFu, 2);
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(r.dtype == HPS_SEQ_F32 ? launch_norm<float>(a, whole, st) : r.dtype == HPS_SEQ_F16 ? launch_norm<_Float16>(a, whole, st) : launch_norm<__bf16>(a, whole, st));
     return HPS_OK;
@@ -262,8 +270,8 @@ hps_status_t hps_seq_norm_rope_grad(const hps_seq_norm_args_t *args, const hps_s
     a.weight_grad[0] = q_weight_grad;
     a.weight_grad[1] = k_weight_grad;
     const bool whole = norm_whole(a, 2 * a.half, size_of(r.dtype));
-    norm_share(a, 0, kGradGroups);
-    norm_share(a, 1, kGradGroups);
+    norm_share(a, 0, kGradGroups, 2);
+    norm_share(a, 1, kGradGroups, 2);
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(r.dtype == HPS_SEQ_F32 ? launch_grad<float>(a, whole, st) : r.dtype == HPS_SEQ_F16 ? launch_grad<_Float16>(a, whole, st) : launch_grad<__bf16>(a, whole, st));
     return HPS_OK;

@@ -34,7 +34,6 @@ struct PackedArgs {
 };
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kFill = 2048;                       // work-groups that keep the device busy, eight to a CU
 
 template <int kCtrl> __device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false); }
 template <int kCtrl> __device__ __forceinline__ double moved(double x) {
@@ -231,10 +230,11 @@ template <typename T, bool kWhole, bool kWithin> struct Keys {
     }
 };
 
-// Work-groups of the launch: the queries' first (as in the norm kernels), then those of keys and values.  Bound by HBM where there are many
-// tokens, else by the chain slot, position, row, largest value, store.
+// Work-groups of the launch: the queries' (as in the norm kernels) and those of keys and values, in turn.  Bound by HBM where there are many
+// tokens (8,192 of 32 and 8 heads of 128, 178 MB moved: 44 us, 4.0 TB/s), else by the chain slot, position, row, largest value, store (64
+// tokens 4.4 us).
 template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kThreads) append_kernel(const PackedArgs a) {
-    // the two kinds in turn, so that one's arithmetic runs beside the other's loads
+    // one kind's arithmetic runs beside the other's loads
     const uint32_t group = a.first_group + blockIdx.x, pairs = 2 * min(a.norm.x[0].groups, a.kv_groups);
     const bool queries = group < pairs ? (group & 1u) == 0 : a.norm.x[0].groups > a.kv_groups;
     const uint32_t mine = group < pairs ? group / 2 : group - pairs / 2;
@@ -274,6 +274,8 @@ template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kTh
     }
 }
 
+// A place's row of codes and its scale to 16 or 32 bits: bound by HBM (8,192 tokens of 8 heads of 128, 42 MB moved: 10.5 us), else by a chain of three
+// reads (64 tokens 3.4 us).
 template <typename T, bool kWhole> __global__ void __launch_bounds__(kThreads) read_kernel(const PackedArgs a) {
     const Place at(a, a.first_group + blockIdx.x);
     if (!at.live || at.d >= a.tile.dim) return;
@@ -302,7 +304,10 @@ template <typename T, bool kWhole> __global__ void __launch_bounds__(kThreads) r
 
 int size_of(int dtype) { return dtype == HPS_SEQ_F32 ? 4 : 2; }
 
-// Lanes, and the heads that a work-group goes through: several where there are tokens enough to fill the device, else one.
+// Lanes, and the heads that a work-group goes through, which share the token's factors: several where there are work-groups enough.  (us, keys and values alone,
+// one head / two / four / eight: 8,192 tokens of 8 heads of 128 33.2 / 23.3 / 17.7 / 14.9, with their queries 65.3 / 53.6 / 44.1 / 46.0; 4,000 tokens 17.6 / 13.2 / 10.0 / 12.9;
+// 8,192 of 4 heads 17.8 / 13.3 / 10.4.)
+constexpr uint32_t kFill = 512;
 void share(PackedArgs &a, uint32_t n_tokens) {
     a.lane_bits = 2;
     while ((8u << a.lane_bits) < a.tile.dim) ++a.lane_bits;
@@ -396,7 +401,7 @@ hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, voi
     put_pages(a, r.pages, r.head_dim);
     // vectors of eight keys, none of which holds pairs of two kinds
     const bool whole = norm_whole(n, 2 * n.half, size, heads16(a.k, a.k_token, a.k_head) && heads16(a.v, a.v_token, a.v_head) && (n.interleaved ? 2 * n.half : n.half) % 8 == 0);
-    norm_share(n, 0, 0xFFFFFFFFu);
+    norm_share(n, 0, 0xFFFFFFFFu, 4);
     share(a, r.n_tokens);
     const uint32_t tokens = (kThreads >> a.lane_bits) / 2;
     const uint64_t kv_groups = a.n_slots ? (uint64_t)((r.n_tokens + tokens - 1) / tokens) * a.head_groups : 0;
