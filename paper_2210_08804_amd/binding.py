@@ -813,8 +813,8 @@ def _packed_pages(pages, dim):
     sb, sh, one = pages.stride()
     if one != 1:
         raise ValueError("pages: the bytes of a tile must be adjacent")
-    block = size * 16 // (17 * dim)
-    if block * dim * 17 != size * 16:
+    block = size * 16 // (17 * dim) if dim else 0
+    if dim == 0 or block * dim * 17 != size * 16:
         raise ValueError(f"pages: {size} bytes are no tile of heads of {dim}")
     return pages.data_ptr(), sb, sh, n, block
 
