@@ -328,7 +328,7 @@ template <typename T, int G, int NT> struct Few {
     }
 
     // Every `stride`-th 32 keys from `from` on, the next ones' codes under way, the blocks of those behind them too.  Bound by reading: 4 tokens behind
-    // 200,003 keys (8 heads of 128, 218 MB) 43 us, 5.1 TB/s, 64 behind up to 8,001 of their own (279 MB) 64 us, where a kernel that only reads as much
+    // 200,003 keys (8 heads of 128, 218 MB) 43 us, 5.1 TB/s, 64 behind up to 8,001 of their own (279 MB) 70 us, where a kernel that only reads as much
     // takes 35 and 45.
     __device__ __forceinline__ void run(uint32_t from, uint32_t stride) {
         if (from >= it.end) return;
