@@ -58,8 +58,12 @@ __device__ __forceinline__ float norm_sum(float x, uint32_t bits) {
     return x;
 }
 
-// 1 / sqrt(mean + eps), to the last bit but one.
-__device__ __forceinline__ float norm_inverse(const NormArgs &a, float squares) { return __builtin_amdgcn_rsqf(__builtin_fmaf(squares, a.per_value, a.eps)); }
+// 1 / sqrt(mean + eps), to the last bit but one.  (The instruction takes numbers below 2^-126 for 0.)
+__device__ __forceinline__ float norm_inverse(const NormArgs &a, float squares) {
+    const float m = __builtin_fmaf(squares, a.per_value, a.eps);
+    const bool low = m < 0x1p-126f;
+    return __builtin_amdgcn_rsqf(low ? m * 0x1p64f : m) * (low ? 0x1p32f : 1.f);
+}
 
 // E floats from an address of 4 bytes.
 template <int E> struct NormFloats { float v[E]; };
@@ -253,6 +257,8 @@ template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_
     }
 }
 
+// In 32 bits, and not 0 where it is not.
+inline float norm_eps(double eps) { return eps > 0 ? std::fmax((float)eps, __FLT_DENORM_MIN__) : 0.f; }
 // Puts a tensor's heads into place i.  false if it is not there or not aligned to its values.
 SEQ_HIDDEN bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, const hps_seq_heads_t *back, int size);
 // Whether every row starts on 16 bytes, no vector holds pairs of two kinds, and `more`; sets the lanes of a head for either.

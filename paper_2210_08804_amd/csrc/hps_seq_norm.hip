@@ -158,7 +158,7 @@ NormArgs args_of(const hps_seq_norm_args_t &r) {
     a.table = r.table;
     a.x[0].weight = r.q_weight;
     a.x[1].weight = r.k_weight;
-    a.eps = (float)r.eps;
+    a.eps = norm_eps(r.eps);
     a.per_value = 1.f / (float)r.head_dim;
     a.n_tokens = r.n_tokens;
     a.head_dim = r.head_dim;
@@ -227,7 +227,7 @@ void norm_share(NormArgs &a, int i, uint32_t most_groups, uint32_t most_each) {
 hps_status_t norm_check(int dtype, uint32_t head_dim, uint32_t rot_dim, const float *table, const int32_t *positions, uint32_t max_pos, uint32_t n_tokens, double eps,
                         const float *q_weight, const float *k_weight) {
     if (hps_status_t st = seq_check_rope(dtype, head_dim, rot_dim, table, positions, max_pos, n_tokens)) return st;
-    SEQ_REQUIRE(std::isfinite(eps) && eps >= 0, "eps must be finite and >= 0");
+    SEQ_REQUIRE(eps >= 0 && eps <= __FLT_MAX__, "eps must be finite and >= 0");
     SEQ_REQUIRE(seq_aligned(q_weight, 4) && seq_aligned(k_weight, 4), "q_weight and k_weight must be 4-byte aligned");
     return HPS_OK;
 }

@@ -235,3 +235,30 @@ def test_gradients_by_differences():
         slope = (loss(1, what) - loss(-1, what)) / (2 * step)
         # third derivatives along a unit-size direction times step^2 / 6 (values and their derivatives are of size 1; 768 of them), and 32 bits' roundings over the step
         assert abs(slope - along) <= T * H * D * (step * step + 64 * 2.0 ** -24 / step)
+
+
+@pytest.mark.parametrize("size", [1e-15, 1e-18, 1e-19, 3e-20, 1e-20])
+@pytest.mark.parametrize("dim", [64, 63])
+def test_small_heads(size, dim):
+    """Mean squares on both sides of 2^-126, eps 0.  Below it a square, a sum of dim squares and their mean are each off by 2^-150 at most: the mean by 2^-149 in all, where it is
+    size^2 at least, and the root by half of that."""
+    g = torch.Generator().manual_seed(5)
+    x, dy = size * (1 + torch.rand(3, 2, dim, generator=g) / 2), torch.randn(3, 2, dim, generator=g)
+    y, dx = torch.empty_like(x).cuda(), torch.empty_like(x).cuda()
+    B.hps_seq_norm_rope(x.cuda(), y, eps=0.0)
+    B.hps_seq_norm_rope_grad(x.cuda(), dy.cuda(), dx, eps=0.0)
+    xd, d = x.double(), dy.double()
+    r = xd.square().mean(-1, keepdim=True).rsqrt()
+    n = xd * r
+    off = dim * 2.0 ** -24 + 2.0 ** -149 / size ** 2
+    assert ((y.cpu().double() - n).abs() <= off * n).all()
+    # r, n and the mean of d n (n <= 1.5) are each off by `off` at most: (1 + 2 * 1.5 * 1.5) * off, and the sum's own dim * 2^-24
+    expected = r * (d - n * (d * n).mean(-1, keepdim=True))
+    assert ((dx.cpu().double() - expected).abs() <= r * d.abs().amax(-1, keepdim=True) * 8 * off).all()
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e-38, 1e-41, 1e-60])
+def test_heads_of_zeros_stay_zeros(eps):
+    x, y = torch.zeros(2, 3, 64, device="cuda"), torch.ones(2, 3, 64, device="cuda")
+    B.hps_seq_norm_rope(x, y, eps=eps)
+    assert (y == 0).all()

@@ -38,7 +38,7 @@ def norm(**bad):
     return B._SEQ_NORM.pack(d["q"], 64, 64, d["k"], 64, 64, d["q_out"], 64, 64, d["k_out"], 64, 64, *list(d.values())[4:])
 
 
-NORM_BAD = [dict(q=0), dict(q_out=A + 2), dict(k=0), dict(k_out=0), dict(qw=A + 2), dict(kw=A + 1), dict(positions=0), dict(table=A + 4), dict(eps=-1e-6), dict(eps=math.inf),
+NORM_BAD = [dict(q=0), dict(q_out=A + 2), dict(k=0), dict(k_out=0), dict(qw=A + 2), dict(kw=A + 1), dict(positions=0), dict(table=A + 4), dict(eps=-1e-6), dict(eps=math.inf), dict(eps=1e39),
             dict(eps=math.nan), dict(n=1 << 31), dict(qh=65536), dict(dim=0), dict(dim=513), dict(rot=0), dict(rot=63), dict(rot=66), dict(max_pos=0), dict(max_pos=(1 << 31) + 1), dict(dtype=3),
             dict(dtype=-1)]
 
