@@ -51,15 +51,19 @@ struct hps_seq_attention_session {
 
 // What the host goes by where it cuts a call into work-groups.
 struct SeqAttendShape {
-    uint32_t wide_rows, narrow_rows, wide_keys, narrow_keys;                // rows of a work-group; keys of a step: of a wide work-group, of a narrow one's wave
+    uint32_t wide_rows, wide_keys, narrow_keys;        // rows of a wide work-group; keys of a step: of a wide work-group, of a narrow one's wave
+    uint32_t (*narrow_rows)(uint64_t most, uint32_t head_dim);              // rows of a narrow work-group, where the most rows that such ones serve behind a stretch are `most`
     uint32_t solo_keys;                                // own keys up to which a wave takes a request where there are many
     bool (*wide)(bool own, uint64_t rows, uint32_t keys, uint64_t stretches, uint32_t head_dim);              // whether rows share keys: `rows` behind each of so many stretches of keys
     uint32_t (*beside)(bool wide, uint32_t head_dim);  // work-groups of a CU at a time
     double (*step)(bool wide, double groups, double beside, uint32_t cus, double size);     // us; size: head_dim / 128
 };
 
-// Sets the launch's sizes in `a` and in the two numbers.
-SEQ_HIDDEN hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const hps_seq_attention_session &s, uint32_t &groups, uint32_t &parts);
+// A launch: its work-groups, the parts that they leave, the rows of narrow ones.
+struct SeqAttendCut { uint32_t groups, parts, narrow_rows; };
+
+// Sets the launch's sizes in `a` and `cut`.  What kind of work-groups histories and own tokens have is decided here and nowhere else: a.history_wide, a.own_mode.
+SEQ_HIDDEN hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const hps_seq_attention_session &s, SeqAttendCut &cut);
 // In front of the attention: flags histories that a bound of 0 keeps out of the launch.  Behind it: joins the parts.
 SEQ_HIDDEN hipError_t seq_attend_check(const SeqAttendArgs &a, hipStream_t st);
 SEQ_HIDDEN hipError_t seq_attend_join(const SeqAttendArgs &a, int dtype, uint32_t parts, hipStream_t st);

@@ -254,7 +254,9 @@ uint32_t choose_chunks(const SeqAttendShape &shape, uint64_t tiles, uint32_t key
 // key heads of 128: 64 requests of 64 / 256 / 512 keys 14.6, 21.9, 32.4 / 13.9, 14.9, 19.9; 512 of 64 / 256 / 512 / 1,024 keys 26.2, 38.0,
 // 63.2, 134.1 / 43.6, 50.6, 69.6, 129.2).
 constexpr SeqAttendShape kShape = {
-    kWideRows, kNarrowRows, kWideKeys, kNarrowKeys, 512,
+    kWideRows, kWideKeys, kNarrowKeys,
+    [](uint64_t, uint32_t) { return kNarrowRows; },
+    512,
     [](bool own, uint64_t rows, uint32_t keys, uint64_t, uint32_t) { return rows > (!own && keys >= 16384 ? 2 : 1) * kNarrowRows; },
     [](bool, uint32_t head_dim) { return head_dim <= 128 ? 2u : 1u; },
     [](bool wide, double n, double beside, uint32_t cus, double size) { return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(2.2, beside * 0.0121 * size); },
@@ -316,19 +318,24 @@ template <typename T> hipError_t launch_join(const Args &a, uint32_t parts, hipS
 
 }  // namespace
 
-hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const hps_seq_attention_session &s, uint32_t &groups, uint32_t &parts) {
+hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const hps_seq_attention_session &s, SeqAttendCut &cut) {
     const uint64_t rows = (uint64_t)a.n_tokens * a.q_heads, part_limit = s.part_rows / rows;
     // own tokens: one part at least, so that every row has one
     const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, requests_heads = (uint64_t)a.n_requests * a.kv_heads;
+    const uint64_t group_rows = a.n_groups && a.max_prefix ? (uint64_t)a.max_group * a.ratio : 0;
     const uint32_t own_keys = a.max_len ? a.max_len : 1;
-    if (shape.wide(true, own_rows, own_keys, requests_heads, a.head_dim)) {
+    const bool own_wide = shape.wide(true, own_rows, own_keys, requests_heads, a.head_dim);
+    a.history_wide = group_rows && shape.wide(false, group_rows, a.max_prefix, (uint64_t)a.n_groups * a.kv_heads, a.head_dim);
+    const uint64_t own_narrow = own_wide ? 0 : own_rows, group_narrow = a.history_wide ? 0 : group_rows;
+    const uint32_t narrow_rows = cut.narrow_rows = shape.narrow_rows(own_narrow > group_narrow ? own_narrow : group_narrow, a.head_dim);
+    if (own_wide) {
         a.own_mode = kOwnWide;
         a.own_tiles = div_up(own_rows, shape.wide_rows);
         a.own_chunks = choose_chunks(shape, requests_heads * a.own_tiles, own_keys, true, rows, a.head_dim, s.cus, part_limit / 2);
         a.own_chunk = div_up(div_up(own_keys, a.own_chunks), shape.wide_keys) * shape.wide_keys;
     } else {
         a.own_mode = requests_heads > 2 * s.cus && own_keys <= shape.solo_keys ? kOwnSolo : kOwnSplit;
-        a.own_tiles = div_up(own_rows, shape.narrow_rows);
+        a.own_tiles = div_up(own_rows, narrow_rows);
         const uint32_t step = a.own_mode == kOwnSolo ? shape.narrow_keys : shape.narrow_keys * kWaves;
         a.own_chunks = a.own_mode == kOwnSolo ? 1 : choose_chunks(shape, requests_heads * a.own_tiles, own_keys, false, rows, a.head_dim, s.cus, part_limit / 2);
         a.own_chunk = div_up(div_up(own_keys, a.own_chunks), step) * step;
@@ -336,10 +343,8 @@ hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const
     if (a.own_tiles == 0) a.own_tiles = 1;
     const uint64_t own_items = requests_heads * a.own_tiles * a.own_chunks, own_groups = a.own_mode == kOwnSolo ? (own_items + kWaves - 1) / kWaves : own_items;
     uint64_t history_groups = 0;
-    if (a.n_groups && a.max_prefix && a.max_group) {
-        const uint64_t group_rows = (uint64_t)a.max_group * a.ratio;
-        a.history_wide = shape.wide(false, group_rows, a.max_prefix, (uint64_t)a.n_groups * a.kv_heads, a.head_dim);
-        a.history_tiles = div_up(group_rows, a.history_wide ? shape.wide_rows : shape.narrow_rows);
+    if (group_rows) {
+        a.history_tiles = div_up(group_rows, a.history_wide ? shape.wide_rows : narrow_rows);
         const uint32_t step = a.history_wide ? shape.wide_keys : shape.narrow_keys * kWaves;
         a.history_chunks = choose_chunks(shape, (uint64_t)a.history_tiles * a.n_groups * a.kv_heads, a.max_prefix, a.history_wide, rows, a.head_dim, s.cus, part_limit - a.own_chunks);
         a.history_chunk = div_up(div_up(a.max_prefix, a.history_chunks), step) * step;
@@ -359,9 +364,9 @@ hps_status_t seq_attend_cut(SeqAttendArgs &a, const SeqAttendShape &shape, const
     a.by_history_chunks = divisor(a.history_chunks);
     a.by_own_chunks = divisor(a.own_chunks);
     a.by_own_tiles = divisor(a.own_tiles);
-    parts = a.history_chunks + a.own_chunks;
-    a.direct = parts == 1;
-    groups = (uint32_t)(history_groups + own_groups);
+    cut.parts = a.history_chunks + a.own_chunks;
+    a.direct = cut.parts == 1;
+    cut.groups = (uint32_t)(history_groups + own_groups);
     return HPS_OK;
 }
 
@@ -459,12 +464,12 @@ hps_status_t hps_seq_attention(hps_seq_attention_t *s, const hps_seq_attention_a
     a.page_block = (uint32_t)(r.pages.block_stride * 2);
     a.page_token = (uint32_t)(r.pages.token_stride * 2);
     a.page_head = r.pages.head_stride * 2;
-    uint32_t groups, parts;
-    if (hps_status_t st = seq_attend_cut(a, kShape, *s, groups, parts)) return st;
+    SeqAttendCut cut;
+    if (hps_status_t st = seq_attend_cut(a, kShape, *s, cut)) return st;
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(seq_attend_check(a, st));
-    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, groups, st) : launch<__bf16>(a, groups, st));
-    SEQ_TRY(seq_attend_join(a, r.dtype, parts, st));
+    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, cut.groups, st) : launch<__bf16>(a, cut.groups, st));
+    SEQ_TRY(seq_attend_join(a, r.dtype, cut.parts, st));
     return HPS_OK;
 }
 

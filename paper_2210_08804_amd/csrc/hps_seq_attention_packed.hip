@@ -850,6 +850,12 @@ uint32_t beside(bool wide, uint32_t head_dim) { return head_dim > 128 ? (wide ? 
 double step_time(bool wide, double n, double beside, uint32_t cus, double size) {
     return wide ? (n <= cus ? 1.33 : 1.9) * (0.35 + 0.65 * size) : std::fmax(0.32 + 0.68 * size, std::ceil(beside / cus) * (0.17 + 0.7 * size));
 }
+// Rows of a tile of few: 16 where all that are served so fit one, else 32 (heads up to 128, whose registers suffice).  (Measured, us a call, 16 / 32: 16 rows,
+// 200,003 keys 50.8 / 55.6, of 64 values 32.3 / 40.1; 32 rows, 65,536 keys 30.0 / 27.1, 96 rows 59.9 / 49.8; 512 rows, 8,192 keys 45.0 / 38.2; where there are few
+// keys 16 can be ahead too: 192 rows, 1,000 keys 13.3 / 15.3.)
+uint32_t narrow_rows(uint64_t most, uint32_t head_dim) { return head_dim <= 128 && most > 16 ? 32u : 16u; }
+
+constexpr SeqAttendShape kShape = {kWideRows, kWideKeys, 32, narrow_rows, 512, wide_rows, beside, step_time};
 
 }  // namespace
 
@@ -875,20 +881,13 @@ hps_status_t hps_seq_attention_packed(hps_seq_attention_t *s, const hps_seq_atte
         a.k = reinterpret_cast<const char *>(s->part_o);
         a.packed_block = a.page_head = 0;
     }
-    // rows of a tile of few: 16 where all that are served so fit one, else 32 (heads up to 128, whose registers suffice).  (Measured, us a call, 16 / 32: 16 rows,
-    // 200,003 keys 50.8 / 55.6, of 64 values 32.3 / 40.1; 32 rows, 65,536 keys 30.0 / 27.1, 96 rows 59.9 / 49.8; 512 rows, 8,192 keys 45.0 / 38.2; where there are few
-    // keys 16 can be ahead too: 192 rows, 1,000 keys 13.3 / 15.3.)
-    const uint64_t own_rows = (uint64_t)a.max_new * a.ratio, group_rows = r.n_groups && r.max_prefix ? (uint64_t)a.max_group * a.ratio : 0;
-    const bool own_many = wide_rows(true, own_rows, r.max_len, (uint64_t)r.n_requests * r.kv_heads, r.head_dim);
-    const bool group_many = group_rows && wide_rows(false, group_rows, r.max_prefix, (uint64_t)r.n_groups * r.kv_heads, r.head_dim);
-    const bool two = r.head_dim <= 128 && ((!own_many && own_rows > 16) || (!group_many && group_rows > 16));
-    const SeqAttendShape shape = {kWideRows, two ? 32u : 16u, kWideKeys, 32, 512, wide_rows, beside, step_time};
-    uint32_t groups, parts;
-    if (hps_status_t st = seq_attend_cut(a, shape, *s, groups, parts)) return st;
+    SeqAttendCut cut;
+    if (hps_status_t st = seq_attend_cut(a, kShape, *s, cut)) return st;
+    const bool mixed = a.own_mode == kOwnWide || a.history_wide, two = cut.narrow_rows == 32;
     hipStream_t st = static_cast<hipStream_t>(stream);
     SEQ_TRY(seq_attend_check(a, st));
-    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, own_many || group_many, two, groups, st) : launch<__bf16>(a, own_many || group_many, two, groups, st));
-    SEQ_TRY(seq_attend_join(a, r.dtype, parts, st));
+    SEQ_TRY(r.dtype == HPS_SEQ_F16 ? launch<_Float16>(a, mixed, two, cut.groups, st) : launch<__bf16>(a, mixed, two, cut.groups, st));
+    SEQ_TRY(seq_attend_join(a, r.dtype, cut.parts, st));
     return HPS_OK;
 }
 

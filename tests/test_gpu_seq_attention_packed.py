@@ -491,3 +491,20 @@ def test_a_step_of_a_server(dtype):
             t += n
         past, info = lens, more
     B.hps_seq_attention_destroy(s)
+
+
+@pytest.mark.parametrize("bounds", [{}, dict(max_new=16)])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_many_requests_without_anything_to_attend_to(D, bounds):
+    """Tables of width 0 and no history: every row gets 0, whichever kernel the number of rows asks for."""
+    n, new, H, K = 512, 16, 32, 8
+    q = torch.ones(n * new, H, D, dtype=BF, device="cuda")
+    out, lse = torch.full_like(q, 9.0), torch.full((n * new, H), 9.0, device="cuda")
+    pages = torch.zeros(4, K, B.hps_seq_packed_bytes(16, D), dtype=torch.uint8, device="cuda")
+    offsets = torch.arange(0, n * new + 1, new, dtype=torch.int32, device="cuda")
+    s = B.hps_seq_attention_create(n * new * H, D)
+    B.hps_seq_attention_packed(s, q, pages, torch.empty(n, 0, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), offsets, out, lse=lse, **bounds)
+    torch.cuda.synchronize()
+    flags = B.hps_seq_attention_flags(s)
+    B.hps_seq_attention_destroy(s)
+    assert flags == 0 and (out == 0).all() and (lse == -math.inf).all()
