@@ -158,7 +158,8 @@ struct Item {
 };
 constexpr int32_t kAll = 0x7FFFFFFF;
 
-template <typename T, int DT, bool kExact> struct Engine {                  // head_dim <= 32 * DT, or just that
+// kCleared: places of LDS rows that no load fills are zeros.
+template <typename T, int DT, bool kExact, bool kCleared = true> struct Engine {            // head_dim <= 32 * DT, or just that
     typedef typename Type<T>::frag frag;
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     static constexpr int kRow = DT <= 2 ? 128 : DT <= 4 ? 256 : 512;        // bytes of a row in LDS
@@ -331,12 +332,14 @@ template <typename T, int DT, bool kExact> struct Engine {                  // h
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = Type<T>::mfma(values<kAt + 16 * kRow>(d), w[1], o[d]);
     }
-    // Whether any value of 32 keys, kAt bytes behind the first ones, is not finite.
+    // Whether any value of 32 keys, kAt bytes behind the first ones, is not finite.  (Where places that the head does not
+    // fill are not cleared they hold what an earlier kernel left, and have no say.)
     template <int kAt> __device__ __forceinline__ bool any_odd() const {
         constexpr uint32_t e = Type<T>::kExp;
         uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < 2 * kLoads; ++i) {
+            if (!kCleared && !kFull && (lane % kChunks ^ sw_v(i * kLoadRows + lane / kChunks)) >= 4 * DT) continue;
             const u32x4 y = *(lds_u32x4 *)((lds_char *)(uintptr_t)(here + lane * 16) + kAt + i * 1024);
 #pragma unroll
             for (int j = 0; j < 4; ++j) odd |= (uint32_t)((y[j] & e) == e) | (uint32_t)((y[j] >> 16 & e) == e);

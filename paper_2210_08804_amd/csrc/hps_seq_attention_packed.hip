@@ -436,8 +436,8 @@ template <typename T, int G, int NT> struct Few {
 
 // ---- many rows
 
-template <typename T, int G> struct Wide : Engine<T, G, true> {
-    typedef Engine<T, G, true> E;
+template <typename T, int G> struct Wide : Engine<T, G, true, false> {
+    typedef Engine<T, G, true, false> E;
     typedef typename E::frag frag;
     typedef __attribute__((address_space(3))) uint32_t lds1;
     typedef __attribute__((address_space(3))) u32x2 lds2;

@@ -508,3 +508,28 @@ def test_many_requests_without_anything_to_attend_to(D, bounds):
     flags = B.hps_seq_attention_flags(s)
     B.hps_seq_attention_destroy(s)
     assert flags == 0 and (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+def test_many_rows_do_not_see_what_a_kernel_left(D, dtype):
+    """The same bits, whether the kernel in front left zeros or infinities in the LDS of every CU."""
+    def leave(x):
+        pages, out = torch.full((4, 64, 16, 256), x, dtype=BF, device="cuda"), torch.empty(128, 16, 256, dtype=BF, device="cuda")
+        s = B.hps_seq_attention_create(128 * 16, 256)
+        B.hps_seq_attention(s, torch.ones_like(out), pages, pages.clone(), torch.arange(4, dtype=torch.int32, device="cuda").repeat(128, 1),
+                            torch.full((128,), 256, dtype=torch.int32, device="cuda"), torch.arange(129, dtype=torch.int32, device="cuda"), out, max_new=1)
+        torch.cuda.synchronize()
+        B.hps_seq_attention_destroy(s)
+
+    p = Shared(dtype, D, 8, 1, 32, [(200, 6)], MANY, seed=D)
+    p.q[:] = 0                                         # equal weights, and values that cancel: sums in another order are other sums
+    for table, n in zip(p.block_table, p.lens.tolist()):
+        for i in range(n):
+            at, big = (int(table[i // 32]), i % 32), torch.randn(1, D, generator=torch.Generator().manual_seed(i // 3))
+            p.v[at] = (big * (2.0 ** 10, -2.0 ** 10, 2.0 ** -12)[i % 3]).to(dtype)
+    leave(0.0)
+    want = p.run()
+    leave(math.inf)
+    got = p.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
