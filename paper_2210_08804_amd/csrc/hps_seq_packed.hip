@@ -82,7 +82,7 @@ __device__ __forceinline__ void odd_floats(const double (&y)[8], float (&x)[8]) 
         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
         : "v"(y[0]), "v"(y[1]), "v"(y[2]), "v"(y[3]), "v"(y[4]), "v"(y[5]), "v"(y[6]), "v"(y[7]));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(__float_as_uint(x[j]) | min((uint32_t)__builtin_bit_cast(uint64_t, y[j]) & 0x1FFFFFFFu, 1u));
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(__float_as_uint(x[j]) | (uint32_t)((double)x[j] != y[j]));     // below 2^-126 too, where more than 29 bits are cut
 }
 
 // 1 / sqrt(x): the instruction's 2^-26 or so, and a step that leaves the third power of it.

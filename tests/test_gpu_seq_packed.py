@@ -234,3 +234,18 @@ def test_stream_of_its_own_and_graphs():
         assert torch.equal(q_out.cpu(), eager_q) and torch.equal(pages.cpu(), eager_pages)
         for x, w in zip(read, P.unpacked(eager_pages, 16, 128)):
             assert torch.equal(x.cpu().double(), w.transpose(1, 2).flatten(0, 1)[c.slots.long()])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_keys_next_to_a_border_of_the_least_scale(dtype, interleaved):
+    """The same among numbers below 2^-126, of which 32 bits tell less the smaller they are."""
+    middles = torch.tensor([.25, .75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0]) * 2.0 ** -126
+    for off in (2.0 ** -22, 2.0 ** -24, 2.0 ** -40, 2.0 ** -49, 0.0):
+        for sign in (1, -1):
+            c = Case(dtype, 1, 0, 1, 64, 16, 64, norm=False, seed=12)
+            c.row[:] = 2.0 ** -60
+            cos = middles.repeat(4) * 2.0 ** 60
+            c.table = torch.stack((cos, torch.full_like(cos, sign * off * 2.0 ** -66)), -1)[None]
+            c.positions[:] = 0
+            c.check(interleaved)
