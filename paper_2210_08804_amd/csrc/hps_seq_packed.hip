@@ -85,10 +85,10 @@ __device__ __forceinline__ void odd_floats(const double (&y)[8], float (&x)[8]) 
     for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(__float_as_uint(x[j]) | (uint32_t)((double)x[j] != y[j]));     // below 2^-126 too, where more than 29 bits are cut
 }
 
-// 1 / sqrt(x): the instruction's 2^-26 or so, and a step that leaves the third power of it.
+// 1 / sqrt(x): the instruction's 2^-26 or so, and a step that leaves the third power of it.  (0 for infinity, which the step would make no number.)
 __device__ __forceinline__ double inverse_root(double x) {
-    const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0);
-    return __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
+    const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0), z = __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
+    return y == 0.0 ? 0.0 : z;
 }
 
 // Eight values' codes.  The conversion takes 32 bits, rounds to the nearest, of two to the even code, and ends at 6.

@@ -249,3 +249,16 @@ def test_keys_next_to_a_border_of_the_least_scale(dtype, interleaved):
             c.table = torch.stack((cos, torch.full_like(cos, sign * off * 2.0 ** -66)), -1)[None]
             c.positions[:] = 0
             c.check(interleaved)
+
+
+@pytest.mark.parametrize("odd", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("D", [64, 96, 256])
+def test_normed_keys_that_are_infinite(D, odd):
+    """An infinite key divides the others of its head by infinity, to zeros of either sign; one that is no number spoils its head."""
+    for rot, at in ((None, 3), (D, 40), (D // 2, D - 1)):
+        c = Case(BF, 5, 2, 2, D, 16, rot, seed=13)
+        c.row[2, 2 * D + at] = odd
+        _, pages = c.run()
+        _, _, want, mask = c.want()
+        for got, expected in zip(P.unpacked(pages, 16, D), P.unpacked(want, 16, D)):
+            assert torch.equal(torch.isnan(got), torch.isnan(expected)) and torch.equal(got.nan_to_num(7.25), expected.nan_to_num(7.25))
