@@ -238,7 +238,8 @@ hps_status_t hps_seq_attention_flags(hps_seq_attention_t *s, uint32_t *flags, in
  * head_dim <= 512 values, a weight for each value (fp32 [head_dim], the tensor's own; NULL = ones), and the turning of
  * hps_seq_rope with its conventions (a token with a negative position is passed over; turned values are NaN at
  * positions of max_pos or more).  table NULL: nothing is turned and positions is not read.  Arithmetic is in 32 bits,
- * rounded once; a head whose squares sum to more than 32 bits hold comes out as 0, and mean squares below 2^-126 lose bits.  A tensor of 0 heads may have
+ * rounded once, at any size of a head that the type holds (where its squares are beyond 32 bits, or below, it is scaled by a power of
+ * two first); beside an infinite value the others of its head come out as 0.  A tensor of 0 heads may have
  * NULL data; an output may be its input, exactly.  eps >= 0, finite in 32 bits.
  */
 typedef struct {

@@ -19,10 +19,10 @@ struct NormArgs {
     const int32_t *positions;
     const float *table;
     float *parts, *weight_grad[2];
-    float eps, per_value;                              // 1 / head_dim
+    float eps, eps_small, per_value;                   // eps_small: eps * 2^200; 1 / head_dim
     uint32_t n_tokens, head_dim, half, max_pos, lane_bits;                  // half = rot_dim / 2; lanes of a head: 1 << lane_bits
     uint32_t first_group;                              // of this launch
-    int32_t interleaved, norm;
+    int16_t interleaved, norm;                         // of 16 bits: a call whose arguments are over 272 bytes takes 0.2 us more
 };
 
 constexpr uint32_t kNormThreads = 256;
@@ -58,12 +58,20 @@ __device__ __forceinline__ float norm_sum(float x, uint32_t bits) {
     return x;
 }
 
-// 1 / sqrt(mean + eps), to the last bit but one.  (The instruction takes numbers below 2^-126 for 0.)
-__device__ __forceinline__ float norm_inverse(const NormArgs &a, float squares) {
-    const float m = __builtin_fmaf(squares, a.per_value, a.eps);
+// 1 / sqrt(m), to the last bit but one.  (The instruction takes numbers below 2^-126 for 0.)
+__device__ __forceinline__ float norm_inverse(float m) {
     const bool low = m < 0x1p-126f;
     return __builtin_amdgcn_rsqf(low ? m * 0x1p64f : m) * (low ? 0x1p32f : 1.f);
 }
+
+// Heads whose squares 32 bits do not hold, small ones (with an eps as small: their mean m = mean(x^2) + eps lost bits) and large ones (m is infinite): they
+// are multiplied by a power of two, and m is formed anew.  Any other head keeps its m, bit for bit, and a wave of such heads pays for the question alone (0 to 1.5 % of a call).
+struct NormFit {
+    float by, eps;
+    static __device__ __forceinline__ bool needed(float m) { return !(m >= 0x1p-90f && m < __builtin_inff()); }
+    __device__ __forceinline__ NormFit(const NormArgs &a, float m)
+        : by(m < 0x1p-90f ? 0x1p100f : m == __builtin_inff() ? 0x1p-72f : 1.f), eps(m < 0x1p-90f ? a.eps_small : m == __builtin_inff() ? a.eps * 0x1p-72f * 0x1p-72f : a.eps) {}
+};
 
 // E floats from an address of 4 bytes.
 template <int E> struct NormFloats { float v[E]; };
@@ -242,7 +250,20 @@ template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
                 for (int j = 0; j < 2 * E; ++j) sum = __builtin_fmaf(x[i][j], x[i][j], sum);
-            r = norm_inverse(a, norm_sum(sum, a.lane_bits));
+            float m = __builtin_fmaf(norm_sum(sum, a.lane_bits), a.per_value, a.eps);
+            if (__builtin_expect(__ballot(NormFit::needed(m)) != 0, 0)) {
+                const NormFit fit(a, m);
+                sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) {
+                        x[i][j] *= fit.by;
+                        sum = __builtin_fmaf(x[i][j], x[i][j], sum);
+                    }
+                m = __builtin_fmaf(norm_sum(sum, a.lane_bits), a.per_value, fit.eps);
+            }
+            r = norm_inverse(m);
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -259,6 +280,10 @@ template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_
 
 // In 32 bits, and not 0 where it is not.
 inline float norm_eps(double eps) { return eps > 0 ? std::fmax((float)eps, __FLT_DENORM_MIN__) : 0.f; }
+inline void norm_set_eps(NormArgs &a, double eps) {
+    a.eps = norm_eps(eps);
+    a.eps_small = norm_eps(std::fmin(eps, 0x1p-80) * 0x1p200);              // not read where eps is larger
+}
 // Puts a tensor's heads into place i.  false if it is not there or not aligned to its values.
 SEQ_HIDDEN bool norm_put(NormArgs &a, int i, uint32_t heads, const hps_seq_heads_t &in, const hps_seq_heads_t &out, const hps_seq_heads_t *back, int size);
 // Whether every row starts on 16 bytes, no vector holds pairs of two kinds, and `more`; sets the lanes of a head for either.

@@ -57,8 +57,41 @@ template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_
                     products = __builtin_fmaf(z[i][j] * sp[i].w[j], x[i][j], products);
                 }
             }
-            const float r = norm_inverse(a, norm_sum(squares, a.lane_bits));
-            const float c = norm_sum(products, a.lane_bits) * r * a.per_value;
+            const float m = __builtin_fmaf(norm_sum(squares, a.lane_bits), a.per_value, a.eps);
+            products = norm_sum(products, a.lane_bits);
+            float r = norm_inverse(m), c = products * r * a.per_value;
+            // products alone may be beyond what 32 bits hold, or below: then their sum is formed of n, as for a head that does not fit
+            const bool odd = NormFit::needed(m) || !(__builtin_fabsf(products) >= 0x1p-100f && __builtin_fabsf(products) < __builtin_inff());
+            if (__builtin_expect(__ballot(odd) != 0, 0)) {
+                const NormFit fit(a, m);
+                squares = products = 0.f;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) {
+                        const float y = x[i][j] * fit.by;
+                        squares = __builtin_fmaf(y, y, squares);
+                    }
+                r = norm_inverse(__builtin_fmaf(norm_sum(squares, a.lane_bits), a.per_value, fit.eps));
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) {
+                        float y = x[i][j], w = sp[i].w[j];                  // nothing that the other way has: kept for here it costs a wave of a SIMD
+                        asm("" : "+v"(y), "+v"(w));
+                        products = __builtin_fmaf(z[i][j] * w, y * fit.by * r, products);
+                    }
+                products = norm_sum(products, a.lane_bits) * a.per_value;
+                c = odd ? products : c;                // a head that fits keeps its bits beside one that does not
+                // back to the head as it is, whose r may itself be beyond 32 bits: with r / k, k dz and k^2 c for r, dz and c the gradients are what they were
+                const float k = fit.by > 1.f && r > 0x1p20f ? 0x1p28f : fit.by < 1.f && r < 0x1p-48f ? 0x1p-4f : 1.f;
+                r *= fit.by / k;
+                c *= k * k;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) z[i][j] *= k;
+            }
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
 #pragma unroll
@@ -158,7 +191,7 @@ NormArgs args_of(const hps_seq_norm_args_t &r) {
     a.table = r.table;
     a.x[0].weight = r.q_weight;
     a.x[1].weight = r.k_weight;
-    a.eps = norm_eps(r.eps);
+    norm_set_eps(a, r.eps);
     a.per_value = 1.f / (float)r.head_dim;
     a.n_tokens = r.n_tokens;
     a.head_dim = r.head_dim;

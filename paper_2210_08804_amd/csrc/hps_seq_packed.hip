@@ -377,7 +377,7 @@ hps_status_t hps_seq_append_packed(const hps_seq_append_packed_args_t *args, voi
     n.positions = r.positions;
     n.table = r.table;
     n.x[0].weight = r.q_weight;
-    n.eps = norm_eps(r.eps);
+    norm_set_eps(n, r.eps);
     n.per_value = 1.f / (float)r.head_dim;
     n.n_tokens = r.n_tokens;
     n.head_dim = r.head_dim;

@@ -262,3 +262,33 @@ def test_heads_of_zeros_stay_zeros(eps):
     x, y = torch.zeros(2, 3, 64, device="cuda"), torch.ones(2, 3, 64, device="cuda")
     B.hps_seq_norm_rope(x, y, eps=eps)
     assert (y == 0).all()
+
+
+SIZES = [(F32, s) for s in (1e-42, 1e-38, 1e-30, 1e-24, 1e-22, 1e19, 1e20, 1e30, 1e38)] + [(BF, s) for s in (1e-38, 1e-30, 1e-22, 1e20, 1e38)]
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,size", SIZES)
+def test_heads_of_any_size(dtype, size, interleaved):
+    """Heads whose squares 32 bits do not hold, beside ordinary ones; gradients of them too."""
+    for D, rot, eps in ((64, 64, 0.0), (64, None, 0.0), (63, 32, 0.0), (128, 64, min(size * size / 4, 1e-6)), (64, 32, min(size * size * 1e-6, 1e30))):
+        h = Heads(dtype, 5, 3, 2, D, rot, seed=16)
+        odd, (q, k) = h.row.clone(), h.cut(h.row)
+        for x in h.cut(odd):
+            x.copy_((x.double().clamp(-2, 2) * size).to(dtype))
+        h.row[1], h.row[4] = odd[1], odd[4]
+        h.cut(h.row)[0][2, 1] = h.cut(odd)[0][2, 1]    # one of a token's heads
+        h.check(eps=eps, interleaved=interleaved)
+        if size < 1:
+            h.back = (h.back.double() * max(size, 1e-20) ** 0.5).to(dtype)
+        h.check_grads(eps=eps, interleaved=interleaved)
+
+
+def test_gradients_whose_products_are_large_or_small():
+    """Values and gradients whose products' sum 32 bits do not hold, where they hold the heads' gradients."""
+    h = Heads(F32, 3, 2, 1, 64, 64, seed=17)
+    h.row[1] *= 1e18
+    h.back[1] *= 1e22
+    h.row[2] *= 1e-12
+    h.back[2] *= 1e-32
+    h.check_grads(eps=0.0)

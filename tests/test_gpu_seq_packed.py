@@ -262,3 +262,10 @@ def test_normed_keys_that_are_infinite(D, odd):
         _, _, want, mask = c.want()
         for got, expected in zip(P.unpacked(pages, 16, D), P.unpacked(want, 16, D)):
             assert torch.equal(torch.isnan(got), torch.isnan(expected)) and torch.equal(got.nan_to_num(7.25), expected.nan_to_num(7.25))
+
+
+def test_queries_and_keys_of_any_size():
+    for size in (1e-30, 1e-22, 1e20):
+        c = Case(BF, 9, 2, 2, 64, 16, 64, seed=18)
+        c.row[:, :] = (c.row.double() * size).to(BF)
+        c.check(eps=0.0)
