@@ -26,13 +26,13 @@ FLAGS = [
 
 
 def build(extra=()):
-    """Every source at a time, each into an object of its own, then the library."""
+    """Every source at a time, each into an object of its own, then the library; `extra` goes to the compilations and to the link."""
     with tempfile.TemporaryDirectory() as d:
         objects = [os.path.join(d, os.path.basename(s) + ".o") for s in SRCS]
         compile_one = lambda s, o: subprocess.run([HIPCC, *FLAGS, *extra, "-c", s, "-o", o], check=True)  # noqa: E731
         with ThreadPoolExecutor(min(len(SRCS), os.cpu_count() or 1)) as pool:
             list(pool.map(compile_one, SRCS, objects))
-        subprocess.run([HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB, "-lpthread"], check=True)
+        subprocess.run([HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", *extra, *objects, "-o", LIB, "-lpthread"], check=True)
     return LIB
 
 
