@@ -533,3 +533,52 @@ def test_many_rows_do_not_see_what_a_kernel_left(D, dtype):
     leave(math.inf)
     got = p.run()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 256])
+def test_hidden_groups_of_every_head_size(D, dtype):
+    """Groups of keys and of values behind a query's own place that are no numbers, in each of a head's groups."""
+    for kind, H, K, new in ((Packed, 4, 4, 13), (Packed, 4, 2, 13), (Packed, 16, 2, 20), (Shared, 16, 1, 16), (Shared, 32, 2, 24)):      # up to 16 rows, up to 32, more, many
+        for group in range(D // 32):
+            p = kind(dtype, D, H, K, 16, [(50, 1)], [(40, new)], seed=5)
+            p.v[int(p.block_table[0, 2]), 6, 0, 32 * group + 7 * group % 32] = math.nan         # token 38
+            p.v[int(p.block_table[0, 1]), 15, K - 1, 32 * group + 31] = math.inf                # token 31
+            out, lse = p.run()
+            want, want_lse, bound, lse_bound = p.want()
+            assert torch.isnan(out[-1]).any() and torch.isfinite(lse).all()
+            R.close(out, want, bound)
+            R.close(lse, want_lse, lse_bound)
+            p.k[int(p.block_table[0, 2]), 5, :, 32 * group + 9] = math.nan                      # token 37: a group of every head
+            out, lse = p.run()
+            first = 37 - (40 - new)
+            assert torch.isnan(out[first:]).all() and torch.isnan(lse[first:]).all()
+            R.close(out[:first], want[:first], bound[:first])
+            R.close(lse[:first], want_lse[:first], lse_bound[:first])
+
+
+@pytest.mark.parametrize("D", [32, 96, 128, 256])
+@pytest.mark.parametrize("kind,H,K,new", [(Packed, 2, 2, 1), (Packed, 16, 1, 9), (Shared, 16, 1, 16)])
+def test_scales_beyond_the_type_of_every_head_size(kind, H, K, new, D):
+    """The same for each of a head's groups, of values and of keys."""
+    for dtype, last in ((BF, 252), (HF, 140)):
+        for group in range(D // 32):
+            p = kind(dtype, D, H, K, 16, [(40, 1)], [(new, new)], seed=7)
+            tiles = p.tiles()
+            _, _, ks, vs = P.places(16, D)
+            b = int(p.prefix_table[0, 1])
+            tiles[b, 0, vs[3, group]], tiles[b, 0, ks[5, group]] = 0, 0
+            p.tiles = lambda: tiles  # noqa: B023
+            p.check()
+            for byte in (last + 1, 255):
+                tiles[b, 0, vs[3, group]] = byte
+                out, lse = p.run()
+                want, _, bound, _ = p.want()
+                spoilt = torch.zeros(D, dtype=torch.bool)
+                spoilt[32 * group:32 * group + 32] = True
+                assert torch.isnan(out[:, :H // K, spoilt]).all() and torch.isfinite(out[:, :, ~spoilt]).all() and torch.isfinite(lse).all()
+                R.close(out, want, bound)
+            tiles[b, 0, vs[3, group]], tiles[b, 0, ks[5, group]] = 0, last + 1
+            out, lse = p.run()
+            assert torch.isnan(out[:, :H // K]).all() and torch.isnan(lse[:, :H // K]).all()
+            assert torch.isfinite(out[:, H // K:]).all() and torch.isfinite(lse[:, H // K:]).all()
