@@ -261,7 +261,8 @@ hps_status_t hps_seq_norm_rope(const hps_seq_norm_args_t *args, void *stream);
  * outputs (read here).  q_grad and k_grad receive those of its inputs, in the tensors' type (each may be the
  * matching input or output gradient, exactly); q_weight_grad and k_weight_grad [head_dim] fp32 those of the weights,
  * summed over all tokens and heads (overwritten; NULL: not wanted; 0 for a tensor without heads or tokens).  Sums are
- * in 32 bits and in an order that depends on the sizes alone.  Tokens that are passed over have no part in the
+ * in 32 bits and in an order that depends on the sizes, the kind of pairs and whether every row starts on 16 bytes, so that
+ * the same call gives the same bits.  Tokens that are passed over have no part in the
  * sums, and their rows of q_grad and k_grad are not written.  parts: scratch memory of 2 * HPS_SEQ_NORM_PARTS * head_dim
  * floats, needed where a weight's gradient is; calls that share it must not overlap (replays of captured graphs included).
  */

@@ -862,6 +862,7 @@ def hps_seq_read_packed(pages, slots, k_out=None, v_out=None, stream=None) -> No
     if status:
         _check_seq(status)
 
+
 def hps_seq_attention_packed(session, q, pages, block_table, lens, token_offsets, out, prefix_table=None, prefix_lens=None, group_offsets=None,
                              lse=None, scale=None, max_new=None, max_len=None, max_prefix=None, max_group=None, stream=None) -> None:
     """hps_seq_attention over packed pages uint8 [blocks, kv heads, hps_seq_packed_bytes(block size, dim)]; the other arguments are as there."""

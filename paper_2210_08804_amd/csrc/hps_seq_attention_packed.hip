@@ -63,8 +63,7 @@ template <int G> __device__ __forceinline__ uint32_t value_group(uint32_t c, int
 template <int G> constexpr int key_scale(int s) { return G == 3 ? s : G == 8 ? s / 4 : 0; }
 template <int G> constexpr int value_scale(int p) { return G == 3 ? p : 0; }
 
-// kBytes bytes of a tile, in dwords (the last one may be part of one).
-template <int kWords> struct Words { uint32_t w[kWords]; };
+// kWords dwords of a tile from an address that is a multiple of kAlign bytes, in the widest loads that allows.
 template <int kWords, int kAlign> __device__ __forceinline__ void load_words(const char *from, uint32_t (&to)[kWords]) {
     constexpr int kEach = kAlign >= 16 && kWords % 4 == 0 ? 4 : kAlign >= 8 && kWords % 2 == 0 ? 2 : 1;
     typedef uint32_t piece __attribute__((ext_vector_type(kEach)));
@@ -836,7 +835,9 @@ template <typename T> hipError_t launch(Args &a, bool mixed, bool two, uint32_t 
 
 // Many rows pay where what they save is more than their longer start, 7 us: a row of 32 takes 0.76 us for a million keys and heads, one of 128,
 // of which all have to be filled, 0.66 (0.45 and 0.27 at 64 values a head).  (Measured, us a call, few / many, 8 heads of 128: 192 rows, 65,536 keys 89 / 99, 256
-// rows 110 / 106, 512 rows 203 / 187; 512 rows, 8,192 keys 39 / 45, 1,024 rows 64 / 64; heads of 64 34 / 37, 49 / 46.)
+// rows 110 / 106, 512 rows 203 / 187; 512 rows, 8,192 keys 39 / 45, 1,024 rows 64 / 64; heads of 64 34 / 37, 49 / 46.  128 rows, 65,536 keys, heads of 32 / 64 / 96 / 256:
+// 40 / 38, 45 / 42, 58 / 51, 126 / 123; 512 rows 132 / 103, 149 / 119, 192 / 148, 450 / 382; 256 rows, 8,192 keys 18 / 22, 21 / 25, 30 / 30, 48 / 60; 512 rows 28 / 29, 32 / 37, 38 / 42,
+// 72 / 77, where the rule takes the slower one at 256 values alone; 2,048 rows 69 / 58, 78 / 68, 104 / 86, 245 / 223.)
 bool wide_rows(bool, uint64_t rows, uint32_t keys, uint64_t stretches, uint32_t head_dim) {
     const double size = head_dim / 128.0, work = (double)keys * (double)stretches * 1e-6;
     const double few = head_dim > 128 ? 0.95 * size : 0.14 + 0.62 * size, many = head_dim > 128 ? 0.82 * size : std::fmax(0.12, 0.77 * size - 0.12);      // 16 rows a tile beyond 128 values

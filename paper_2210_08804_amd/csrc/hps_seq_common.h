@@ -1,4 +1,4 @@
-// What the two files behind hps_seq.h share.  Not part of the C ABI, and not exported.
+// What the files behind hps_seq.h share.  Not part of the C ABI, and not exported.
 #ifndef HPS_SEQ_COMMON_H
 #define HPS_SEQ_COMMON_H
 

@@ -17,7 +17,8 @@ template <typename T, int E, bool kWithin> __global__ void __launch_bounds__(kNo
 //   dx = r (g - n mean(g n)),
 // so a head takes one pass with two sums.  A work-group goes through tokens with its weights' sums in registers, joins its lanes' in
 // LDS at the end, and a second kernel adds up the work-groups'.  Bound by HBM where there are many (16,384 tokens of 32 heads of 64 of 32 bits,
-// 403 MB moved: 78 us, 5.2 TB/s, and 4.8 of the sums), else by the chain (2,003 of 24 heads of 96 of 16 bits, 28 MB: 10.6 and 3.9).
+// 403 MB moved: 78 us, 5.2 TB/s, and 4.8 of the sums), else by the chain position, angles and rows, sums, store of each token, of which nothing is requested
+// ahead (2,003 of 24 heads of 96 of 16 bits, 28 MB: 10.4 to 11.4 and 3.9).
 template <typename T, int E, bool kWithin> __device__ __forceinline__ void norm_backward(const NormArgs &a, const NormTensor &g, uint32_t which, uint32_t group) {
     constexpr int kPer = E == 1 ? 4 : 1;
     __shared__ float l_sum[kNormThreads][kPer * 2 * E + 1];
