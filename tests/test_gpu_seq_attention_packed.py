@@ -560,7 +560,7 @@ def test_hidden_groups_of_every_head_size(D, dtype):
 @pytest.mark.parametrize("D", [32, 96, 128, 256])
 @pytest.mark.parametrize("kind,H,K,new", [(Packed, 2, 2, 1), (Packed, 16, 1, 9), (Shared, 16, 1, 16)])
 def test_scales_beyond_the_type_of_every_head_size(kind, H, K, new, D):
-    """The same for each of a head's groups, of values and of keys."""
+    """Scale bytes above the type's last one, and 0, in each of a head's groups, of values and of keys."""
     for dtype, last in ((BF, 252), (HF, 140)):
         for group in range(D // 32):
             p = kind(dtype, D, H, K, 16, [(40, 1)], [(new, new)], seed=7)

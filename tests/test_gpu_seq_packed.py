@@ -239,7 +239,7 @@ def test_stream_of_its_own_and_graphs():
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF])
 def test_keys_next_to_a_border_of_the_least_scale(dtype, interleaved):
-    """The same among numbers below 2^-126, of which 32 bits tell less the smaller they are."""
+    """Keys beside the middle of two codes where the scale is the least: numbers below 2^-126, of which 32 bits tell less the smaller they are."""
     middles = torch.tensor([.25, .75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0]) * 2.0 ** -126
     for off in (2.0 ** -22, 2.0 ** -24, 2.0 ** -40, 2.0 ** -49, 0.0):
         for sign in (1, -1):
